@@ -432,6 +432,149 @@ int hscale_quantize(const void *W, int64_t out, int64_t in, float global_scale,
                     const uint8_t *scale_codes, uint8_t *packed_e2m1,
                     hipStream_t stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * A stored layer in use: served beside low-rank adapters, and the adapters
+ * trained on it.  W^ is the layer that hscale_search or hscale_quantize
+ * stored: W^[r, j] = global_scale * l_c * v, with c the group's scale code
+ * and v the signed E2M1 value.
+ *
+ * Unlike above, the entry points of this part keep a token's values to that
+ * token: what is not finite in a row of X or dY, or in the rows of tokens
+ * that are not scored, reaches no other token's result.  Adapters' weights
+ * must be finite where a token of the call uses them.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Low-rank adapters beside a shared layer of `out` x `in`: adapter a adds
+ * alpha[a] * B[a] (A[a] x) to the layer's result for the tokens that use it.
+ */
+typedef struct hscale_adapters {
+    int32_t count;          /* 0 .. 4096; 0: no adapters */
+    int32_t rank;           /* 8 .. 256, a multiple of 8 (smaller ones are padded with zeros) */
+    const void *A;          /* bf16 [count, rank, in], 16-byte aligned */
+    const void *B;          /* bf16 [count, out, rank], 16-byte aligned */
+    const float *alpha;     /* fp32 [count], or NULL for 1 */
+    const int32_t *adapter; /* int32 [tokens]: each token's adapter, any number
+                               outside 0 .. count - 1 for none; NULL: all use 0 */
+} hscale_adapters;
+
+/* Workspace bytes hscale_adapted_linear needs (0 when a size is 0 or invalid;
+ * count = 0 without adapters). */
+size_t hscale_adapted_linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t count, int32_t rank);
+
+/*
+ * Y[t] = W^ X[t] + alpha[a] B[a] (A[a] X[t]), a = adapter[t]: a stored layer
+ * applied to the tokens of many requests, each with an adapter of its own or
+ * none, from one token to many.
+ *
+ * X          bf16 [tokens, in] with rows ldx elements apart, 16-byte aligned
+ *            rows (ldx % 8 == 0); ldx <= 2^21
+ * codes, packed, global_scale   as hscale_output_error
+ * adapters   host struct, read during the call; NULL for none
+ * Y          bf16 [tokens, out] with rows ldy elements apart
+ * workspace  256-byte aligned
+ * tokens <= 2^24, in and out <= 2^21, in % 16 == 0, in > 0.
+ *
+ * Products are bf16 (l_c v is exact in it), sums fp32, in an order that the
+ * sizes fix: the same call gives the same bits.  A[a] X[t] enters the second
+ * product in at least 16 bits; Y is rounded once.
+ */
+int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx, int64_t out, float global_scale,
+                          const uint8_t *scale_codes, const uint8_t *packed_e2m1, const hscale_adapters *adapters,
+                          void *Y, int64_t ldy, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Activations kept in 8 bits for a backward pass.  Per token and block of 128
+ * activations (a row's last block may be shorter), each step rounded to fp32:
+ *   m = max(max |x|, 2^-100),  scale = m * fp32(1 / 127),
+ *   q = round to nearest even of x * (127 / m), in -127 .. 127
+ * which stands for the value bf16(q * scale).
+ *
+ * X      bf16 [tokens, in], rows ldx apart, 16-byte aligned rows; finite
+ * q      int8 [tokens, in], 8-byte aligned
+ * scale  fp32 [tokens, ceil(in / 128)]
+ */
+int hscale_pack_activations(const void *X, int64_t tokens, int64_t in, int64_t ldx, int8_t *q, float *scale,
+                            hipStream_t stream);
+
+/* X[t, j] = bf16(q[t, j] * scale[t, j / 128]), rows of X ldx apart. */
+int hscale_unpack_activations(const int8_t *q, const float *scale, int64_t tokens, int64_t in, void *X, int64_t ldx,
+                              hipStream_t stream);
+
+/* Workspace bytes hscale_adapted_linear_grad needs (0 when a size is 0 or
+ * invalid). */
+size_t hscale_adapted_linear_grad_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t count,
+                                                  int32_t rank);
+
+/*
+ * The gradients of hscale_adapted_linear at the checkpointed activations
+ * x_t = bf16(q scale), with v_t = alpha[a] B[a]^T dY[t], u_t = alpha[a] A[a] x_t:
+ *   dX[t] = W^^T dY[t] + A[a]^T v_t
+ *   dA[a] = sum of v_t x_t^T,  dB[a] = sum of dY[t] u_t^T  over a's tokens
+ * An adapter that no token uses gets zeros.  The layer itself is frozen.
+ *
+ * dY         bf16 [tokens, out], rows lddy <= 2^21 apart (read as it lies if
+ *            its rows are 16-byte aligned and out % 16 == 0, else through a
+ *            copy in the workspace)
+ * q, scale   as hscale_pack_activations writes them
+ * dX         bf16 [tokens, in], rows lddx apart; NULL: not computed
+ * dA, dB     bf16, shaped as A and B; written
+ * tokens = 0 writes zeros to dA and dB.  adapters is required.  Arithmetic
+ * and limits as hscale_adapted_linear; sums over tokens in fp32, in a fixed
+ * order.
+ */
+int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int64_t lddy, const int8_t *q,
+                               const float *scale, int64_t in, float global_scale, const uint8_t *scale_codes,
+                               const uint8_t *packed_e2m1, const hscale_adapters *adapters, void *dX, int64_t lddx,
+                               void *dA, void *dB, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes hscale_token_loss needs (0 when a size is 0 or invalid). */
+size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab);
+
+/*
+ * Softmax cross entropy of each token over a vocabulary, without storing the
+ * logits l = X W^T (bf16 products, fp32 sums):
+ *   lse[t] = log sum_v exp(l[t, v]),  loss[t] = lse[t] - l[t, target[t]]
+ * A target outside 0 .. vocab - 1 marks a token that is not scored: loss 0.
+ *
+ * X          bf16 [tokens, d], rows ldx <= 2^21 apart, 16-byte aligned rows
+ * W          bf16 [vocab, d], 16-byte aligned: the output head
+ * target     int64 [tokens]
+ * loss, lse  fp32 [tokens]
+ * workspace  256-byte aligned
+ * d % 16 == 0, 0 < d <= 2^21; tokens, vocab <= 2^24, tokens x vocab <= 2^38.
+ * Exponentials are taken relative to the running maximum; bitwise
+ * reproducible.
+ */
+int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
+                      const int64_t *target, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
+/* Workspace bytes hscale_token_loss_grad needs (0 when a size is 0 or
+ * invalid). */
+size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab);
+
+/*
+ * Gradient of sum_t weight[t] loss[t] with respect to X and W, from the lse
+ * that hscale_token_loss wrote: with
+ *   g[t, v] = weight[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),
+ * dX = g W and dW = g^T X.  The logits are computed again, a piece of the
+ * vocabulary at a time; g is rounded to bf16 for the two products, whose sums
+ * are fp32.  Tokens that are not scored (target or weight 0) get dX = 0 and
+ * add nothing to dW, whatever their X and lse hold.
+ *
+ * weight     fp32 [tokens]: d(total) / d(loss[t]); 1 / n for a mean over n
+ * dX         bf16 [tokens, d], rows lddx apart (8-byte aligned rows); NULL:
+ *            not computed
+ * dW         bf16 [vocab, d], 8-byte aligned, written; NULL: not computed
+ * tokens = 0 writes zeros to dW.  Other arguments as hscale_token_loss.
+ */
+int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
+                           const int64_t *target, const float *lse, const float *weight, void *dX, int64_t lddx,
+                           void *dW, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

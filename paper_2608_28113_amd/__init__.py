@@ -12,4 +12,6 @@ The compute is in ``libhscale.so`` (hand-written HIP, C ABI in
 from ._lib import HScaleError, EXPORTS  # noqa: F401
 from .ops import (hdiag, hdiag_accumulate, hdiag_finalize, hdiag_noalloc, hdiag_workspace_bytes, quantize,  # noqa: F401
                   output_error, output_error_workspace_bytes, search, search_block, search_layers, search_stats,
-                  shift_summary)
+                  shift_summary, adapted_linear, adapted_linear_workspace_bytes, adapted_linear_grad,
+                  adapted_linear_grad_workspace_bytes, pack_activations, unpack_activations, token_loss,
+                  token_loss_workspace_bytes, token_loss_grad, token_loss_grad_workspace_bytes)

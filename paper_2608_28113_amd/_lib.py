@@ -38,6 +38,16 @@ EXPORTS = (
     "hscale_output_error_least_workspace_bytes",
     "hscale_output_error",
     "hscale_quantize",
+    "hscale_adapted_linear_workspace_bytes",
+    "hscale_adapted_linear",
+    "hscale_pack_activations",
+    "hscale_unpack_activations",
+    "hscale_adapted_linear_grad_workspace_bytes",
+    "hscale_adapted_linear_grad",
+    "hscale_token_loss_workspace_bytes",
+    "hscale_token_loss",
+    "hscale_token_loss_grad_workspace_bytes",
+    "hscale_token_loss_grad",
 )
 
 HSCALE_INIT_MAXABS, HSCALE_INIT_4OVER6, HSCALE_INIT_GIVEN = 0, 1, 2
@@ -48,6 +58,14 @@ class HScaleLayer(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("out", ctypes.c_int64), ("in_", ctypes.c_int64),
                 ("h", ctypes.c_void_p), ("global_scale", ctypes.c_float), ("init_codes", ctypes.c_void_p),
                 ("scale_codes", ctypes.c_void_p), ("packed_e2m1", ctypes.c_void_p)]
+
+
+
+class HScaleAdapters(ctypes.Structure):
+    """struct hscale_adapters of include/hscale.h (natural C layout)."""
+    _fields_ = [("count", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
+                ("alpha", ctypes.c_void_p), ("adapter", ctypes.c_void_p)]
+
 
 _lib = None
 
@@ -106,6 +124,27 @@ def load() -> ctypes.CDLL:
     lib.hscale_output_error_least_workspace_bytes.restype = sz
     lib.hscale_output_error.argtypes = [P, i64, i64, P, i64, f32, P, P, P, P, sz, P]
     lib.hscale_output_error.restype = ctypes.c_int
+    AD = ctypes.POINTER(HScaleAdapters)
+    lib.hscale_adapted_linear_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.hscale_adapted_linear_workspace_bytes.restype = sz
+    lib.hscale_adapted_linear.argtypes = [P, i64, i64, i64, i64, f32, P, P, AD, P, i64, P, sz, P]
+    lib.hscale_adapted_linear.restype = ctypes.c_int
+    lib.hscale_pack_activations.argtypes = [P, i64, i64, i64, P, P, P]
+    lib.hscale_pack_activations.restype = ctypes.c_int
+    lib.hscale_unpack_activations.argtypes = [P, P, i64, i64, P, i64, P]
+    lib.hscale_unpack_activations.restype = ctypes.c_int
+    lib.hscale_adapted_linear_grad_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.hscale_adapted_linear_grad_workspace_bytes.restype = sz
+    lib.hscale_adapted_linear_grad.argtypes = [P, i64, i64, i64, P, P, i64, f32, P, P, AD, P, i64, P, P, P, sz, P]
+    lib.hscale_adapted_linear_grad.restype = ctypes.c_int
+    lib.hscale_token_loss_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.hscale_token_loss_workspace_bytes.restype = sz
+    lib.hscale_token_loss.argtypes = [P, i64, i64, i64, P, i64, P, P, P, P, sz, P]
+    lib.hscale_token_loss.restype = ctypes.c_int
+    lib.hscale_token_loss_grad_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.hscale_token_loss_grad_workspace_bytes.restype = sz
+    lib.hscale_token_loss_grad.argtypes = [P, i64, i64, i64, P, i64, P, P, P, P, i64, P, P, sz, P]
+    lib.hscale_token_loss_grad.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -219,3 +258,66 @@ def hscale_output_error(X: int, tokens: int, in_: int, W: int, out: int, global_
     return load().hscale_output_error(X or None, tokens, in_, W or None, out, global_scale, scale_codes or None,
                                       packed_e2m1 or None, row_err or None, workspace or None, workspace_bytes,
                                       stream or None)
+
+
+def _adapters(adapters):
+    """A pointer to struct hscale_adapters of (count, rank, A, B, alpha, adapter), or NULL for None."""
+    if adapters is None:
+        return None
+    count, rank, *ptrs = adapters
+    return ctypes.byref(HScaleAdapters(count, rank, *(p or None for p in ptrs)))
+
+
+def hscale_adapted_linear_workspace_bytes(tokens: int, in_: int, out: int, count: int, rank: int) -> int:
+    return int(load().hscale_adapted_linear_workspace_bytes(tokens, in_, out, count, rank))
+
+
+def hscale_adapted_linear(X: int, tokens: int, in_: int, ldx: int, out: int, global_scale: float, scale_codes: int,
+                          packed_e2m1: int, adapters, Y: int, ldy: int, workspace: int, workspace_bytes: int,
+                          stream: int) -> int:
+    return load().hscale_adapted_linear(X or None, tokens, in_, ldx, out, global_scale, scale_codes or None,
+                                        packed_e2m1 or None, _adapters(adapters), Y or None, ldy, workspace or None,
+                                        workspace_bytes, stream or None)
+
+
+def hscale_pack_activations(X: int, tokens: int, in_: int, ldx: int, q: int, scale: int, stream: int) -> int:
+    return load().hscale_pack_activations(X or None, tokens, in_, ldx, q or None, scale or None, stream or None)
+
+
+def hscale_unpack_activations(q: int, scale: int, tokens: int, in_: int, X: int, ldx: int, stream: int) -> int:
+    return load().hscale_unpack_activations(q or None, scale or None, tokens, in_, X or None, ldx, stream or None)
+
+
+def hscale_adapted_linear_grad_workspace_bytes(tokens: int, in_: int, out: int, count: int, rank: int) -> int:
+    return int(load().hscale_adapted_linear_grad_workspace_bytes(tokens, in_, out, count, rank))
+
+
+def hscale_adapted_linear_grad(dY: int, tokens: int, out: int, lddy: int, q: int, scale: int, in_: int,
+                               global_scale: float, scale_codes: int, packed_e2m1: int, adapters, dX: int, lddx: int,
+                               dA: int, dB: int, workspace: int, workspace_bytes: int, stream: int) -> int:
+    return load().hscale_adapted_linear_grad(dY or None, tokens, out, lddy, q or None, scale or None, in_,
+                                             global_scale, scale_codes or None, packed_e2m1 or None,
+                                             _adapters(adapters), dX or None, lddx, dA or None, dB or None,
+                                             workspace or None, workspace_bytes, stream or None)
+
+
+def hscale_token_loss_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
+    return int(load().hscale_token_loss_workspace_bytes(tokens, d, vocab))
+
+
+def hscale_token_loss(X: int, tokens: int, d: int, ldx: int, W: int, vocab: int, target: int, loss: int, lse: int,
+                      workspace: int, workspace_bytes: int, stream: int) -> int:
+    return load().hscale_token_loss(X or None, tokens, d, ldx, W or None, vocab, target or None, loss or None,
+                                    lse or None, workspace or None, workspace_bytes, stream or None)
+
+
+def hscale_token_loss_grad_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
+    return int(load().hscale_token_loss_grad_workspace_bytes(tokens, d, vocab))
+
+
+def hscale_token_loss_grad(X: int, tokens: int, d: int, ldx: int, W: int, vocab: int, target: int, lse: int,
+                           weight: int, dX: int, lddx: int, dW: int, workspace: int, workspace_bytes: int,
+                           stream: int) -> int:
+    return load().hscale_token_loss_grad(X or None, tokens, d, ldx, W or None, vocab, target or None, lse or None,
+                                         weight or None, dX or None, lddx, dW or None, workspace or None,
+                                         workspace_bytes, stream or None)

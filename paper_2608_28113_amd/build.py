@@ -16,7 +16,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
-SOURCES = [CSRC / "hdiag.hip", CSRC / "search.hip", CSRC / "diag.hip"]  # share csrc/common.h
+SOURCES = [CSRC / "hdiag.hip", CSRC / "search.hip", CSRC / "diag.hip",  # share csrc/common.h
+           CSRC / "adapt.hip", CSRC / "loss.hip"]  # and csrc/matmul.h
 INCLUDE = ROOT / "include"
 LIB = PKG / "libhscale.so"
 PROBE_SOURCES = [CSRC / "probes.hip"]

@@ -1,0 +1,471 @@
+// Softmax cross entropy of tokens over a large vocabulary, and its gradient,
+// behind the C ABI of include/hscale.h, without keeping the logits:
+//
+//   l_tv = x_t . w_v,  lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t,target
+//   g_tv = weight_t (exp(l_tv - lse_t) - [v = target]),  dX = g W,  dW = g^T X
+//
+// The loss takes one pass of matrix products whose tiles end as a maximum and
+// a sum of exponentials per token; the gradient computes the logits again, a
+// piece of the vocabulary at a time, and only that piece of g is held.
+
+#include "matmul.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int64_t kMaxWidth = (int64_t)1 << 21;   // of a token's vector
+constexpr int64_t kMaxTokens = (int64_t)1 << 24;
+constexpr int64_t kMaxVocab = (int64_t)1 << 24;
+constexpr int64_t kMaxLogits = (int64_t)1 << 38;  // one launch's tiles: below 2^32 threads
+
+typedef Tile<2, 4, 4, 2> Large;   // 256 x 256
+typedef Tile<2, 2, 2, 2> Small;   // 128 x 128
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// (maximum, sum of exponentials relative to it) of two parts; a part without
+// terms is (-inf, 0).
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x);
+    if (m == -INFINITY) return make_float2(m, a.y + b.y);  // keeps the NaN of a part that has one
+    return make_float2(m, a.y * exp_of(a.x - m) + b.y * exp_of(b.x - m));
+}
+
+struct LogitArgs {
+    Operand W, X;            // [vocab, d], [tokens, d]
+    const int64_t *target;   // [tokens]
+    unsigned mtiles;
+    // loss
+    float2 *parts;           // [mtiles, tokens]
+    float *at;               // [tokens]: the target's logit
+    // gradient: vocabulary from v0 on
+    int64_t v0, vocab;       // of the whole
+    const float *lse, *weight;
+    uint16_t *g;             // [tokens, ldg]
+    int64_t ldg;
+};
+
+template <class T>
+__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_tile_kernel(const LogitArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    unsigned mt, nt;
+    tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
+    const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    Acc<T> acc;
+    acc.clear();
+    tile_product<T, Along, Along>(acc, lds, a.W, m0, a.X, n0, 0, a.X.k);
+    const Place<T> at;
+    float2 *red = reinterpret_cast<float2 *>(lds);  // [kWM][kBN]
+    const int words = a.vocab - m0 < T::kBM ? (int)(a.vocab - m0) : T::kBM;
+    const int first = at.m(0, 0);  // element (i, e) is word first + 32 i + 8 (e / 4) + e % 4
+#pragma unroll
+    for (int j = 0; j < T::kNJ; ++j) {
+        const int64_t t = n0 + at.n(j);
+        const int64_t y = t < a.X.rows ? a.target[t] - m0 : -1;
+        const int own = y >= 0 && y < words ? (int)y - first : -1;
+        float2 p = make_float2(-INFINITY, 0.0f);
+        float hit = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int k = 32 * i + 8 * (e >> 2) + (e & 3);
+                if (k < words - first) p.x = fmaxf(p.x, acc.v[i][j][e]);
+                if (k == own) hit = acc.v[i][j][e];
+            }
+        if (own >= 0 && (own & 4) == 0 && own < 32 * T::kMI) a.at[t] = hit;  // the one lane that holds it
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int k = 32 * i + 8 * (e >> 2) + (e & 3);
+                if (k < words - first) p.y += exp_of(acc.v[i][j][e] - p.x);
+            }
+        const float2 o = make_float2(__shfl_xor(p.x, 32, 64), __shfl_xor(p.y, 32, 64));
+        p = join(p, o);
+        if (at.lane < 32) red[at.wm * T::kBN + at.n(j)] = p;
+    }
+    __syncthreads();
+    for (int n = threadIdx.x; n < T::kBN; n += T::kThreads) {
+        if (n0 + n >= a.X.rows) continue;
+        float2 p = red[n];
+#pragma unroll
+        for (int w = 1; w < T::kWM; ++w) p = join(p, red[w * T::kBN + n]);
+        a.parts[(int64_t)mt * a.X.rows + n0 + n] = p;
+    }
+}
+
+// 64 tokens per block, four threads to a token.
+__global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ parts, int64_t tiles, int64_t tokens,
+                                                   const int64_t *__restrict__ target, int64_t vocab,
+                                                   const float *__restrict__ at, float *__restrict__ loss,
+                                                   float *__restrict__ lse) {
+    __shared__ float2 red[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t t = (int64_t)blockIdx.x * 64 + lane;
+    float2 p = make_float2(-INFINITY, 0.0f);
+    if (t < tokens)
+        for (int64_t k = w; k < tiles; k += 4) p = join(p, parts[k * tokens + t]);
+    red[w][lane] = p;
+    __syncthreads();
+    if (w != 0 || t >= tokens) return;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) p = join(p, red[k][lane]);
+    const float l = p.x + logf(p.y);
+    const int64_t y = target[t];
+    lse[t] = l;
+    loss[t] = y >= 0 && y < vocab ? l - at[t] : 0.0f;
+}
+
+// g of a piece of the vocabulary, bf16; zeros where a token is not scored and
+// beyond the vocabulary.
+template <class T>
+__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_slope_kernel(const LogitArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    unsigned mt, nt;
+    tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
+    const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    Acc<T> acc;
+    acc.clear();
+    tile_product<T, Along, Along>(acc, lds, a.W, m0, a.X, n0, 0, a.X.k);
+    const Place<T> at;
+    const int64_t v1 = a.vocab - a.v0 - m0;
+    const int words = v1 < T::kBM ? (int)v1 : T::kBM;
+    const int first = at.m(0, 0);  // element (i, e) is word first + 32 i + 8 (e / 4) + e % 4
+#pragma unroll
+    for (int j = 0; j < T::kNJ; ++j) {
+        const int64_t t = n0 + at.n(j);
+        const bool in = t < a.X.rows;
+        const int64_t y = in ? a.target[t] : -1;
+        const bool scored = y >= 0 && y < a.vocab;
+        const float w = scored ? a.weight[t] : 0.0f, l = in ? a.lse[t] : 0.0f;
+        const int64_t yl = y - a.v0 - m0;
+        const int own = scored && yl >= 0 && yl < words ? (int)yl - first : -1;
+        const int some = w != 0.0f ? words - first : 0;
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int k = 32 * i + 8 * (e >> 2) + (e & 3);
+                const float p = exp_of(acc.v[i][j][e] - l) - (k == own ? 1.0f : 0.0f);
+                acc.v[i][j][e] = k < some ? w * p : 0.0f;
+            }
+    }
+    store_bf16<T>(acc, a.g, a.ldg, m0, a.ldg, n0, a.X.rows, true);
+}
+
+struct DxArgs {
+    Operand W, g;    // W [vocab piece, d] across, g [tokens, piece]
+    unsigned mtiles, tiles;
+    int64_t k_split;
+    bool add;
+    float *sum;      // [splits, tokens, d]
+};
+
+template <class T>
+__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_dx_kernel(const DxArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    unsigned mt, nt;
+    tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
+    const int64_t split = blockIdx.x / a.tiles;
+    const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.g.k ? k0 + a.k_split : a.g.k;
+    Acc<T> acc;
+    acc.clear();
+    if (k0 < k1) tile_product<T, Across, Along>(acc, lds, a.W, m0, a.g, n0, k0, k1);
+    const Place<T> at;
+    float *sum = a.sum + split * a.g.rows * a.W.rows;
+#pragma unroll
+    for (int j = 0; j < T::kNJ; ++j) {
+        const int64_t n = n0 + at.n(j);
+        if (n >= a.g.rows) continue;
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t m = m0 + at.m(i, 4 * q);
+                if (m >= a.W.rows) continue;  // d % 16 == 0: whole fours
+                float4 *dst = reinterpret_cast<float4 *>(sum + n * a.W.rows + m);
+                float4 v = a.add ? *dst : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                v.x += acc.v[i][j][4 * q];
+                v.y += acc.v[i][j][4 * q + 1];
+                v.z += acc.v[i][j][4 * q + 2];
+                v.w += acc.v[i][j][4 * q + 3];
+                *dst = v;
+            }
+    }
+}
+
+__global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int splits, int64_t fours,
+                                                      int64_t d, uint16_t *__restrict__ dX, int64_t lddx) {
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
+        float4 v = sum[id];
+        for (int s = 1; s < splits; ++s) {
+            const float4 o = sum[(int64_t)s * fours + id];
+            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        const int64_t t = id / (d / 4), c = id % (d / 4) * 4;
+        *reinterpret_cast<uint2 *>(dX + t * lddx + c) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+    }
+}
+
+// X with zeros in the rows that are not scored, so that what lies there does
+// not meet the zeros of g in a product.
+__global__ __launch_bounds__(256) void scored_rows(const uint16_t *__restrict__ X, int64_t ldx, int64_t tokens,
+                                                   int64_t d, const int64_t *__restrict__ target,
+                                                   const float *__restrict__ weight, int64_t vocab,
+                                                   u32x4 *__restrict__ S) {
+    const int64_t words = d / 8, total = tokens * words, stride = (int64_t)gridDim.x * 256;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
+        const int64_t t = id / words, c = id - t * words;
+        const int64_t y = target[t];
+        u32x4 v = {0, 0, 0, 0};
+        if (y >= 0 && y < vocab && weight[t] != 0.0f) v = *reinterpret_cast<const u32x4 *>(X + t * ldx + c * 8);
+        S[id] = v;
+    }
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(uint2 *__restrict__ p, int64_t n) {
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < n; id += stride) p[id] = make_uint2(0u, 0u);
+}
+
+struct DwArgs {
+    Operand X, g;    // X [tokens, d] across, g [tokens, piece] across
+    unsigned mtiles;
+    int64_t cols;    // rows of dW in this piece
+    uint16_t *dW;    // [cols, d]
+};
+
+template <class T>
+__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_dw_kernel(const DwArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    unsigned mt, nt;
+    tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
+    const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    Acc<T> acc;
+    acc.clear();
+    tile_product<T, Across, Across>(acc, lds, a.X, m0, a.g, n0, 0, a.g.k);
+    store_bf16<T>(acc, a.dW, a.X.rows, m0, a.X.rows, n0, a.cols, true);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The 256 x 256 tile where its blocks fill the chip at least once.
+inline bool large_tiles(int64_t m, int64_t n) { return cdiv(m, Large::kBM) * cdiv(n, Large::kBN) >= 256; }
+inline int64_t tile_rows(int64_t m, int64_t n) { return large_tiles(m, n) ? Large::kBM : Small::kBM; }
+inline int64_t tile_cols(int64_t m, int64_t n) { return large_tiles(m, n) ? Large::kBN : Small::kBN; }
+
+struct LossPlan {
+    size_t parts, at, total;
+};
+
+LossPlan loss_plan(int64_t tokens, int64_t vocab) {
+    LossPlan p;
+    p.parts = round_up((size_t)cdiv(vocab, tile_rows(vocab, tokens)) * tokens * sizeof(float2), 256);
+    p.at = round_up((size_t)tokens * 4, 256);
+    p.total = p.parts + p.at;
+    return p;
+}
+
+// A piece of g takes up to 512 MB, and at least 2048 of the vocabulary.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+constexpr int64_t kLeastPiece = 2048;
+constexpr int64_t kPieceStep = 256;
+
+struct LossGradPlan {
+    int64_t piece, pieces, k_split;
+    int splits;
+    size_t g, sum, rows, total;
+};
+
+LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
+    LossGradPlan p;
+    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (2 * tokens) / kPieceStep * kPieceStep);
+    p.pieces = cdiv(vocab, fit);
+    p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
+    p.pieces = cdiv(vocab, p.piece);
+    const int64_t blocks = cdiv(d, tile_rows(d, tokens)) * cdiv(tokens, tile_cols(d, tokens));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / blocks, cdiv(p.piece, 512)));
+    p.k_split = cdiv(cdiv(p.piece, want), kStageK) * kStageK;
+    p.splits = (int)cdiv(p.piece, p.k_split);
+    p.g = round_up((size_t)tokens * p.piece * 2, 256);
+    p.sum = round_up((size_t)p.splits * tokens * d * 4, 256);
+    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
+    p.total = p.g + p.sum + p.rows;
+    return p;
+}
+
+bool loss_sizes_ok(int64_t tokens, int64_t d, int64_t vocab) {
+    return tokens >= 0 && tokens <= kMaxTokens && d >= 0 && d % 16 == 0 && d <= kMaxWidth && vocab >= 0 &&
+           vocab <= kMaxVocab && tokens * vocab <= kMaxLogits;
+}
+
+struct Range {
+    const void *p;
+    size_t n;
+};
+
+bool any_overlap(const Range *w, int nw, const Range *r, int nr) {
+    for (int i = 0; i < nw; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlaps(w[i].p, w[i].n, w[j].p, w[j].n)) return true;
+        for (int j = 0; j < nr; ++j)
+            if (overlaps(w[i].p, w[i].n, r[j].p, r[j].n)) return true;
+    }
+    return false;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) {
+    if (!loss_sizes_ok(tokens, d, vocab) || tokens == 0 || d == 0 || vocab == 0) return 0;
+    return loss_plan(tokens, vocab).total;
+}
+
+int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
+                      const int64_t *target, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream) {
+    if (!loss_sizes_ok(tokens, d, vocab) || (tokens > 1 && (ldx < d || ldx > kMaxWidth))) return HSCALE_ERR_SHAPE;
+    if (tokens == 0) return HSCALE_OK;
+    if (d == 0 || vocab == 0) return HSCALE_ERR_SHAPE;
+    if (!X || !W || !target || !loss || !lse || !workspace) return HSCALE_ERR_NULL;
+    if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(W, 16) || !aligned(target, 8) ||
+        !aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 256))
+        return HSCALE_ERR_ALIGN;
+    const LossPlan p = loss_plan(tokens, vocab);
+    if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+    const Range w[] = {{loss, (size_t)tokens * 4}, {lse, (size_t)tokens * 4}, {workspace, p.total}};
+    const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8}};
+    if (any_overlap(w, 3, r, 3)) return HSCALE_ERR_OVERLAP;
+    LogitArgs a{};
+    a.W = Operand{W, d, vocab, d};
+    a.X = Operand{X, ldx, tokens, d};
+    a.target = target;
+    a.parts = static_cast<float2 *>(workspace);
+    a.at = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.parts);
+    a.vocab = vocab;
+    a.mtiles = (unsigned)cdiv(vocab, tile_rows(vocab, tokens));
+    const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_cols(vocab, tokens))));
+    if (large_tiles(vocab, tokens))
+        hipLaunchKernelGGL((loss_tile_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((loss_tile_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
+    if (const int st = launch_status()) return st;
+    hipLaunchKernelGGL(loss_finish, dim3((unsigned)cdiv(tokens, 64)), dim3(256), 0, stream, a.parts,
+                       (int64_t)a.mtiles, tokens, target, vocab, a.at, loss, lse);
+    return launch_status();
+}
+
+size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) {
+    if (!loss_sizes_ok(tokens, d, vocab) || tokens == 0 || d == 0 || vocab == 0) return 0;
+    return loss_grad_plan(tokens, d, vocab, true).total;
+}
+
+int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
+                           const int64_t *target, const float *lse, const float *weight, void *dX, int64_t lddx,
+                           void *dW, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!loss_sizes_ok(tokens, d, vocab) ||
+        (tokens > 1 && (ldx < d || ldx > kMaxWidth || (dX && lddx < d))))
+        return HSCALE_ERR_SHAPE;
+    if (tokens == 0 && (!dW || d == 0 || vocab == 0)) return HSCALE_OK;
+    if (d == 0 || vocab == 0) return HSCALE_ERR_SHAPE;
+    if (tokens == 0) {
+        if (!aligned(dW, 8)) return HSCALE_ERR_ALIGN;
+        hipLaunchKernelGGL(clear_kernel, dim3(grid_for(vocab * d / 4, 256)), dim3(256), 0, stream,
+                           static_cast<uint2 *>(dW), vocab * d / 4);
+        return launch_status();
+    }
+    if (!X || !W || !target || !lse || !weight || !workspace) return HSCALE_ERR_NULL;
+    if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(W, 16) || !aligned(target, 8) ||
+        !aligned(lse, 4) || !aligned(weight, 4) || !aligned(dX, 8) || (dX && tokens > 1 && lddx % 4 != 0) ||
+        !aligned(dW, 8) || !aligned(workspace, 256))
+        return HSCALE_ERR_ALIGN;
+    const LossGradPlan p = loss_grad_plan(tokens, d, vocab, dW != nullptr);
+    if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+    const Range w[] = {{dX, dX ? span(tokens, lddx, d, 2) : 0}, {dW, dW ? (size_t)vocab * d * 2 : 0},
+                       {workspace, p.total}};
+    const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8},
+                       {lse, (size_t)tokens * 4}, {weight, (size_t)tokens * 4}};
+    if (any_overlap(w, 3, r, 5)) return HSCALE_ERR_OVERLAP;
+
+    char *ws = static_cast<char *>(workspace);
+    uint16_t *g = reinterpret_cast<uint16_t *>(ws);
+    float *sum = reinterpret_cast<float *>(ws + p.g);
+    u32x4 *rows = reinterpret_cast<u32x4 *>(ws + p.g + p.sum);
+    if (dW) {
+        hipLaunchKernelGGL(scored_rows, dim3(grid_for(tokens * d / 8, 256)), dim3(256), 0, stream,
+                           static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, rows);
+        if (const int st = launch_status()) return st;
+    }
+    for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
+        const int64_t cols = std::min(p.piece, vocab - v0), ldg = cdiv(cols, kPieceStep) * kPieceStep;
+        const uint16_t *Wp = static_cast<const uint16_t *>(W) + v0 * d;
+        LogitArgs a{};
+        a.W = Operand{Wp, d, cols, d};
+        a.X = Operand{X, ldx, tokens, d};
+        a.target = target;
+        a.v0 = v0;
+        a.vocab = vocab;
+        a.lse = lse;
+        a.weight = weight;
+        a.g = g;
+        a.ldg = ldg;
+        a.mtiles = (unsigned)(ldg / tile_rows(cols, tokens));
+        const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_cols(cols, tokens))));
+        if (large_tiles(cols, tokens))
+            hipLaunchKernelGGL((loss_slope_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL((loss_slope_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
+        if (const int st = launch_status()) return st;
+        if (dX) {
+            DxArgs x{};
+            x.W = Operand{Wp, d, d, cols};
+            x.g = Operand{g, ldg, tokens, ldg};
+            x.mtiles = (unsigned)cdiv(d, tile_rows(d, tokens));
+            x.tiles = (unsigned)(x.mtiles * cdiv(tokens, tile_cols(d, tokens)));
+            x.k_split = p.k_split;
+            x.add = v0 > 0;
+            x.sum = sum;
+            const dim3 blocks(x.tiles * (unsigned)p.splits);
+            if (large_tiles(d, tokens))
+                hipLaunchKernelGGL((loss_dx_kernel<Large>), blocks, dim3(Large::kThreads), 0, stream, x);
+            else
+                hipLaunchKernelGGL((loss_dx_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, x);
+            if (const int st = launch_status()) return st;
+        }
+        if (dW) {
+            DwArgs b{};
+            b.X = Operand{rows, d, d, tokens};
+            b.g = Operand{g, ldg, ldg, tokens};
+            b.mtiles = (unsigned)cdiv(d, tile_rows(d, cols));
+            b.cols = cols;
+            b.dW = static_cast<uint16_t *>(dW) + v0 * d;
+            const dim3 blocks((unsigned)(b.mtiles * cdiv(cols, tile_cols(d, cols))));
+            if (large_tiles(d, cols))
+                hipLaunchKernelGGL((loss_dw_kernel<Large>), blocks, dim3(Large::kThreads), 0, stream, b);
+            else
+                hipLaunchKernelGGL((loss_dw_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, b);
+            if (const int st = launch_status()) return st;
+        }
+    }
+    if (dX) {
+        const int64_t fours = tokens * d / 4;
+        hipLaunchKernelGGL(loss_dx_finish, dim3(grid_for(fours, 256)), dim3(256), 0, stream,
+                           reinterpret_cast<const float4 *>(sum), p.splits, fours, d, static_cast<uint16_t *>(dX),
+                           lddx);
+        return launch_status();
+    }
+    return HSCALE_OK;
+}
+
+}  // extern "C"

@@ -384,3 +384,219 @@ def output_error(X: torch.Tensor, W: torch.Tensor, global_scale: float, scale_co
                  scale_codes.data_ptr(), packed_e2m1.data_ptr(), row_err.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_output_error")
     return row_err
+
+
+# ---------------------------------------------------------------------------
+# A stored layer in use
+# ---------------------------------------------------------------------------
+
+CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
+
+
+def _rows_in(t, name: str) -> int:
+    """t is a 2-D bf16 CUDA view with unit column stride; its row stride."""
+    if not _on_device(t) or t.dtype != torch.bfloat16 or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D bf16 CUDA tensor")
+    return _row_view(t, torch.bfloat16, t.shape, t.device, name)
+
+
+def _rows_out(t, name: str, shape, device) -> tuple[torch.Tensor, int]:
+    """A caller-provided bf16 view of rows (checked) or a new tensor, and its row stride."""
+    if t is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=device), shape[1]
+    return t, _row_view(t, torch.bfloat16, shape, device, name)
+
+
+def _stored(scale_codes, packed_e2m1, n: int, device) -> int:
+    """The stored layer's tensors, for `n` inputs; its outputs."""
+    if not isinstance(packed_e2m1, torch.Tensor) or packed_e2m1.dim() != 2:
+        raise ValueError("packed_e2m1 must be a 2-D uint8 tensor")
+    m = packed_e2m1.shape[0]
+    _tensor(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), device)
+    _tensor(scale_codes, "scale_codes", torch.uint8, (m, n // 16), device)
+    return m
+
+
+def _adapters(A, B, alpha, adapter, tokens: int, n: int, m: int, device):
+    """The adapters' checked (count, rank, pointers...) for the library, or None."""
+    if A is None or B is None:
+        if not (A is None and B is None and alpha is None and adapter is None):
+            raise ValueError("alpha and adapter need both A and B")
+        return None
+    if not isinstance(A, torch.Tensor) or A.dim() != 3:
+        raise ValueError("A must be a 3-D bf16 tensor [adapters, rank, in]")
+    count, rank = A.shape[0], A.shape[1]
+    _tensor(A, "A", torch.bfloat16, (count, rank, n), device)
+    _tensor(B, "B", torch.bfloat16, (count, m, rank), device)
+    if alpha is not None:
+        _tensor(alpha, "alpha", torch.float32, (count,), device)
+    if adapter is not None:
+        _tensor(adapter, "adapter", torch.int32, (tokens,), device)
+    elif count != 1:
+        raise ValueError("adapter (int32, one number a token) is required unless there is exactly one adapter")
+    return (count, rank, A.data_ptr(), B.data_ptr(), 0 if alpha is None else alpha.data_ptr(),
+            0 if adapter is None else adapter.data_ptr())
+
+
+def adapted_linear_workspace_bytes(tokens: int, in_features: int, out_features: int, adapters: int = 0,
+                                   rank: int = 0) -> int:
+    """Bytes of scratch adapted_linear needs."""
+    return _lib.hscale_adapted_linear_workspace_bytes(tokens, in_features, out_features, adapters, rank)
+
+
+def adapted_linear(X: torch.Tensor, global_scale: float, scale_codes: torch.Tensor, packed_e2m1: torch.Tensor,
+                   A: torch.Tensor | None = None, B: torch.Tensor | None = None, alpha: torch.Tensor | None = None,
+                   adapter: torch.Tensor | None = None, Y: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Y = X W^T of a stored NVFP4 layer, and each token's low-rank adapter
+    beside it: Y[t] += alpha[a] B[a] (A[a] X[t]), a = adapter[t].
+
+    X is bf16 [tokens, in] (rows may be strided, 16-byte aligned), Y bf16
+    [tokens, out] (rows may be strided).  A is bf16 [adapters, rank, in], B
+    bf16 [adapters, out, rank] (rank a multiple of 8 up to 256), alpha fp32
+    [adapters] (1 when None), adapter int32 [tokens], where a number outside
+    0 .. adapters - 1 means none; with one adapter it may be None: all use it.
+    """
+    ldx = _rows_in(X, "X")
+    T, n = X.shape
+    dev = X.device
+    m = _stored(scale_codes, packed_e2m1, n, dev)
+    ad = _adapters(A, B, alpha, adapter, T, n, m, dev)
+    Y, ldy = _rows_out(Y, "Y", (T, m), dev)
+    need = adapted_linear_workspace_bytes(T, n, m, *(ad[:2] if ad else (0, 0)))
+    ws_ptr, ws_bytes = _workspace(workspace, need, dev)
+    _check(_call(dev, _lib.hscale_adapted_linear, X.data_ptr(), T, n, ldx, m, float(global_scale),
+                 scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad, Y.data_ptr(), ldy, ws_ptr, ws_bytes,
+                 _stream(stream, dev)), "hscale_adapted_linear")
+    return Y
+
+
+def pack_activations(X: torch.Tensor, q: torch.Tensor | None = None, scale: torch.Tensor | None = None, stream=None):
+    """A checkpoint of bf16 X [tokens, in] (rows may be strided) in 8 bits:
+    (q int8 [tokens, in], scale fp32 [tokens, ceil(in / 128)])."""
+    ldx = _rows_in(X, "X")
+    T, n = X.shape
+    dev = X.device
+    q = _out(q, "q", torch.int8, (T, n), dev)
+    scale = _out(scale, "scale", torch.float32, (T, -(-n // CHECKPOINT_BLOCK)), dev)
+    _check(_call(dev, _lib.hscale_pack_activations, X.data_ptr(), T, n, ldx, q.data_ptr(), scale.data_ptr(),
+                 _stream(stream, dev)), "hscale_pack_activations")
+    return q, scale
+
+
+def _checkpoint(q, scale) -> tuple[int, int]:
+    """The checked checkpoint's (tokens, in)."""
+    if not _on_device(q) or q.dtype != torch.int8 or q.dim() != 2 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous 2-D int8 CUDA tensor")
+    T, n = q.shape
+    _tensor(scale, "scale", torch.float32, (T, -(-n // CHECKPOINT_BLOCK)), q.device)
+    return T, n
+
+
+def unpack_activations(q: torch.Tensor, scale: torch.Tensor, X: torch.Tensor | None = None, stream=None):
+    """The bf16 [tokens, in] values that a checkpoint stands for."""
+    T, n = _checkpoint(q, scale)
+    dev = q.device
+    X, ldx = _rows_out(X, "X", (T, n), dev)
+    _check(_call(dev, _lib.hscale_unpack_activations, q.data_ptr(), scale.data_ptr(), T, n, X.data_ptr(), ldx,
+                 _stream(stream, dev)), "hscale_unpack_activations")
+    return X
+
+
+def adapted_linear_grad_workspace_bytes(tokens: int, in_features: int, out_features: int, adapters: int,
+                                        rank: int) -> int:
+    """Bytes of scratch adapted_linear_grad needs."""
+    return _lib.hscale_adapted_linear_grad_workspace_bytes(tokens, in_features, out_features, adapters, rank)
+
+
+def adapted_linear_grad(dY: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, global_scale: float,
+                        scale_codes: torch.Tensor, packed_e2m1: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                        alpha: torch.Tensor | None = None, adapter: torch.Tensor | None = None,
+                        dX: torch.Tensor | None = None, dA: torch.Tensor | None = None,
+                        dB: torch.Tensor | None = None, need_dX: bool = True, workspace: torch.Tensor | None = None,
+                        stream=None):
+    """Gradients (dX, dA, dB) of adapted_linear, all bf16, at the checkpoint
+    (q, scale) that pack_activations made of its X, from dY bf16 [tokens, out]
+    (rows may be strided).  The stored layer is frozen.  need_dX=False skips
+    dX (None is returned for it)."""
+    lddy = _rows_in(dY, "dY")
+    T, m = dY.shape
+    dev = dY.device
+    if _checkpoint(q, scale)[0] != T or q.device != dev:
+        raise ValueError(f"the checkpoint must have dY's {T} tokens, on {dev}")
+    n = q.shape[1]
+    if _stored(scale_codes, packed_e2m1, n, dev) != m:
+        raise ValueError(f"the stored layer must have dY's {m} outputs")
+    ad = _adapters(A, B, alpha, adapter, T, n, m, dev)
+    if ad is None:
+        raise ValueError("A and B are required")
+    if not need_dX and dX is not None:
+        raise ValueError("dX given although need_dX is False")
+    dX, lddx = _rows_out(dX, "dX", (T, n), dev) if need_dX else (None, n)
+    dA = _out(dA, "dA", torch.bfloat16, A.shape, dev)
+    dB = _out(dB, "dB", torch.bfloat16, B.shape, dev)
+    ws_ptr, ws_bytes = _workspace(workspace, adapted_linear_grad_workspace_bytes(T, n, m, *ad[:2]), dev)
+    _check(_call(dev, _lib.hscale_adapted_linear_grad, dY.data_ptr(), T, m, lddy, q.data_ptr(), scale.data_ptr(), n,
+                 float(global_scale), scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad,
+                 0 if dX is None else dX.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr(), ws_ptr, ws_bytes,
+                 _stream(stream, dev)), "hscale_adapted_linear_grad")
+    return dX, dA, dB
+
+
+def token_loss_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
+    """Bytes of scratch token_loss needs."""
+    return _lib.hscale_token_loss_workspace_bytes(tokens, d, vocab)
+
+
+def _head(X, W, target) -> None:
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("W must be a 2-D bf16 tensor [vocab, d]")
+    _tensor(W, "W", torch.bfloat16, (W.shape[0], X.shape[1]), X.device)
+    _tensor(target, "target", torch.int64, (X.shape[0],), X.device)
+
+
+def token_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: torch.Tensor | None = None,
+               lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Softmax cross entropy of each token over the vocabulary, without the
+    logits X W^T in memory: (loss, lse), fp32 [tokens].  X is bf16 [tokens, d]
+    (rows may be strided), W bf16 [vocab, d], target int64 [tokens]; a target
+    outside 0 .. vocab - 1 is not scored (loss 0)."""
+    ldx = _rows_in(X, "X")
+    T, d = X.shape
+    dev = X.device
+    _head(X, W, target)
+    loss = _out(loss, "loss", torch.float32, (T,), dev)
+    lse = _out(lse, "lse", torch.float32, (T,), dev)
+    ws_ptr, ws_bytes = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev)
+    _check(_call(dev, _lib.hscale_token_loss, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0], target.data_ptr(),
+                 loss.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)), "hscale_token_loss")
+    return loss, lse
+
+
+def token_loss_grad_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
+    """Bytes of scratch token_loss_grad needs."""
+    return _lib.hscale_token_loss_grad_workspace_bytes(tokens, d, vocab)
+
+
+def token_loss_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, weight: torch.Tensor,
+                    dX: torch.Tensor | None = None, dW: torch.Tensor | None = None, need_dX: bool = True,
+                    need_dW: bool = True, workspace: torch.Tensor | None = None, stream=None):
+    """(dX, dW), bf16, of sum_t weight[t] loss[t], from the lse of token_loss
+    on the same X, W and target.  weight is fp32 [tokens] (1 / n for a mean
+    over n tokens).  What is not needed is not computed (None)."""
+    ldx = _rows_in(X, "X")
+    T, d = X.shape
+    dev = X.device
+    _head(X, W, target)
+    _tensor(lse, "lse", torch.float32, (T,), dev)
+    _tensor(weight, "weight", torch.float32, (T,), dev)
+    if (not need_dX and dX is not None) or (not need_dW and dW is not None):
+        raise ValueError("an output was given that is not needed")
+    dX, lddx = _rows_out(dX, "dX", (T, d), dev) if need_dX else (None, d)
+    dW = _out(dW, "dW", torch.bfloat16, tuple(W.shape), dev) if need_dW else None
+    ws_ptr, ws_bytes = _workspace(workspace, token_loss_grad_workspace_bytes(T, d, W.shape[0]), dev)
+    _check(_call(dev, _lib.hscale_token_loss_grad, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0],
+                 target.data_ptr(), lse.data_ptr(), weight.data_ptr(), 0 if dX is None else dX.data_ptr(), lddx,
+                 0 if dW is None else dW.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)),
+           "hscale_token_loss_grad")
+    return dX, dW
