@@ -8,9 +8,9 @@
 //   dx_t = s_g W^T dy_t + A_a^T v_t
 //   dA_a = sum_t v_t x_t^T,      dB_a = sum_t dy_t u_t^T     over its tokens
 //
-// W^ without s_g is exact in bf16 (an E2M1 value has 2 significant bits, an
-// E4M3 scale 4), so the products with W^ are bf16 products accumulated in
-// fp32, and s_g multiplies the sum.  u and v are kept as two bf16 parts
+// An E2M1 value has 2 significant bits and an E4M3 scale 4, so with the power
+// of two of s_g = f 2^e (1 <= f < 2) W^ is exact in bf16: the products with W^
+// are bf16 products accumulated in fp32, and f multiplies the sum.  u and v are kept as two bf16 parts
 // (within 2^-16), so that nothing of the adapters' part is rounded to 8 bits
 // before the result is.
 
@@ -63,13 +63,13 @@ __device__ __forceinline__ u32x4 stored_eight(uint32_t src, float l) {
     return u32x4{stored_pair<0>(src, l), stored_pair<1>(src, l), stored_pair<2>(src, l), stored_pair<3>(src, l)};
 }
 
-// W^ [groups * 16] without s_g, one group per thread.
+// W^ [groups * 16] with 2^e in place of s_g, one group per thread.
 __global__ __launch_bounds__(256) void stored_to_bf16(const uint8_t *__restrict__ codes,
-                                                      const uint2 *__restrict__ packed, int64_t groups,
+                                                      const uint2 *__restrict__ packed, int64_t groups, float two_e,
                                                       u32x4 *__restrict__ W) {
     const int64_t stride = (int64_t)gridDim.x * 256;
     for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += stride) {
-        const float l = e4m3fn_value(codes[g]);
+        const float l = e4m3fn_value(codes[g]) * two_e;
         const uint2 p = packed[g];
         W[2 * g] = stored_eight(p.x, l);
         W[2 * g + 1] = stored_eight(p.y, l);
@@ -236,11 +236,12 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs a, int slo
     }
 }
 
-// alpha times the sum of the splits, as two bf16 parts: low[t, j] and
+// alpha / f times the sum of the splits (f multiplies the result that takes it),
+// or alpha times it, as two bf16 parts: low[t, j] and
 // low[t, rank_pad + j].  Tokens without an adapter are left as they are; what
 // reads `low` skips them.
 __global__ __launch_bounds__(256) void shrink_finish(const float *__restrict__ partial, int splits, int64_t tokens,
-                                                     int rank, int rank_pad, const float *__restrict__ alpha,
+                                                     int rank, int rank_pad, const float *__restrict__ alpha, float f,
                                                      const int32_t *__restrict__ ids, int count,
                                                      uint16_t *__restrict__ low) {
     const int64_t total = tokens * rank_pad, stride = (int64_t)gridDim.x * 256;
@@ -253,6 +254,7 @@ __global__ __launch_bounds__(256) void shrink_finish(const float *__restrict__ p
         if (j < rank) {
             for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + id];
             if (alpha) v *= alpha[a];
+            v /= f;
         }
         const uint32_t hi = bf16_rne(v);
         low[t * 2 * rank_pad + j] = (uint16_t)hi;
@@ -273,74 +275,87 @@ struct LowRank {
     const int32_t *ids;
 };
 
-// acc += for each token n of the tile, other_a (low_n): k runs over the rank
+// The stages that add other_a (low_n) for the tokens n of a tile to its
+// products: for each adapter that the tile's tokens have, k runs over the rank
 // twice, once for each part of low.  Tokens of other adapters enter as zeros.
 template <class T, Layout LP>
-__device__ __forceinline__ void low_rank_product(Acc<T> &acc, uint8_t *lds, const LowRank &w, int64_t m0,
-                                                 int64_t rows, int64_t n0, int64_t tokens) {
-    using SP = Stage<LP, T::kBM, T::kWaves>;
-    using SQ = Stage<Along, T::kBN, T::kWaves>;
-    const Place<T> at;
-    const int wave = at.wm + at.wn * T::kWM, lane = at.lane;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
-    const int64_t n1 = n0 + T::kBN < tokens ? n0 + T::kBN : tokens;
-    const int deep = 2 * w.rank_pad;
-    const u32x4 rq = raw_buffer(w.low + n0 * deep, (n1 - n0) * deep * 2);
-    for (int a = -1;;) {
-        a = next_adapter(w.ids, w.count, n0, n1, a);
-        if (a == INT_MAX) break;
-        const uint16_t *P = w.other + (int64_t)a * w.other_size + (LP == Along ? m0 * w.ld : m0);
-        const int64_t prows = rows - m0 < T::kBM ? rows - m0 : T::kBM;
-        const u32x4 rp = raw_buffer(P, LP == Along ? ((prows - 1) * w.ld + w.rank) * 2
-                                                   : ((w.rank - 1) * w.ld + prows) * 2);
-        for (int s = 0; s < deep; s += kStageK) {
+struct LowRankStages {
+    static constexpr bool kAny = true;
+    using SP = Stage<LP, T::kBM, T::kWaves, T::kK>;
+    using SQ = Stage<Along, T::kBN, T::kWaves, T::kK>;
+    int stages;
+
+    const LowRank &w;
+    int64_t m0, prows, n0, n1;
+    int wave, lane;
+    int tile[T::kBN / 64];       // adapters of the tile's tokens, over the wave
+    int copied[SQ::kCopies];     // of the rows that this lane copies
+    int adapter = -1, step = 0;  // of the next stage
+
+    __device__ __forceinline__ LowRankStages(const LowRank &low, int64_t m, int64_t rows, int64_t n, int64_t tokens)
+        : stages(0), w(low), m0(m), prows(rows - m < T::kBM ? rows - m : T::kBM), n0(n),
+          n1(n + T::kBN < tokens ? n + T::kBN : tokens) {
+        const Place<T> at;
+        wave = at.wm + at.wn * T::kWM;
+        lane = at.lane;
+        if (!w.low) return;
 #pragma unroll
-            for (int i = 0; i < SP::kCopies; ++i) {
-                const int row = (wave + i * T::kWaves) * (64 / SP::kLanesPerRow) + lane / SP::kLanesPerRow;
-                const int pos = lane % SP::kLanesPerRow;
-                uint32_t off;
-                if (LP == Along) {
-                    const int k = s + (pos ^ ((row >> 1) & 7)) * 8, j = k >= w.rank_pad ? k - w.rank_pad : k;
-                    off = row < prows && k < deep && j < w.rank ? (uint32_t)(row * w.ld * 2 + j * 2) : kNoRead;
-                } else {
-                    const int k = s + row, j = k >= w.rank_pad ? k - w.rank_pad : k;
-                    const int col = ((((pos >> 2) ^ SP::across_swizzle(row)) << 2) | (pos & 3)) * 8;
-                    off = col < prows && k < deep && j < w.rank ? (uint32_t)(j * w.ld * 2 + col * 2) : kNoRead;
-                }
-                copy_to_lds(rp, off, lds0 + i * T::kWaves * 1024);
-            }
+        for (int i = 0; i < T::kBN / 64; ++i) tile[i] = of(i * 64 + lane);
 #pragma unroll
-            for (int i = 0; i < SQ::kCopies; ++i) {
-                const int row = (wave + i * T::kWaves) * 8 + (lane >> 3);
-                const int k = s + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
-                const bool ok = n0 + row < n1 && k < deep && adapter_of(w.ids, w.count, n0 + row) == a;
-                copy_to_lds(rq, ok ? (uint32_t)((row * deep + k) * 2) : kNoRead,
-                            lds0 + SP::kBytes + i * T::kWaves * 1024);
-            }
-            wait_and_barrier();
+        for (int i = 0; i < SQ::kCopies; ++i) copied[i] = of(SQ::row_of(i, wave, lane));
+        for (int a = next(-1); a != INT_MAX; a = next(a)) stages += per_adapter();
+    }
+    __device__ __forceinline__ int of(int row) const {
+        return n0 + row < n1 ? adapter_of(w.ids, w.count, n0 + row) : kNoAdapter;
+    }
+    __device__ __forceinline__ int per_adapter() const { return (2 * w.rank_pad + T::kK - 1) / T::kK; }
+    __device__ __forceinline__ int next(int after) const {
+        int least = INT_MAX;
 #pragma unroll
-            for (int kk = 0; kk < kStageK / 16; ++kk) {
-                bf16x8 fp[T::kMI], fq[T::kNJ];
+        for (int i = 0; i < T::kBN / 64; ++i)
+            if (tile[i] > after) least = min(least, tile[i]);
 #pragma unroll
-                for (int i = 0; i < T::kMI; ++i)
-                    fp[i] = SP::read(lds, SP::read_offset((at.wm * T::kMI + i) * 32, kk, lane));
+        for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+        return __builtin_amdgcn_readfirstlane(least);
+    }
+    // Column of the adapter's rank that k of its stages stands for, or none.
+    __device__ __forceinline__ int column(int k) const {
+        const int j = k >= w.rank_pad ? k - w.rank_pad : k;
+        return k < 2 * w.rank_pad && j < w.rank ? j : -1;
+    }
+    __device__ __forceinline__ void set(SP &sp, SQ &sq, bool some) {
+        if (!some) {  // stages past the last
+            sp.left = sq.left = 0;
+            return;
+        }
+        if (step == 0) adapter = next(adapter);
+        const int k0 = step * T::kK, deep = 2 * w.rank_pad;
+        step = step + 1 == per_adapter() ? 0 : step + 1;
+        const uint16_t *P = w.other + (int64_t)adapter * w.other_size + (LP == Along ? m0 * w.ld : m0);
+        sp.base = reinterpret_cast<const char *>(P);
+        sp.left = LP == Along ? ((prows - 1) * w.ld + w.rank) * 2 : ((w.rank - 1) * w.ld + prows) * 2;
+        sq.base = reinterpret_cast<const char *>(w.low + n0 * deep);
+        sq.left = (n1 - n0) * deep * 2;
+        sp.k_left = sq.k_left = INT_MAX;
 #pragma unroll
-                for (int j = 0; j < T::kNJ; ++j)
-                    fq[j] = SQ::read(lds + SP::kBytes, SQ::read_offset((at.wn * T::kNJ + j) * 32, kk, lane));
+        for (int i = 0; i < SP::kCopies; ++i) {
+            const int row = SP::row_of(i, wave, lane), c = SP::at(row, lane);
+            const int j = column(LP == Along ? k0 + c * 8 : k0 + row);
+            const bool ok = j >= 0 && (LP == Along ? row : c * 8) < prows;
+            const int64_t at = LP == Along ? row * w.ld + j : j * w.ld + c * 8;
+            sp.off[i] = ok ? (uint32_t)(at * 2) : kNoRead;
+        }
 #pragma unroll
-                for (int i = 0; i < T::kMI; ++i)
-#pragma unroll
-                    for (int j = 0; j < T::kNJ; ++j)
-                        acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc.v[i][j], 0, 0, 0);
-            }
-            wait_and_barrier();
+        for (int i = 0; i < SQ::kCopies; ++i) {
+            const int row = SQ::row_of(i, wave, lane), k = k0 + SQ::at(row, lane) * 8;
+            sq.off[i] = k < deep && copied[i] == adapter ? (uint32_t)((row * deep + k) * 2) : kNoRead;
         }
     }
-}
+};
 
 struct LayerArgs {
     Operand W, X;  // m: the layer's other side, n: tokens
-    float s_g;
+    float scale;
     LowRank low;   // low.low NULL: no adapters
     uint16_t *Y;   // [tokens, m] at ldy
     int64_t ldy;
@@ -349,17 +364,16 @@ struct LayerArgs {
 };
 
 template <class T, Layout LW>
-__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void layer_kernel(const LayerArgs a) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void layer_kernel(const LayerArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
     const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
     Acc<T> acc;
     acc.clear();
-    tile_product<T, LW, Along>(acc, lds, a.W, m0, a.X, n0, 0, a.X.k);
-    acc.scale(a.s_g);
-    if (a.low.low) low_rank_product<T, LW>(acc, lds, a.low, m0, a.W.rows, n0, a.X.rows);
-    store_bf16<T>(acc, a.Y, a.ldy, m0, a.W.rows, n0, a.X.rows, a.wide);
+    tile_product<T, LW, Along>(acc, lds, a.W, m0, a.X, n0, 0, a.X.k,
+                               LowRankStages<T, LW>(a.low, m0, a.W.rows, n0, a.X.rows));
+    store_bf16<T>(acc, lds, a.Y, a.ldy, m0, a.W.rows, n0, a.X.rows, a.wide, a.scale);
 }
 
 // ---------------------------------------------------------------------------
@@ -485,15 +499,15 @@ struct OuterArgs {
     float *partial;       // [splits, count, rank, width]
 };
 
-constexpr int kOuterCols = 128;
+constexpr int kOuterCols = 128, kOuterTokens = 64;
 
 // 128 columns x 32 ranks of one adapter x one split of the tokens.  Stages of
 // 64 tokens, laid out as Stage<Across>; tokens of other adapters are not
 // read and enter as zeros, stages without any are skipped.
 template <bool kCheckpoint>
 __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
-    using SZ = Stage<Across, kOuterCols, 4>;
-    using SL = Stage<Across, 64, 4>;
+    using SZ = Stage<Across, kOuterCols, 4, kOuterTokens>;
+    using SL = Stage<Across, 64, 4, kOuterTokens>;
     __shared__ __attribute__((aligned(16))) uint8_t lds[SZ::kBytes + SL::kBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c0 = (int64_t)blockIdx.x * kOuterCols;
@@ -504,7 +518,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
     f32x16 acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-    for (int64_t s = t0; s < t1; s += kStageK) {
+    for (int64_t s = t0; s < t1; s += kOuterTokens) {
         const bool mine = s + lane < t1 && adapter_of(a.ids, a.count, s + lane) == adapter;
         const uint64_t mask = __ballot(mine);
         if (mask == 0) continue;
@@ -535,7 +549,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
         }
         __syncthreads();
 #pragma unroll
-        for (int kk = 0; kk < kStageK / 16; ++kk) {
+        for (int kk = 0; kk < kOuterTokens / 16; ++kk) {
             const bf16x8 fz = SZ::read(lds, SZ::read_offset(wave * 32, kk, lane));
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
@@ -557,11 +571,11 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
     }
 }
 
-// The sum of the splits as bf16: dA [count, rank, width] as it lies, or
+// `scale` times the sum of the splits as bf16: dA [count, rank, width] as it lies, or
 // dB [count, columns, rank] (columns <= width) transposed.
 template <bool kTransposed>
 __global__ __launch_bounds__(256) void outer_finish(const float *__restrict__ partial, int splits, int64_t count,
-                                                    int rank, int64_t width, int64_t columns,
+                                                    int rank, int64_t width, int64_t columns, float scale,
                                                     uint16_t *__restrict__ G) {
     const int64_t total = count * rank * width, stride = (int64_t)gridDim.x * 256;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
@@ -573,11 +587,11 @@ __global__ __launch_bounds__(256) void outer_finish(const float *__restrict__ pa
             if (c >= columns) continue;
             float v = 0.0f;
             for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + src];
-            G[(a * columns + c) * rank + r % rank] = (uint16_t)bf16_rne(v);
+            G[(a * columns + c) * rank + r % rank] = (uint16_t)bf16_rne(v * scale);
         } else {
             float v = 0.0f;
             for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + src];
-            G[id] = (uint16_t)bf16_rne(v);
+            G[id] = (uint16_t)bf16_rne(v * scale);
         }
     }
 }
@@ -606,8 +620,6 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 // Host side
 // ---------------------------------------------------------------------------
 
-typedef Tile<2, 4, 4, 2> Large;   // 256 x 256
-typedef Tile<2, 2, 2, 2> Small;   // 128 x 128
 
 constexpr int kTargetBlocks = 1024;
 constexpr int64_t kFewTokens = 64;
@@ -659,10 +671,10 @@ int shrink(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, cons
 }
 
 int shrink_to_low(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, const Adapters &ad, const Low &p,
-                  float *partial, uint16_t *low, hipStream_t stream) {
+                  float f, float *partial, uint16_t *low, hipStream_t stream) {
     if (const int st = shrink(z, tokens, width, A, ad, p, partial, stream)) return st;
     hipLaunchKernelGGL(shrink_finish, dim3(grid_for(tokens * rank_pad(ad.rank), 256)), dim3(256), 0, stream, partial,
-                       p.splits, tokens, ad.rank, rank_pad(ad.rank), ad.alpha, ad.ids, ad.count, low);
+                       p.splits, tokens, ad.rank, rank_pad(ad.rank), ad.alpha, f, ad.ids, ad.count, low);
     return launch_status();
 }
 
@@ -743,7 +755,7 @@ struct GradPlan {
 inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
     const int64_t blocks = cdiv(width, kOuterCols) * (rank_pad(rank) / 32) * count;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256)));
-    split = cdiv(cdiv(tokens, want), kStageK) * kStageK;
+    split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
     splits = (int)cdiv(tokens, split);
 }
 
@@ -783,6 +795,13 @@ int check_adapters(const hscale_adapters *w, Adapters &ad) {
     return HSCALE_OK;
 }
 
+// s = f 2^e with 1 <= f < 2.
+inline void split_scale(float s, float &f, float &two_e) {
+    int e;
+    f = 2.0f * std::frexp(s, &e);
+    two_e = std::ldexp(1.0f, e - 1);
+}
+
 struct Range {
     const void *p;
     size_t n;
@@ -799,11 +818,11 @@ bool any_overlap(const Range *w, int nw, const Range *r, int nr) {
     return false;
 }
 
-int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, void *W,
+int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, float two_e, void *W,
                    hipStream_t stream) {
     const int64_t groups = out * (in / kGroup);
     hipLaunchKernelGGL(stored_to_bf16, dim3(grid_for(groups, 256)), dim3(256), 0, stream, codes,
-                       reinterpret_cast<const uint2 *>(packed), groups, static_cast<u32x4 *>(W));
+                       reinterpret_cast<const uint2 *>(packed), groups, two_e, static_cast<u32x4 *>(W));
     return launch_status();
 }
 
@@ -895,20 +914,22 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
         return launch_status();
     }
     void *W = ws;
+    float f, two_e;
+    split_scale(global_scale, f, two_e);
     float *partial = reinterpret_cast<float *>(ws + p.weights);
     uint16_t *low = reinterpret_cast<uint16_t *>(ws + p.weights + p.low_partial);
-    if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, W, stream)) return st;
+    if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, two_e, W, stream)) return st;
     LayerArgs a{};
     if (ad.count) {
-        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.low, partial, low, stream)) return st;
+        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.low, f, partial, low, stream)) return st;
         a.low = LowRank{low, ad.B, out * ad.rank, ad.rank, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
     }
     a.W = Operand{W, in, out, in};
     a.X = Operand{X, ldx, tokens, in};
-    a.s_g = global_scale;
+    a.scale = f;
     a.Y = y;
     a.ldy = ldy;
-    a.wide = aligned(Y, 8) && ldy % 4 == 0;
+    a.wide = aligned(Y, 16) && (tokens == 1 || ldy % 8 == 0);
     return layer<Along>(a, stream);
 }
 
@@ -954,6 +975,8 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
 
     char *ws = static_cast<char *>(workspace);
     void *W = ws;
+    float f, two_e;
+    split_scale(global_scale, f, two_e);
     uint16_t *wide_dy = reinterpret_cast<uint16_t *>(ws += p.weights);
     uint16_t *turned = reinterpret_cast<uint16_t *>(ws += p.dy);
     float *partial = reinterpret_cast<float *>(ws += p.turned);
@@ -972,23 +995,23 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
         hipLaunchKernelGGL(turn_kernel, dim3(grid_for(ad.count * ad.rank * p.width, 256)), dim3(256), 0, stream, ad.B,
                            (int64_t)ad.count, out, ad.rank, p.width, turned);
         if (const int st = launch_status()) return st;
-        if (const int st = shrink_to_low(dy, tokens, p.width, turned, ad, p.v, partial, v, stream)) return st;
-        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.u, partial, u, stream)) return st;
+        if (const int st = shrink_to_low(dy, tokens, p.width, turned, ad, p.v, f, partial, v, stream)) return st;
+        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.u, 1.0f, partial, u, stream)) return st;
         if (dX) {
-            if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, W, stream)) return st;
+            if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, two_e, W, stream)) return st;
             LayerArgs a{};
             a.W = Operand{W, in, in, out};
             a.X = Operand{dy.p, dy.ld, tokens, p.width};
-            a.s_g = global_scale;
+            a.scale = f;
             a.low = LowRank{v, ad.A, in * ad.rank, in, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
             a.Y = static_cast<uint16_t *>(dX);
             a.ldy = lddx;
-            a.wide = aligned(dX, 8) && lddx % 4 == 0;
+            a.wide = aligned(dX, 16) && (tokens == 1 || lddx % 8 == 0);
             if (const int st = layer<Across>(a, stream)) return st;
         }
     }
     auto outer_of = [&](const Rows &z, int64_t width, int64_t columns, const uint16_t *low, int64_t split, int splits,
-                        void *G, bool transposed) {
+                        float by, void *G, bool transposed) {
         if (tokens > 0) {
             const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, split, outer};
             const dim3 grid((unsigned)cdiv(width, kOuterCols), (unsigned)(rank_pad(ad.rank) / 32 * ad.count),
@@ -1002,14 +1025,14 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
         const dim3 grid(grid_for((int64_t)ad.count * ad.rank * width, 256));
         if (transposed)
             hipLaunchKernelGGL((outer_finish<true>), grid, dim3(256), 0, stream, outer, splits, (int64_t)ad.count,
-                               ad.rank, width, columns, static_cast<uint16_t *>(G));
+                               ad.rank, width, columns, by, static_cast<uint16_t *>(G));
         else
             hipLaunchKernelGGL((outer_finish<false>), grid, dim3(256), 0, stream, outer, splits, (int64_t)ad.count,
-                               ad.rank, width, columns, static_cast<uint16_t *>(G));
+                               ad.rank, width, columns, by, static_cast<uint16_t *>(G));
         return launch_status();
     };
-    if (const int st = outer_of(x, in, in, v, p.split_a, p.splits_a, dA, false)) return st;
-    return outer_of(dy, tokens > 0 ? p.width : out, out, u, p.split_b, p.splits_b, dB, true);
+    if (const int st = outer_of(x, in, in, v, p.split_a, p.splits_a, f, dA, false)) return st;
+    return outer_of(dy, tokens > 0 ? p.width : out, out, u, p.split_b, p.splits_b, 1.0f, dB, true);
 }
 
 }  // extern "C"

@@ -20,8 +20,6 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 24;
 constexpr int64_t kMaxVocab = (int64_t)1 << 24;
 constexpr int64_t kMaxLogits = (int64_t)1 << 38;  // one launch's tiles: below 2^32 threads
 
-typedef Tile<2, 4, 4, 2> Large;   // 256 x 256
-typedef Tile<2, 2, 2, 2> Small;   // 128 x 128
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -48,7 +46,7 @@ struct LogitArgs {
 };
 
 template <class T>
-__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_tile_kernel(const LogitArgs a) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_tile_kernel(const LogitArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
@@ -122,7 +120,7 @@ __global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ pa
 // g of a piece of the vocabulary, bf16; zeros where a token is not scored and
 // beyond the vocabulary.
 template <class T>
-__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_slope_kernel(const LogitArgs a) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(const LogitArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
@@ -153,7 +151,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_slope_kernel(
                 acc.v[i][j][e] = k < some ? w * p : 0.0f;
             }
     }
-    store_bf16<T>(acc, a.g, a.ldg, m0, a.ldg, n0, a.X.rows, true);
+    store_bf16<T>(acc, lds, a.g, a.ldg, m0, a.ldg, n0, a.X.rows, true);
 }
 
 struct DxArgs {
@@ -165,7 +163,7 @@ struct DxArgs {
 };
 
 template <class T>
-__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_dx_kernel(const DxArgs a) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dx_kernel(const DxArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
@@ -238,10 +236,11 @@ struct DwArgs {
     unsigned mtiles;
     int64_t cols;    // rows of dW in this piece
     uint16_t *dW;    // [cols, d]
+    bool wide;
 };
 
 template <class T>
-__global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_dw_kernel(const DwArgs a) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(const DwArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
@@ -249,7 +248,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWaves / 4) void loss_dw_kernel(con
     Acc<T> acc;
     acc.clear();
     tile_product<T, Across, Across>(acc, lds, a.X, m0, a.g, n0, 0, a.g.k);
-    store_bf16<T>(acc, a.dW, a.X.rows, m0, a.X.rows, n0, a.cols, true);
+    store_bf16<T>(acc, lds, a.dW, a.X.rows, m0, a.X.rows, n0, a.cols, a.wide);
 }
 
 // ---------------------------------------------------------------------------
@@ -294,7 +293,7 @@ LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     p.pieces = cdiv(vocab, p.piece);
     const int64_t blocks = cdiv(d, tile_rows(d, tokens)) * cdiv(tokens, tile_cols(d, tokens));
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / blocks, cdiv(p.piece, 512)));
-    p.k_split = cdiv(cdiv(p.piece, want), kStageK) * kStageK;
+    p.k_split = cdiv(cdiv(p.piece, want), Large::kK) * Large::kK;
     p.splits = (int)cdiv(p.piece, p.k_split);
     p.g = round_up((size_t)tokens * p.piece * 2, 256);
     p.sum = round_up((size_t)p.splits * tokens * d * 4, 256);
@@ -450,9 +449,10 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             b.mtiles = (unsigned)cdiv(d, tile_rows(d, cols));
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;
+            b.wide = aligned(dW, 16);
             const dim3 blocks((unsigned)(b.mtiles * cdiv(cols, tile_cols(d, cols))));
             if (large_tiles(d, cols))
-                hipLaunchKernelGGL((loss_dw_kernel<Large>), blocks, dim3(Large::kThreads), 0, stream, b);
+                hipLaunchKernelGGL((loss_dw_kernel<LargeAcross>), blocks, dim3(LargeAcross::kThreads), 0, stream, b);
             else
                 hipLaunchKernelGGL((loss_dw_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, b);
             if (const int st = launch_status()) return st;

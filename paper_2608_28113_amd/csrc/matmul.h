@@ -22,7 +22,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr uint32_t kRawWord3 = 0x00020000u;   // raw (untyped) buffer, 32-bit data format
 constexpr uint32_t kNoRead = 0x7FFF0000u;     // an offset beyond every descriptor: reads zeros
 constexpr int64_t kMostBytes = 0x7FF00000;    // of one descriptor
-constexpr int kStageK = 64;                   // k per LDS stage
 
 __device__ __forceinline__ u32x4 raw_buffer(const void *p, int64_t bytes) {
     const uint64_t a = reinterpret_cast<uintptr_t>(p);
@@ -68,19 +67,21 @@ struct Operand {
 
 enum Layout { Along, Across };
 
-// Stages of one operand's kRows x kStageK tile in LDS, filled by kWaves waves
-// with copies of 1 KB (16 bytes a lane).  Along: a row holds its 64 k (128
-// bytes), the 16-byte chunk c at position c ^ ((row / 2) % 8), so that the 16
-// rows that an operand read serves at a time fall in 16 different 16-byte
-// columns of the banks.  Across: a row holds one k of all kRows (2 kRows
-// bytes), its 64-byte chunk c at c ^ (k % 4) (for 64 rows c ^ (k / 2 % 2)), so
-// that the four k rows of a transposed read fall in different banks.
-template <Layout L, int kRows, int kWaves>
+// Stages of one operand's kRows x kK tile in LDS, filled by kWaves waves with
+// copies of 1 KB (16 bytes a lane).  Along: a row holds its 32 or 64 k (64 or
+// 128 bytes), the 16-byte chunk c at position c ^ ((row / 4) % 4) or
+// c ^ ((row / 2) % 8), so that the 16 rows that an operand read serves at a
+// time fall in 16 different 16-byte columns of the banks.  Across: a row holds
+// one k of all kRows (2 kRows bytes), its 64-byte chunk c at c ^ (k % 4) (for
+// 64 rows c ^ (k / 2 % 2)), so that the four k rows of a transposed read fall
+// in different banks.
+template <Layout L, int kRows, int kWaves, int kK>
 struct Stage {
-    static constexpr int kBytes = kRows * kStageK * 2;
+    static_assert(kK == 32 || kK == 64, "k of a stage");
+    static constexpr int kBytes = kRows * kK * 2;
     static constexpr int kCopies = kBytes / 1024 / kWaves;  // per wave and stage
     static_assert(kBytes % (1024 * kWaves) == 0, "whole copies per wave");
-    static constexpr int kRowBytes = L == Along ? kStageK * 2 : kRows * 2;
+    static constexpr int kRowBytes = L == Along ? kK * 2 : kRows * 2;
     static constexpr int kLanesPerRow = kRowBytes / 16;
 
     uint32_t off[kCopies];  // of this lane from the stage's first byte
@@ -88,8 +89,11 @@ struct Stage {
     int64_t left;           // bytes from base to the array's end
     int64_t step;           // bytes from stage to stage
     int64_t k_left;
-    int chunk;              // Along: the lane's 16-byte chunk of its row
+    int chunk;              // Along: the lane's 16-byte chunk of its rows
 
+    static __device__ __forceinline__ int along_swizzle(int row) {
+        return kK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+    }
     static __device__ __forceinline__ int across_swizzle(int k) { return kRows == 64 ? (k >> 1) & 1 : k & 3; }
 
     // The tile at row r0, and k from k0 on.
@@ -99,56 +103,77 @@ struct Stage {
         if (L == Along) {
             base = reinterpret_cast<const char *>(o.p) + (r0 * o.ld + k0) * 2;
             left = ((rows - 1) * o.ld + k_left) * 2;
-            step = kStageK * 2;
+            step = kK * 2;
         } else {
             base = reinterpret_cast<const char *>(o.p) + (k0 * o.ld + r0) * 2;
             left = ((k_left - 1) * o.ld + rows) * 2;
-            step = kStageK * o.ld * 2;
+            step = kK * o.ld * 2;
         }
         if (rows <= 0 || k_left <= 0) left = 0;
+        chunk = at(row_of(0, wave, lane), lane);
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-            const int row = (wave + i * kWaves) * (64 / kLanesPerRow) + lane / kLanesPerRow;
-            const int pos = lane % kLanesPerRow;
-            if (L == Along) {
-                chunk = pos ^ ((row >> 1) & 7);  // the same for every i: kWaves is even
-                off[i] = row < rows ? (uint32_t)(row * o.ld * 2 + chunk * 16) : kNoRead;
-            } else {
-                const int col = ((((pos >> 2) ^ across_swizzle(row)) << 2) | (pos & 3)) * 8;
-                off[i] = col < rows ? (uint32_t)(row * o.ld * 2 + col * 2) : kNoRead;
-            }
+            const int row = row_of(i, wave, lane), c = at(row, lane);
+            if (L == Along)
+                off[i] = row < rows ? (uint32_t)(row * o.ld * 2 + c * 16) : kNoRead;
+            else
+                off[i] = c * 8 < rows ? (uint32_t)(row * o.ld * 2 + c * 16) : kNoRead;
         }
     }
 
-    // Starts the copies of the next stage into LDS address `dst` (of this
-    // wave's first copy).
-    __device__ __forceinline__ void issue(uint32_t dst) {
-        if (L == Along && k_left < kStageK && chunk * 8 >= k_left) {  // k past the end: the row's next values are not read
+    // The LDS row that this lane fills in copy i, and the 16-byte chunk of its
+    // row that belongs at the lane's position (Along: the same in every copy).
+    static __device__ __forceinline__ int row_of(int i, int wave, int lane) {
+        return (wave + i * kWaves) * (64 / kLanesPerRow) + lane / kLanesPerRow;
+    }
+    static __device__ __forceinline__ int at(int row, int lane) {
+        const int pos = lane % kLanesPerRow;
+        return L == Along ? pos ^ along_swizzle(row) : (((pos >> 2) ^ across_swizzle(row)) << 2) | (pos & 3);
+    }
+
+    // Before the copies of a stage: its descriptor, and k past the end turned
+    // into reads of nothing (a row's next values are not read).  Stages past
+    // the last are all nothing: zeros, and no memory traffic.
+    __device__ __forceinline__ u32x4 begin() {
+        if (L == Along && k_left < kK) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) off[i] = kNoRead;
+            for (int i = 0; i < kCopies; ++i)
+                if (chunk * 8 >= k_left) off[i] = kNoRead;
         }
-        const u32x4 r = raw_buffer(base, left);
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy_to_lds(r, off[i], dst + i * kWaves * 1024);
+        return raw_buffer(base, left);
+    }
+    // Copy i of the stage to LDS address `dst` (of this wave's first copy).
+    __device__ __forceinline__ void copy(const u32x4 &r, int i, uint32_t dst) const {
+        copy_to_lds(r, off[i], dst + i * kWaves * 1024);
+    }
+    __device__ __forceinline__ void end() {
         base += step;
         left -= step;
-        k_left -= kStageK;
+        k_left -= kK;
     }
 
-    // Offset of the 8 k of step kk (16 k) that this lane holds of a 32-row
-    // operand block at row r.
-    static __device__ __forceinline__ int read_offset(int r, int kk, int lane) {
-        if (L == Along) {
-            const int row = r + (lane & 31);
-            return row * kRowBytes + (((2 * kk + (lane >> 5)) ^ ((row >> 1) & 7)) << 4);
+    // Where this lane finds its 8 k of 16-k step kk of the 32-row operand block
+    // i, counted from row r0: place(i, kk) + shift(i, kk), the shift known at
+    // compile time and the places few.
+        static __device__ __forceinline__ int place(int r0, int which, int lane) {
+        if (L == Along) {  // which = kk
+            const int row = r0 + (lane & 31);
+            return row * kRowBytes + (((2 * which + (lane >> 5)) ^ along_swizzle(row)) << 4);
         }
-        // A transposed read gives lane p of 16 the four k of column p from a
-        // 4-row x 16-column block whose row p / 4 the lane addresses; two
-        // reads are the 8 k.
+        // which = i.  A transposed read gives lane p of 16 the four k of
+        // column p from a 4-row x 16-column block whose row p / 4 the lane
+        // addresses; two reads are the 8 k.
         const int p = lane & 15, g = lane >> 4;
-        const int k = kk * 16 + 8 * (g >> 1) + (p >> 2);
-        const int byte = r * 2 + 32 * (g & 1) + 8 * (p & 3);
+        const int k = 8 * (g >> 1) + (p >> 2);
+        const int byte = (r0 + 32 * which) * 2 + 32 * (g & 1) + 8 * (p & 3);
         return k * kRowBytes + ((((byte >> 6) ^ across_swizzle(k)) << 6) | (byte & 63));
+    }
+    static constexpr __device__ __forceinline__ int shift(int i, int kk) {
+        return L == Along ? i * 32 * kRowBytes : kk * 16 * kRowBytes;
+    }
+    static constexpr __device__ __forceinline__ int which(int i, int kk) { return L == Along ? kk : i; }
+    static __device__ __forceinline__ int read_offset(int r, int kk, int lane) {
+        return place(r, L == Along ? kk : 0, lane) + shift(0, kk);
     }
 
     static __device__ __forceinline__ bf16x8 read(const uint8_t *buf, int offset) {
@@ -161,14 +186,22 @@ struct Stage {
     }
 };
 
-// A tile: kWM x kWN waves, each of 32 kMI x 32 kNJ accumulators of 32 x 32.
-template <int WM, int WN, int MI, int NJ>
+// A tile: WM x WN waves, each of MI x NJ accumulators of 32 x 32, and a ring of
+// R stages of K in LDS, whose copies are spread over W steps of 16 k.
+template <int WM, int WN, int MI, int NJ, int K, int R, int W>
 struct Tile {
-    static constexpr int kWM = WM, kWN = WN, kMI = MI, kNJ = NJ;
+    static constexpr int kWM = WM, kWN = WN, kMI = MI, kNJ = NJ, kK = K, kRing = R, kSpread = W;
     static constexpr int kBM = 32 * WM * MI, kBN = 32 * WN * NJ;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
-    static constexpr int kLds = 2 * (kBM + kBN) * kStageK * 2;  // two stages
+    static constexpr int kLds = R * (kBM + kBN) * K * 2;
+    static constexpr int kBlocks = 160 * 1024 / kLds;  // per CU
+    static constexpr int kOccupancy = kWaves * kBlocks / 4 < 1 ? 1 : kWaves * kBlocks / 4;
+    static_assert(W >= 1 && W <= K / 16 && R >= 2, "copies end before the stage that waits for them");
 };
+
+typedef Tile<2, 2, 4, 4, 64, 2, 2> Large;        // 256 x 256
+typedef Tile<2, 4, 4, 2, 32, 4, 2> LargeAcross;  // the same, for two operands across
+typedef Tile<2, 2, 2, 2, 64, 2, 2> Small;        // 128 x 128, two blocks on a CU
 
 template <class T>
 struct Acc {
@@ -180,14 +213,6 @@ struct Acc {
             for (int j = 0; j < T::kNJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) v[i][j][e] = 0.0f;
-    }
-    __device__ __forceinline__ void scale(float s) {
-#pragma unroll
-        for (int i = 0; i < T::kMI; ++i)
-#pragma unroll
-            for (int j = 0; j < T::kNJ; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[i][j][e] *= s;
     }
 };
 
@@ -208,15 +233,29 @@ struct Place {
     __device__ __forceinline__ int n(int j) const { return (wn * T::kNJ + j) * 32 + (lane & 31); }
 };
 
-// acc += the products over k0 .. k1 of the tile at (m0, n0).  `lds` holds
-// T::kLds bytes; all of the block's threads call it, and every wave has left
-// the LDS when it returns.
-template <class T, Layout LP, Layout LQ>
+template <int N>
+__device__ __forceinline__ void wait_copies_and_barrier() {  // all but the last N copies, and own reads
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(N) : "memory");
+}
+
+// Stages beyond those of the two operands, for tile_product: none.
+struct NoMore {
+    static constexpr bool kAny = false;
+};
+
+// acc += the products over k0 .. k1 of the tile at (m0, n0), and those of the
+// `more.stages` stages that more.set(sp, sq) points the copies at.  `lds`
+// holds T::kLds bytes; all of the block's threads call it, and every wave has
+// left the LDS when it returns.
+template <class T, Layout LP, Layout LQ, class More>
 __device__ __forceinline__ void tile_product(Acc<T> &acc, uint8_t *lds, const Operand &P, int64_t m0,
-                                             const Operand &Q, int64_t n0, int64_t k0, int64_t k1) {
-    using SP = Stage<LP, T::kBM, T::kWaves>;
-    using SQ = Stage<LQ, T::kBN, T::kWaves>;
+                                             const Operand &Q, int64_t n0, int64_t k0, int64_t k1, More more) {
+    using SP = Stage<LP, T::kBM, T::kWaves, T::kK>;
+    using SQ = Stage<LQ, T::kBN, T::kWaves, T::kK>;
     constexpr int kStageBytes = SP::kBytes + SQ::kBytes;
+    constexpr int kCopies = SP::kCopies + SQ::kCopies;  // of a wave and stage
+    constexpr int R = T::kRing, W = T::kSpread, kSteps = T::kK / 16, kMfmas = T::kMI * T::kNJ;
+    constexpr int kUnits = T::kMI + T::kNJ;
     const Place<T> at;
     const int wave = at.wm + at.wn * T::kWM;
     SP sp;
@@ -224,33 +263,102 @@ __device__ __forceinline__ void tile_product(Acc<T> &acc, uint8_t *lds, const Op
     sp.init(P, m0, k0, k1, wave, at.lane);
     sq.init(Q, n0, k0, k1, wave, at.lane);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
-    const int stages = (int)((k1 - k0 + kStageK - 1) / kStageK);
-    auto issue = [&](int buf) {
-        sp.issue(lds0 + buf * kStageBytes);
-        sq.issue(lds0 + buf * kStageBytes + SP::kBytes);
-    };
-    if (stages > 0) issue(0);
-    for (int s = 0; s < stages; ++s) {
-        wait_and_barrier();
-        if (s + 1 < stages) issue((s + 1) & 1);
-        const uint8_t *buf = lds + (s & 1) * kStageBytes;
-#pragma unroll
-        for (int kk = 0; kk < kStageK / 16; ++kk) {
-            bf16x8 fp[T::kMI], fq[T::kNJ];
-#pragma unroll
-            for (int i = 0; i < T::kMI; ++i)
-                fp[i] = SP::read(buf, SP::read_offset((at.wm * T::kMI + i) * 32, kk, at.lane));
-#pragma unroll
-            for (int j = 0; j < T::kNJ; ++j)
-                fq[j] = SQ::read(buf + SP::kBytes, SQ::read_offset((at.wn * T::kNJ + j) * 32, kk, at.lane));
-#pragma unroll
-            for (int i = 0; i < T::kMI; ++i)
-#pragma unroll
-                for (int j = 0; j < T::kNJ; ++j)
-                    acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc.v[i][j], 0, 0, 0);
+    const int own = (int)((k1 - k0 + T::kK - 1) / T::kK);
+    int stages = own, begun = 0;
+    if constexpr (More::kAny) stages += more.stages;
+    if (stages <= 0) return;
+    u32x4 rp, rq;
+    auto begin = [&]() {
+        if constexpr (More::kAny) {
+            if (begun >= own) more.set(sp, sq, begun < stages);
+            ++begun;
         }
+        rp = sp.begin();
+        rq = sq.begin();
+    };
+    auto copy = [&](int c, int buf) {  // copy c of the stage begun
+        const uint32_t dst = lds0 + buf * kStageBytes;
+        if (c < SP::kCopies)
+            sp.copy(rp, c, dst);
+        else
+            sq.copy(rq, c - SP::kCopies, dst + SP::kBytes);
+    };
+    auto end = [&]() {
+        sp.end();
+        sq.end();
+    };
+    int pp[LP == Along ? kSteps : T::kMI], pq[LQ == Along ? kSteps : T::kNJ];
+#pragma unroll
+    for (int k = 0; k < (LP == Along ? kSteps : T::kMI); ++k) pp[k] = SP::place(at.wm * T::kMI * 32, k, at.lane);
+#pragma unroll
+    for (int k = 0; k < (LQ == Along ? kSteps : T::kNJ); ++k) pq[k] = SQ::place(at.wn * T::kNJ * 32, k, at.lane);
+    bf16x8 fp[2][T::kMI], fq[2][T::kNJ];
+    auto read_unit = [&](const uint8_t *buf, int kk, int u) {  // operand block u of step kk
+        if (u < T::kMI)
+            fp[kk & 1][u] = SP::read(buf, pp[SP::which(u, kk)] + SP::shift(u, kk));
+        else
+            fq[kk & 1][u - T::kMI] =
+                SQ::read(buf + SP::kBytes, pq[SQ::which(u - T::kMI, kk)] + SQ::shift(u - T::kMI, kk));
+    };
+
+    // Two sets of operand registers: each 16-k step's operands are read while
+    // the step before it multiplies, across stages too.  At a stage's last
+    // step its operands are in registers, so after the waits (own reads done,
+    // own copies of the next stage landed) and the barrier its buffer takes
+    // the stage kRing further on.  Those copies are started one by one
+    // between the MFMAs of that step and of the next W - 1: in one go they
+    // fill the memory pipeline's queue, and the wave stands before it.
+    constexpr int kFirst = kCopies / W;  // copies in a stage's last step
+#pragma unroll
+    for (int s = 0; s < R; ++s) {
+        begin();
+#pragma unroll
+        for (int c = 0; c < (s < R - 1 ? kCopies : kFirst); ++c) copy(c, s);
+        if (s < R - 1 || W == 1) end();
+    }
+    wait_copies_and_barrier<(R - 2) * kCopies + kFirst>();
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) read_unit(lds, 0, u);
+    int cur = 0, prev = R - 1;
+    for (int s = 0; s < stages; ++s) {
+        const int next = cur + 1 == R ? 0 : cur + 1;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+            const bool last = kk == kSteps - 1;
+            if (last) {
+                wait_copies_and_barrier<(R - 2) * kCopies>();
+                begin();
+            }
+            // after the last stage: old values that nothing uses
+            const uint8_t *from = lds + (last ? next : cur) * kStageBytes;
+            const int w = last ? 0 : kk + 1;  // step of the window
+            const int c0 = w < W ? kCopies * w / W : 0, c1 = w < W ? kCopies * (w + 1) / W : 0;
+#pragma unroll
+            for (int q = 0; q < kMfmas; ++q) {
+                const int i = q % T::kMI, j = q / T::kMI;
+                acc.v[i][j] =
+                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[kk & 1][i], fq[kk & 1][j], acc.v[i][j], 0, 0, 0);
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u)
+                    if (u * kMfmas / kUnits == q) read_unit(from, last ? 0 : kk + 1, u);
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c)
+                    if (c >= c0 && c < c1 && (2 * (c - c0) + 1) * kMfmas / (2 * (c1 - c0)) == q)
+                        copy(c, last ? cur : prev);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (w == W - 1) end();
+        }
+        prev = cur;
+        cur = next;
     }
     wait_and_barrier();
+}
+
+template <class T, Layout LP, Layout LQ>
+__device__ __forceinline__ void tile_product(Acc<T> &acc, uint8_t *lds, const Operand &P, int64_t m0,
+                                             const Operand &Q, int64_t n0, int64_t k0, int64_t k1) {
+    tile_product<T, LP, LQ>(acc, lds, P, m0, Q, n0, k0, k1, NoMore{});
 }
 
 // The (m tile, n tile) of block b of `total`.  Blocks go to the 8 XCDs
@@ -278,12 +386,52 @@ __device__ __forceinline__ void tile_of_block(unsigned b, unsigned total, unsign
     }
 }
 
-// Writes a tile as bf16 to C[n * ld + m]; `wide`: rows of C are 8-byte
-// aligned and m in whole fours.
+// Writes `scale` times a tile as bf16 to C[n * ld + m], for m below `rows` and
+// n below `cols`.  Accumulators hold four consecutive m of 32 rows n at a time; written
+// like that, every store is 32 pieces of 16 bytes, and the 128 KB of a 256 x
+// 256 tile take longer than 600 of its k.  So the tile goes through LDS, 16
+// bytes of a row at chunk position c ^ (n % 32) (of the row's chunks), and out
+// in whole rows.  `wide`: C and its rows are 16-byte aligned; else element by
+// element.
 template <class T>
-__device__ __forceinline__ void store_bf16(const Acc<T> &acc, uint16_t *C, int64_t ld, int64_t m0, int64_t rows,
-                                           int64_t n0, int64_t cols, bool wide) {
+__device__ __forceinline__ void store_bf16(const Acc<T> &acc, uint8_t *lds, uint16_t *C, int64_t ld, int64_t m0,
+                                           int64_t rows, int64_t n0, int64_t cols, bool wide, float scale = 1.0f) {
     const Place<T> at;
+    constexpr int kRow = T::kBM * 2, kChunks = kRow / 16;
+    static_assert(T::kBN * kRow <= T::kLds, "the tile fits the ring");
+    if (wide) {
+#pragma unroll
+        for (int j = 0; j < T::kNJ; ++j) {
+            const int n = at.n(j);
+#pragma unroll
+            for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int m = at.m(i, 4 * q);
+                    const f32x16 &a = acc.v[i][j];
+                    *reinterpret_cast<uint2 *>(lds + n * kRow + (((m >> 3) ^ (n & 31 & (kChunks - 1))) << 4) +
+                                               (m & 4) * 2) =
+                        make_uint2(bf16_pair(a[4 * q] * scale, a[4 * q + 1] * scale),
+                                   bf16_pair(a[4 * q + 2] * scale, a[4 * q + 3] * scale));
+                }
+        }
+        __syncthreads();
+        const int c = threadIdx.x % kChunks;
+        const int64_t m = m0 + c * 8;
+        uint16_t *dst = C + n0 * ld + m;
+        for (int n = threadIdx.x / kChunks; n < T::kBN; n += T::kThreads / kChunks) {
+            if (n0 + n >= cols) break;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + n * kRow + ((c ^ (n & 31 & (kChunks - 1))) << 4));
+            if (m + 8 <= rows) {
+                *reinterpret_cast<u32x4 *>(dst + n * ld) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (m + e < rows) dst[n * ld + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < T::kNJ; ++j) {
         const int64_t n = n0 + at.n(j);
@@ -292,17 +440,9 @@ __device__ __forceinline__ void store_bf16(const Acc<T> &acc, uint16_t *C, int64
 #pragma unroll
         for (int i = 0; i < T::kMI; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t m = m0 + at.m(i, 4 * q);
-                const f32x16 &a = acc.v[i][j];
-                if (wide && m + 4 <= rows) {
-                    *reinterpret_cast<uint2 *>(row + m) = make_uint2(bf16_pair(a[4 * q], a[4 * q + 1]),
-                                                                     bf16_pair(a[4 * q + 2], a[4 * q + 3]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (m + e < rows) row[m + e] = (uint16_t)bf16_rne(a[4 * q + e]);
-                }
+            for (int e = 0; e < 16; ++e) {
+                const int64_t m = m0 + at.m(i, e);
+                if (m < rows) row[m] = (uint16_t)bf16_rne(acc.v[i][j][e] * scale);
             }
     }
 }
