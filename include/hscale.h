@@ -493,7 +493,7 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
  * which stands for the value bf16(q * scale).
  *
  * X      bf16 [tokens, in], rows ldx apart, 16-byte aligned rows; finite
- * q      int8 [tokens, in], 8-byte aligned
+ * q      int8 [tokens, in], 16-byte aligned
  * scale  fp32 [tokens, ceil(in / 128)]
  */
 int hscale_pack_activations(const void *X, int64_t tokens, int64_t in, int64_t ldx, int8_t *q, float *scale,

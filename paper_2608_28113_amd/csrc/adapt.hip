@@ -168,70 +168,114 @@ struct ShrinkArgs {
     const uint16_t *A;      // [count, rank, width]
     int count, rank, rank_pad;
     const int32_t *ids;
-    int64_t k_split;        // of a split, a multiple of 64
+    int64_t k_split;        // of a split, a multiple of kLowK
     float *partial;         // [splits, tokens, rank_pad]
 };
 
-// 32 tokens x 32 ranks x one split of k per block, of which each of 4 waves
-// takes every fourth 16 k; one pass for each adapter that the tokens have
-// (ordinals z, z + slots, ...).  Rows of other adapters are computed and not
-// stored, so no value of another request enters a token's result.
-template <bool kCheckpoint>
-__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs a, int slots) {
-    __shared__ float red[3][32 * 33];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t0 = (int64_t)blockIdx.x * 32, t1 = t0 + 32 < a.tokens ? t0 + 32 : a.tokens;
+// 128 tokens (32 a wave) x 32 kMI ranks x one split of k per block, 128 k at a
+// time; one pass for each adapter that the 128 tokens have, which reads and
+// stores only the rows of its own tokens.  Reading z bounds it: a lane takes
+// its token's k straight into registers while the 128 k before multiply, 16
+// bytes at a time (two lanes 32 consecutive ones); the adapter's rows, the
+// same for all waves, come through LDS, 16-byte chunk c of row j at c ^ (j % 16).
+constexpr int kLowK = 128;
+
+template <bool kCheckpoint, int kMI>
+__global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
+    constexpr int kABytes = 32 * kMI * kLowK * 2;
+    constexpr int kLoads = kCheckpoint ? 4 : 8;  // 16 bytes a lane: 16 or 8 of the 64 k that it takes of 128
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kABytes];
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t0 = (int64_t)blockIdx.x * 128, t1 = t0 + 128 < a.tokens ? t0 + 128 : a.tokens;
     const int64_t k0 = (int64_t)blockIdx.y * a.k_split;
     const int64_t k1 = k0 + a.k_split < a.width ? k0 + a.k_split : a.width;
-    const int rank_tiles = a.rank_pad / 32;
-    const int j0 = (int)(blockIdx.z % rank_tiles) * 32, slot = blockIdx.z / rank_tiles;
-    const int64_t t = t0 + (lane & 31);
-    const bool t_ok = t < t1;
-    const int own = t_ok ? adapter_of(a.ids, a.count, t) : kNoAdapter;
-    const int j = j0 + (lane & 31);
-    int adapter = -1;
-    for (int nth = 0;; ++nth) {
-        adapter = next_adapter(a.ids, a.count, t0, t1, adapter);
-        if (adapter == INT_MAX) break;
-        if (nth % slots != slot) continue;
-        const uint16_t *Arow = a.A + ((int64_t)adapter * a.rank + j) * a.width;
-        f32x16 acc;
+    const int stages = (int)((k1 - k0 + kLowK - 1) / kLowK);
+    const int j0 = (int)blockIdx.z * 32 * kMI, ranks = a.rank - j0 < 32 * kMI ? a.rank - j0 : 32 * kMI;
+    const int64_t t = t0 + wave * 32 + (lane & 31);
+    const int own = t < t1 ? adapter_of(a.ids, a.count, t) : kNoAdapter;
+    const int64_t blocks = (a.width + kCkBlock - 1) / kCkBlock;
+    const char *zrow = reinterpret_cast<const char *>(a.z.p) + (kCheckpoint ? t * a.width : t * a.z.ld * 2);
+    const float *srow = kCheckpoint ? a.z.scale + t * blocks : nullptr;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
+
+    struct Taken {
+        u32x4 v[kLoads];
+        float s;
+    } z[2];
+    for (int adapter = next_adapter(a.ids, a.count, t0, t1, -1); adapter != INT_MAX;
+         adapter = next_adapter(a.ids, a.count, t0, t1, adapter)) {
+        const bool mine = own == adapter;
+        const u32x4 ra = raw_buffer(a.A + ((int64_t)adapter * a.rank + j0) * a.width, ranks * a.width * 2);
+        auto copy_a = [&](int stage) {
+            const int64_t k = k0 + (int64_t)stage * kLowK;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-        for (int64_t k = k0 + wave * 16; k < k1; k += 64) {
-            const int64_t c = k + 8 * (lane >> 5);
-            u32x4 fa = {0, 0, 0, 0}, fz = {0, 0, 0, 0};
-            if (j < a.rank) fa = *reinterpret_cast<const u32x4 *>(Arow + c);
-            if (t_ok) {
-                if (kCheckpoint)
-                    fz = restore8(
-                        *reinterpret_cast<const uint2 *>(reinterpret_cast<const int8_t *>(a.z.p) + t * a.width + c),
-                        a.z.scale[t * ((a.width + kCkBlock - 1) / kCkBlock) + c / kCkBlock]);
-                else
-                    fz = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(a.z.p) + t * a.z.ld + c);
+            for (int i = 0; i < 2 * kMI; ++i) {
+                const int row = (wave + 4 * i) * 4 + (lane >> 4);
+                const int64_t c = k + ((lane & 15) ^ (row & 15)) * 8;
+                copy_to_lds(ra, row < ranks && c < k1 ? (uint32_t)((row * a.width + c) * 2) : kNoRead,
+                            lds0 + (stage & 1) * kABytes + i * 4096);
             }
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa),
-                                                          __builtin_bit_cast(bf16x8, fz), acc, 0, 0, 0);
-        }
-        __syncthreads();
-        if (wave > 0) {
+        };
+        auto take = [&](Taken &r, int stage) {
+            const int64_t k = k0 + (int64_t)stage * kLowK;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) red[wave - 1][(lane >> 5) * 16 * 33 + e * 33 + (lane & 31)] = acc[e];
+            for (int p = 0; p < kLoads; ++p) {
+                const int64_t c = k + (kCheckpoint ? p * 32 + h * 16 : p * 16 + h * 8);
+                r.v[p] = u32x4{0, 0, 0, 0};
+                if (mine && c < k1) r.v[p] = *reinterpret_cast<const u32x4 *>(zrow + (kCheckpoint ? c : 2 * c));
+            }
+            if (kCheckpoint) r.s = mine ? srow[k / kCkBlock] : 0.0f;
+        };
+        f32x16 acc[kMI];
+#pragma unroll
+        for (int i = 0; i < kMI; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+        auto multiply = [&](const Taken &r, int stage) {
+            const uint8_t *buf = lds + (stage & 1) * kABytes + (lane & 31) * (kLowK * 2);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int chunk = kCheckpoint ? 4 * (q >> 1) + 2 * h + (q & 1) : 2 * q + h;
+                u32x4 x;
+                if (kCheckpoint) {
+                    const u32x4 w = r.v[q >> 1 & 3];
+                    x = restore8(q & 1 ? make_uint2(w[2], w[3]) : make_uint2(w[0], w[1]), r.s);
+                } else {
+                    x = r.v[q & (kLoads - 1)];
+                }
+#pragma unroll
+                for (int i = 0; i < kMI; ++i) {
+                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(buf + i * 32 * (kLowK * 2) +
+                                                                       ((chunk ^ (lane & 15)) << 4));
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, __builtin_bit_cast(bf16x8, x), acc[i], 0, 0, 0);
+                }
+            }
+        };
+        copy_a(0);
+        take(z[0], 0);
+        for (int s = 0; s < stages; s += 2) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                if (s + b < stages) {
+                    wait_and_barrier();
+                    if (s + b + 1 < stages) {
+                        copy_a(s + b + 1);
+                        take(z[1 - b], s + b + 1);
+                    }
+                    multiply(z[b], s + b);
+                }
         }
-        __syncthreads();
-        if (wave == 0 && own == adapter) {
+        wait_and_barrier();
+        if (mine) {
             float *dst = a.partial + ((int64_t)blockIdx.y * a.tokens + t) * a.rank_pad + j0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float4 v;
-                float *f = &v.x;
+            for (int i = 0; i < kMI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = (lane >> 5) * 16 * 33 + (4 * q + e) * 33 + (lane & 31);
-                    f[e] = ((acc[4 * q + e] + red[0][at]) + red[1][at]) + red[2][at];
-                }
-                *reinterpret_cast<float4 *>(dst + 8 * q + 4 * (lane >> 5)) = v;
-            }
+                for (int q = 0; q < 4; ++q)
+                    if (j0 + 32 * i < a.rank_pad)
+                        *reinterpret_cast<float4 *>(dst + 32 * i + 8 * q + 4 * h) =
+                            make_float4(acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]);
         }
     }
 }
@@ -292,13 +336,14 @@ struct LowRankStages {
     int copied[SQ::kCopies];     // of the rows that this lane copies
     int adapter = -1, step = 0;  // of the next stage
 
-    __device__ __forceinline__ LowRankStages(const LowRank &low, int64_t m, int64_t rows, int64_t n, int64_t tokens)
+    __device__ __forceinline__ LowRankStages(const LowRank &low, bool some, int64_t m, int64_t rows, int64_t n,
+                                             int64_t tokens)
         : stages(0), w(low), m0(m), prows(rows - m < T::kBM ? rows - m : T::kBM), n0(n),
           n1(n + T::kBN < tokens ? n + T::kBN : tokens) {
         const Place<T> at;
         wave = at.wm + at.wn * T::kWM;
         lane = at.lane;
-        if (!w.low) return;
+        if (!w.low || !some) return;
 #pragma unroll
         for (int i = 0; i < T::kBN / 64; ++i) tile[i] = of(i * 64 + lane);
 #pragma unroll
@@ -360,25 +405,137 @@ struct LayerArgs {
     uint16_t *Y;   // [tokens, m] at ldy
     int64_t ldy;
     bool wide;
-    unsigned mtiles;
+    unsigned mtiles, tiles;
+    int64_t k_split;
+    float *sum;    // [splits, tokens, m]; NULL: one split, written to Y
 };
 
 template <class T, Layout LW>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void layer_kernel(const LayerArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
-    tile_of_block(blockIdx.x, gridDim.x, a.mtiles, mt, nt);
+    tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
+    const int64_t split = blockIdx.x / a.tiles;
     const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.X.k ? k0 + a.k_split : a.X.k;
     Acc<T> acc;
     acc.clear();
-    tile_product<T, LW, Along>(acc, lds, a.W, m0, a.X, n0, 0, a.X.k,
-                               LowRankStages<T, LW>(a.low, m0, a.W.rows, n0, a.X.rows));
-    store_bf16<T>(acc, lds, a.Y, a.ldy, m0, a.W.rows, n0, a.X.rows, a.wide, a.scale);
+    // the adapters' stages with the first split
+    tile_product<T, LW, Along>(acc, lds, a.W, m0, a.X, n0, k0, k1,
+                               LowRankStages<T, LW>(a.low, split == 0, m0, a.W.rows, n0, a.X.rows));
+    if (a.sum)
+        store_sum<T>(acc, a.sum + split * a.X.rows * a.W.rows, m0, a.W.rows, n0, a.X.rows, a.W.rows % 4 == 0, false);
+    else
+        store_bf16<T>(acc, lds, a.Y, a.ldy, m0, a.W.rows, n0, a.X.rows, a.wide, a.scale);
+}
+
+// `scale` times the sum of the splits, a token's row per blockIdx.y.
+__global__ __launch_bounds__(256) void layer_finish(const float *__restrict__ sum, int splits, int64_t tokens,
+                                                    int64_t m, float scale, uint16_t *__restrict__ Y, int64_t ldy) {
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y, plane = tokens * m;
+    if (c >= m) return;
+    const float *src = sum + t * m + c;
+    uint16_t *dst = Y + t * ldy + c;
+    if (m % 4 == 0) {
+        float4 v = *reinterpret_cast<const float4 *>(src);
+        for (int s = 1; s < splits; ++s) {
+            const float4 o = *reinterpret_cast<const float4 *>(src + s * plane);
+            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        const uint32_t lo = bf16_pair(v.x * scale, v.y * scale), hi = bf16_pair(v.z * scale, v.w * scale);
+        if ((reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+        } else {
+            dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16), dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
+        }
+        return;
+    }
+    for (int e = 0; e < 4 && c + e < m; ++e) {
+        float v = src[e];
+        for (int s = 1; s < splits; ++s) v += src[e + s * plane];
+        dst[e] = (uint16_t)bf16_rne(v * scale);
+    }
 }
 
 // ---------------------------------------------------------------------------
 // The layer with its adapters, few tokens
 // ---------------------------------------------------------------------------
+
+// Down to the rank for few tokens: 32 tokens x 32 ranks x up to 1024 k per
+// block, of which each of 8 waves takes an eighth, and one adapter: the nth,
+// in the order of the 32 tokens, that they have.  All of a wave's loads are
+// under way at once.
+constexpr int kFewLowK = 1024;
+
+struct FewLowArgs {
+    const uint16_t *X;
+    int64_t tokens, ldx, in;
+    const uint16_t *A;  // [count, rank, in]
+    int count, rank, rank_pad;
+    const int32_t *ids;
+    float *partial;     // [splits, tokens, rank_pad]
+    int splits, slots;  // blocks: token tiles x rank tiles x splits x slots
+};
+
+__device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t *lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int slot = block % a.slots, split = block / a.slots % a.splits;
+    const int rank_tiles = a.rank_pad / 32, rest = block / a.slots / a.splits;
+    const int j = rest % rank_tiles * 32 + (lane & 31);
+    const int64_t t0 = (int64_t)(rest / rank_tiles) * 32, t1 = t0 + 32 < a.tokens ? t0 + 32 : a.tokens;
+    const int64_t t = t0 + (lane & 31);
+    const int own = t < t1 ? adapter_of(a.ids, a.count, t) : kNoAdapter;
+    bool first = lane < 32 && own != kNoAdapter;
+#pragma unroll
+    for (int k = 0; k < 31; ++k)
+        if (__builtin_amdgcn_readlane(own, k) == own && lane > k) first = false;
+    uint64_t mask = __ballot(first);
+    for (int nth = 0; nth < slot; ++nth) mask &= mask - 1;
+    if (mask == 0) return;
+    const int adapter = __builtin_amdgcn_readlane(own, __builtin_ctzll(mask));
+    const uint16_t *Arow = a.A + ((int64_t)adapter * a.rank + j) * a.in;
+    const uint16_t *Xrow = a.X + t * a.ldx;
+    const int64_t c0 = (int64_t)split * kFewLowK + wave * (kFewLowK / 8) + 8 * (lane >> 5);
+    constexpr int kSteps = kFewLowK / 8 / 16;
+    u32x4 fa[kSteps], fx[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        const int64_t c = c0 + 16 * k;
+        fa[k] = fx[k] = u32x4{0, 0, 0, 0};
+        if (c < a.in && j < a.rank) fa[k] = *reinterpret_cast<const u32x4 *>(Arow + c);
+        if (c < a.in && t < t1) fx[k] = *reinterpret_cast<const u32x4 *>(Xrow + c);
+    }
+    f32x16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[k]),
+                                                      __builtin_bit_cast(bf16x8, fx[k]), acc, 0, 0, 0);
+    float *red = reinterpret_cast<float *>(lds);  // [8 waves][16][64]
+#pragma unroll
+    for (int e = 0; e < 16; ++e) red[(wave * 16 + e) * 64 + lane] = acc[e];
+    __syncthreads();
+    // Thread (wave w, lane) adds elements 2 w and 2 w + 1 of the lane over the waves.
+    if (own != adapter) return;
+    float v[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < 8; ++w)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[e] += red[(w * 16 + 2 * wave + e) * 64 + lane];
+    const int row = 8 * (wave >> 1) + 4 * (lane >> 5) + 2 * (wave & 1);
+    *reinterpret_cast<float2 *>(a.partial + ((int64_t)split * a.tokens + t) * a.rank_pad + j - (lane & 31) + row) =
+        make_float2(v[0], v[1]);
+}
+
+// W^ against few tokens: 128 output rows x 16 kNT tokens x one split of k per
+// block.  8 waves: 32 rows each, and each half of a 256-k chunk its own four.
+// HBM bounds it for few tokens, the conversion of the weights (about 11 cycles
+// for two per lane) and LDS reads of X for 64.  A wave's MFMA operand of
+// weights comes straight from memory, 32 consecutive weights a lane: which k
+// meets which place in a step does not matter, as both operands agree.  X goes
+// through LDS, 16 bytes a lane, row t's 16-byte chunk c at c ^ (t % 16).
+constexpr int kFewK = 256, kFewRows = 128;
 
 struct FewArgs {
     const uint8_t *codes;
@@ -386,59 +543,153 @@ struct FewArgs {
     int64_t out, in;
     const uint16_t *X;
     int64_t tokens, ldx;
-    int64_t k_split;  // a multiple of 128
+    int64_t k_split;  // a multiple of kFewK
+    int row_blocks, splits;
     float *partial;   // [splits, tokens, out]
+    int low_blocks;   // the first blocks go down to the rank
+    FewLowArgs low;
 };
 
-// 64 output rows (16 per wave) x one split of k x 16 kNT tokens.  A lane
-// takes 32 consecutive weights of a row at a time, four MFMA steps: which k
-// meets which place in a step does not matter, as both operands agree.
-template <int kNT>
-__global__ __launch_bounds__(256) void few_kernel(const FewArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * 64 + wave * 16 + (lane & 15);
-    const int64_t t0 = (int64_t)blockIdx.z * 16 * kNT;
-    const bool row_ok = row < a.out;
-    const int64_t k0 = (int64_t)blockIdx.y * a.k_split;
-    const int64_t k1 = k0 + a.k_split < a.in ? k0 + a.k_split : a.in;
-    f32x4 acc[kNT];
+template <bool kEven>  // in % 32 == 0: a lane's two scales are one aligned word
+struct FewWeights {
+    u32x4 p[2];
+    uint32_t c[2];
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t rp, const __amdgpu_buffer_rsrc_t rc,
+                                         uint32_t prow, uint32_t crow, uint32_t p16, uint32_t c16, uint32_t k) {
 #pragma unroll
-    for (int n = 0; n < kNT; ++n) acc[n] = f32x4{0, 0, 0, 0};
-    const uint8_t *prow = a.packed + row * (a.in / 2);
-    const uint8_t *crow = a.codes + row * (a.in / kGroup);
-    for (int64_t k = k0 + (lane >> 4) * 32; k - (lane >> 4) * 32 < k1; k += 128) {
-        uint2 p[2] = {{0, 0}, {0, 0}};
-        float l[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-            if (row_ok && k + 16 * g < k1) {
-                p[g] = *reinterpret_cast<const uint2 *>(prow + (k + 16 * g) / 2);
-                l[g] = e4m3fn_value(crow[(k + 16 * g) / kGroup]);
-            }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const u32x4 w = stored_eight(q & 1 ? p[q >> 1].y : p[q >> 1].x, l[q >> 1]);
-#pragma unroll
-            for (int n = 0; n < kNT; ++n) {
-                const int64_t t = t0 + n * 16 + (lane & 15);
-                u32x4 x = {0, 0, 0, 0};
-                if (t < a.tokens && k + 8 * q < k1)
-                    x = *reinterpret_cast<const u32x4 *>(a.X + t * a.ldx + k + 8 * q);
-                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w),
-                                                                 __builtin_bit_cast(bf16x8, x), acc[n], 0, 0, 0);
+        for (int f = 0; f < 2; ++f) {
+            p[f] = __builtin_amdgcn_raw_buffer_load_b128(rp, prow + f * p16 + k / 2, 0, 0);
+            if (kEven) {
+                c[f] = __builtin_amdgcn_raw_buffer_load_b16(rc, crow + f * c16 + k / 16, 0, 0);
+            } else {
+                c[f] = __builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16, 0, 0);
+                c[f] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16 + 1, 0, 0) << 8;
             }
         }
     }
-#pragma unroll
-    for (int n = 0; n < kNT; ++n) {
-        const int64_t t = t0 + n * 16 + (lane & 15);
-        const int64_t m = (int64_t)blockIdx.x * 64 + wave * 16 + 4 * (lane >> 4);
-        if (t >= a.tokens) continue;
-        float *dst = a.partial + ((int64_t)blockIdx.y * a.tokens + t) * a.out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (m + e < a.out) dst[m + e] = acc[n][e];
+};
+
+template <int kNT, bool kEven>
+__global__ __launch_bounds__(512, 4) void few_kernel(const FewArgs a) {
+    constexpr int kXBytes = 16 * kNT * kFewK * 2;
+    constexpr int kLdsBytes = 2 * kXBytes > 8 * 4096 ? 2 * kXBytes : 8 * 4096;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
+    if ((int)blockIdx.x < a.low_blocks) {
+        few_low(a.low, blockIdx.x, lds);
+        return;
     }
+    const int block = blockIdx.x - a.low_blocks;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rg = wave & 3, half = wave >> 2, g = lane >> 4, l16 = lane & 15;
+    const int64_t r0 = (int64_t)(block % a.row_blocks) * kFewRows;
+    const int split = block / a.row_blocks % a.splits;
+    const int64_t t0 = (int64_t)(block / a.row_blocks / a.splits) * 16 * kNT;
+    const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.in ? k0 + a.k_split : a.in;
+    const int64_t rows = a.out - r0 < kFewRows ? a.out - r0 : kFewRows;
+    const int chunks = (int)((k1 - k0 + kFewK - 1) / kFewK);
+
+    // Weights past a row's end are the next row's, and meet zeros of X; past
+    // the block's last row they read as zeros.
+    const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t *>(a.packed + r0 * (a.in / 2)), 0, (int)(rows * (a.in / 2)), kRawWord3);
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t *>(a.codes + r0 * (a.in / kGroup)), 0, (int)(rows * (a.in / kGroup)), kRawWord3);
+    const uint32_t row = rg * 32 + l16;
+    const uint32_t prow = row * (uint32_t)(a.in / 2), crow = row * (uint32_t)(a.in / kGroup);
+    const uint32_t p16 = 16 * (uint32_t)(a.in / 2), c16 = 16 * (uint32_t)(a.in / kGroup);
+    const uint32_t kl = (uint32_t)k0 + half * 128 + g * 32;
+
+    const int64_t toks = a.tokens - t0 < 16 * kNT ? a.tokens - t0 : 16 * kNT;
+    const u32x4 rx = raw_buffer(a.X + t0 * a.ldx, ((toks - 1) * a.ldx + a.in) * 2);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
+    auto copy_x = [&](int chunk) {  // copy i: rows 2 (wave + 8 i) and the next
+        const int64_t k = k0 + (int64_t)chunk * kFewK;
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) {
+            const int t = 2 * (wave + 8 * i) + (lane >> 5), c = (lane & 31) ^ (t & 15);
+            const uint32_t off = t < toks && k + c * 8 < k1 ? (uint32_t)((t * a.ldx + k + c * 8) * 2) : kNoRead;
+            copy_to_lds(rx, off, lds0 + (chunk & 1) * kXBytes + i * 8192);
+        }
+    };
+
+    f32x4 acc[2][kNT];
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) acc[f][n] = f32x4{0, 0, 0, 0};
+    FewWeights<kEven> w[2];
+    auto compute = [&](const FewWeights<kEven> &v, int chunk) {
+        const uint8_t *x = lds + (chunk & 1) * kXBytes + l16 * (kFewK * 2);
+        float l[2][2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            l[f][0] = e4m3fn_value(v.c[f] & 0xFF);
+            l[f][1] = e4m3fn_value(v.c[f] >> 8 & 0xFF);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            bf16x8 fx[kNT], fw[2];
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+                fx[n] = *reinterpret_cast<const bf16x8 *>(x + n * 16 * (kFewK * 2) +
+                                                          (((half * 16 + g * 4 + q) ^ l16) << 4));
+#pragma unroll
+            for (int f = 0; f < 2; ++f) fw[f] = __builtin_bit_cast(bf16x8, stored_eight(v.p[f][q], l[f][q >> 1]));
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int n = 0; n < kNT; ++n)
+                    acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[f], fx[n], acc[f][n], 0, 0, 0);
+        }
+    };
+    // A chunk's weights and X come while the chunk before it multiplies.
+    copy_x(0);
+    w[0].load(rp, rc, prow, crow, p16, c16, kl);
+    for (int i = 0; i < chunks; i += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (i + h < chunks) {
+                wait_and_barrier();
+                if (i + h + 1 < chunks) {
+                    copy_x(i + h + 1);
+                    w[1 - h].load(rp, rc, prow, crow, p16, c16, kl + (i + h + 1) * kFewK);
+                }
+                compute(w[h], i + h);
+            }
+        }
+    }
+    __syncthreads();
+
+    // The two halves of k, then out: a lane holds four consecutive rows of a token.
+    float4 *red = reinterpret_cast<float4 *>(lds);  // [4 row groups][2][kNT][64]
+    if (half == 1) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+                red[((rg * 2 + f) * kNT + n) * 64 + lane] =
+                    make_float4(acc[f][n][0], acc[f][n][1], acc[f][n][2], acc[f][n][3]);
+    }
+    __syncthreads();
+    if (half == 1) return;
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+            const float4 o = red[((rg * 2 + f) * kNT + n) * 64 + lane];
+            const float v[4] = {acc[f][n][0] + o.x, acc[f][n][1] + o.y, acc[f][n][2] + o.z, acc[f][n][3] + o.w};
+            const int64_t t = n * 16 + l16, m = rg * 32 + f * 16 + 4 * g;
+            if (t >= toks) continue;
+            float *dst = a.partial + ((int64_t)split * a.tokens + t0 + t) * a.out + r0 + m;
+            if (m + 4 <= rows && (a.out & 3) == 0) {
+                *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (m + e < rows) dst[e] = v[e];
+            }
+        }
 }
 
 struct FewFinishArgs {
@@ -460,29 +711,30 @@ __global__ __launch_bounds__(256) void few_finish(const FewFinishArgs a) {
     __shared__ float u[kMaxRank];
     const int64_t t = blockIdx.y, m = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int id = a.low ? adapter_of(a.ids, a.count, t) : kNoAdapter;
+    float y = 0.0f;
+    if (m < a.out)
+        for (int s = 0; s < a.splits; ++s) y += a.partial[((int64_t)s * a.tokens + t) * a.out + m];
+    y *= a.s_g;
     if (id != kNoAdapter) {
+        const uint16_t *b = a.B + ((int64_t)id * a.out + (m < a.out ? m : 0)) * a.rank;
+        u32x4 next = *reinterpret_cast<const u32x4 *>(b);
         if ((int)threadIdx.x < a.rank) {
             float v = 0.0f;
+#pragma unroll 4
             for (int s = 0; s < a.low_splits; ++s)
                 v += a.low[((int64_t)s * a.tokens + t) * a.rank_pad + threadIdx.x];
             u[threadIdx.x] = a.alpha ? v * a.alpha[id] : v;
         }
         __syncthreads();
-    }
-    if (m >= a.out) return;
-    float y = 0.0f;
-    for (int s = 0; s < a.splits; ++s) y += a.partial[((int64_t)s * a.tokens + t) * a.out + m];
-    y *= a.s_g;
-    if (id != kNoAdapter) {
-        const uint16_t *b = a.B + ((int64_t)id * a.out + m) * a.rank;
         for (int j = 0; j < a.rank; j += 8) {
             float v[8];
-            unpack8(*reinterpret_cast<const u32x4 *>(b + j), v);
+            unpack8(next, v);
+            if (j + 8 < a.rank) next = *reinterpret_cast<const u32x4 *>(b + j + 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y = fmaf(v[e], u[j + e], y);
         }
     }
-    a.Y[t * a.ldy + m] = (uint16_t)bf16_rne(y);
+    if (m < a.out) a.Y[t * a.ldy + m] = (uint16_t)bf16_rne(y);
 }
 
 // ---------------------------------------------------------------------------
@@ -501,99 +753,153 @@ struct OuterArgs {
 
 constexpr int kOuterCols = 128, kOuterTokens = 64;
 
-// 128 columns x 32 ranks of one adapter x one split of the tokens.  Stages of
-// 64 tokens, laid out as Stage<Across>; tokens of other adapters are not
-// read and enter as zeros, stages without any are skipped.
-template <bool kCheckpoint>
-__global__ __launch_bounds__(256) void outer_kernel(const OuterArgs a) {
+// 128 columns x 32 kRT ranks of one adapter x one split of the tokens.  Stages
+// of 64 tokens through LDS, laid out as Stage<Across>; the next stage's rows
+// are under way to registers while one multiplies.  Tokens of other adapters
+// are not read and enter as zeros, stages without any are passed over.
+template <bool kCheckpoint, int kRT>
+__global__ __launch_bounds__(256, 2) void outer_kernel(const OuterArgs a) {
     using SZ = Stage<Across, kOuterCols, 4, kOuterTokens>;
-    using SL = Stage<Across, 64, 4, kOuterTokens>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[SZ::kBytes + SL::kBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    using SL = Stage<Across, 64, 4, kOuterTokens>;  // of 32 ranks: both parts
+    constexpr int kZ = kCheckpoint ? 2 : 4, kL = 2 * kRT;  // 16-byte words a thread
+    __shared__ __attribute__((aligned(16))) uint8_t lds[SZ::kBytes + kRT * SL::kBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     const int64_t c0 = (int64_t)blockIdx.x * kOuterCols;
-    const int rank_tiles = a.rank_pad / 32;
-    const int j0 = (int)(blockIdx.y % rank_tiles) * 32, adapter = blockIdx.y / rank_tiles;
+    const int groups = (a.rank_pad / 32 + kRT - 1) / kRT;
+    const int j0 = (int)(blockIdx.y % groups) * 32 * kRT, adapter = blockIdx.y / groups;
     const int64_t t0 = (int64_t)blockIdx.z * a.t_split;
     const int64_t t1 = t0 + a.t_split < a.tokens ? t0 + a.t_split : a.tokens;
-    f32x16 acc;
+    const int64_t blocks = (a.width + kCkBlock - 1) / kCkBlock;
+
+    u32x4 z[kZ], l[kL];
+    float scale[kZ];
+    // The next stage from s on that has a token of the adapter; its rows.
+    auto fetch = [&](int64_t s) {
+        uint64_t mask = 0;
+        for (; s < t1; s += kOuterTokens) {
+            mask = __ballot(s + lane < t1 && adapter_of(a.ids, a.count, s + lane) == adapter);
+            if (mask) break;
+        }
+        if (!mask) return t1;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-    for (int64_t s = t0; s < t1; s += kOuterTokens) {
-        const bool mine = s + lane < t1 && adapter_of(a.ids, a.count, s + lane) == adapter;
-        const uint64_t mask = __ballot(mine);
-        if (mask == 0) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {  // 16 threads of 8 columns to a token
-            const int row = i * 16 + (threadIdx.x >> 4), col = (threadIdx.x & 15) * 8;
-            u32x4 v = {0, 0, 0, 0};
-            if ((mask >> row & 1) && c0 + col < a.width) {
-                const int64_t t = s + row, c = c0 + col;
-                if (kCheckpoint)
-                    v = restore8(
-                        *reinterpret_cast<const uint2 *>(reinterpret_cast<const int8_t *>(a.z.p) + t * a.width + c),
-                        a.z.scale[t * ((a.width + kCkBlock - 1) / kCkBlock) + c / kCkBlock]);
-                else
-                    v = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(a.z.p) + t * a.z.ld + c);
+        for (int i = 0; i < kZ; ++i) {  // 8 or 16 threads to a token, 16 or 8 columns each
+            const int row = kCheckpoint ? i * 32 + (tid >> 3) : i * 16 + (tid >> 4);
+            const int64_t t = s + row, c = c0 + (kCheckpoint ? (tid & 7) * 16 : (tid & 15) * 8);
+            const bool some = (mask >> row & 1) && c < a.width;
+            z[i] = u32x4{0, 0, 0, 0};
+            if (kCheckpoint) {
+                if (some) z[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const int8_t *>(a.z.p) + t * a.width + c);
+                scale[i] = some ? a.z.scale[t * blocks + blockIdx.x] : 0.0f;
+            } else if (some) {
+                z[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(a.z.p) + t * a.z.ld + c);
             }
-            *reinterpret_cast<u32x4 *>(lds + row * SZ::kRowBytes +
-                                       (((col >> 5) ^ SZ::across_swizzle(row)) << 6) + (col & 31) * 2) = v;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {  // 8 threads to a token: 4 of the first part's 32 ranks, 4 of the second's
-            const int row = i * 32 + (threadIdx.x >> 3), part = (threadIdx.x >> 2) & 1, j = (threadIdx.x & 3) * 8;
-            u32x4 v = {0, 0, 0, 0};
-            if (mask >> row & 1)
-                v = *reinterpret_cast<const u32x4 *>(a.low + (s + row) * 2 * a.rank_pad + part * a.rank_pad + j0 + j);
-            *reinterpret_cast<u32x4 *>(lds + SZ::kBytes + row * SL::kRowBytes +
-                                       ((part ^ SL::across_swizzle(row)) << 6) + j * 2) = v;
+        for (int i = 0; i < kL; ++i) {  // 8 threads to a token's 32 ranks: 4 to each part
+            const int row = (i & 1) * 32 + (tid >> 3), part = (tid >> 2) & 1, j = j0 + (i >> 1) * 32 + (tid & 3) * 8;
+            l[i] = u32x4{0, 0, 0, 0};
+            if ((mask >> row & 1) && j < a.rank_pad)
+                l[i] = *reinterpret_cast<const u32x4 *>(a.low + (s + row) * 2 * a.rank_pad + part * a.rank_pad + j);
+        }
+        return s;
+    };
+    auto put = [&](int row, int col, u32x4 v) {
+        *reinterpret_cast<u32x4 *>(lds + row * SZ::kRowBytes + (((col >> 5) ^ SZ::across_swizzle(row)) << 6) +
+                                   (col & 31) * 2) = v;
+    };
+
+    f32x16 acc[kRT];
+#pragma unroll
+    for (int r = 0; r < kRT; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[r][e] = 0.0f;
+    static_assert(kCkBlock == kOuterCols, "a block's columns have one scale a token");
+    for (int64_t s = fetch(t0); s < t1;) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kZ; ++i) {
+            if (kCheckpoint) {
+                const int row = i * 32 + (tid >> 3), col = (tid & 7) * 16;
+                put(row, col, restore8(make_uint2(z[i][0], z[i][1]), scale[i]));
+                put(row, col + 8, restore8(make_uint2(z[i][2], z[i][3]), scale[i]));
+            } else {
+                put(i * 16 + (tid >> 4), (tid & 15) * 8, z[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kL; ++i) {
+            const int row = (i & 1) * 32 + (tid >> 3), part = (tid >> 2) & 1;
+            *reinterpret_cast<u32x4 *>(lds + SZ::kBytes + (i >> 1) * SL::kBytes + row * SL::kRowBytes +
+                                       ((part ^ SL::across_swizzle(row)) << 6) + (tid & 3) * 16) = l[i];
         }
         __syncthreads();
+        s = fetch(s + kOuterTokens);
 #pragma unroll
         for (int kk = 0; kk < kOuterTokens / 16; ++kk) {
             const bf16x8 fz = SZ::read(lds, SZ::read_offset(wave * 32, kk, lane));
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const bf16x8 fl = SL::read(lds + SZ::kBytes, SL::read_offset(part * 32, kk, lane));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fz, fl, acc, 0, 0, 0);
-            }
-        }
-        __syncthreads();
-    }
-    const int j = j0 + (lane & 31);
-    if (j >= a.rank) return;
-    float *dst = a.partial + (((int64_t)blockIdx.z * a.count + adapter) * a.rank + j) * a.width;
+            for (int r = 0; r < kRT; ++r)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int64_t c = c0 + wave * 32 + 8 * q + 4 * (lane >> 5);
-        if (c < a.width)
-            *reinterpret_cast<float4 *>(dst + c) =
-                make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+                for (int part = 0; part < 2; ++part) {
+                    const bf16x8 fl = SL::read(lds + SZ::kBytes + r * SL::kBytes, SL::read_offset(part * 32, kk, lane));
+                    acc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fz, fl, acc[r], 0, 0, 0);
+                }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kRT; ++r) {
+        const int j = j0 + r * 32 + (lane & 31);
+        if (j >= a.rank) continue;
+        float *dst = a.partial + (((int64_t)blockIdx.z * a.count + adapter) * a.rank + j) * a.width;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t c = c0 + wave * 32 + 8 * q + 4 * (lane >> 5);
+            if (c < a.width)
+                *reinterpret_cast<float4 *>(dst + c) =
+                    make_float4(acc[r][4 * q], acc[r][4 * q + 1], acc[r][4 * q + 2], acc[r][4 * q + 3]);
+        }
     }
 }
 
-// `scale` times the sum of the splits as bf16: dA [count, rank, width] as it lies, or
-// dB [count, columns, rank] (columns <= width) transposed.
-template <bool kTransposed>
-__global__ __launch_bounds__(256) void outer_finish(const float *__restrict__ partial, int splits, int64_t count,
-                                                    int rank, int64_t width, int64_t columns, float scale,
-                                                    uint16_t *__restrict__ G) {
-    const int64_t total = count * rank * width, stride = (int64_t)gridDim.x * 256;
-    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
-        int64_t src = id, c = 0;
-        if (kTransposed) {
-            const int64_t a = id / (rank * width), r = id - a * rank * width;
-            c = r / rank;
-            src = (a * rank + r % rank) * width + c;
-            if (c >= columns) continue;
-            float v = 0.0f;
-            for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + src];
-            G[(a * columns + c) * rank + r % rank] = (uint16_t)bf16_rne(v * scale);
+// `scale` times the sum of the splits as bf16: dA [count, rank, width] as it
+// lies, four columns a thread.
+__global__ __launch_bounds__(256) void outer_finish(const float4 *__restrict__ partial, int splits, int64_t fours,
+                                                    float scale, uint16_t *__restrict__ G) {
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int s = 0; s < splits; ++s) {
+            const float4 o = partial[(int64_t)s * fours + id];
+            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        const uint32_t lo = bf16_pair(v.x * scale, v.y * scale), hi = bf16_pair(v.z * scale, v.w * scale);
+        uint16_t *dst = G + id * 4;
+        if ((reinterpret_cast<uintptr_t>(G) & 7) == 0) {
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
         } else {
-            float v = 0.0f;
-            for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + src];
-            G[id] = (uint16_t)bf16_rne(v * scale);
+            dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16), dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
         }
     }
+}
+
+// The same for dB [count, columns, rank], 32 columns of one adapter a block:
+// sums in along the columns, out along the ranks.
+__global__ __launch_bounds__(256) void outer_finish_turned(const float *__restrict__ partial, int splits,
+                                                           int64_t count, int rank, int64_t width, int64_t columns,
+                                                           float scale, uint16_t *__restrict__ G) {
+    __shared__ float tile[kMaxRank * 33];
+    const int64_t c0 = (int64_t)blockIdx.x * 32, a = blockIdx.y, plane = count * rank * width;
+    const int64_t c = c0 + (threadIdx.x & 31);
+    for (int r = threadIdx.x >> 5; r < rank; r += 8) {
+        float v = 0.0f;
+        if (c < columns)
+            for (int s = 0; s < splits; ++s) v += partial[s * plane + (a * rank + r) * width + c];
+        tile[r * 33 + (threadIdx.x & 31)] = v * scale;
+    }
+    __syncthreads();
+    const int n = (int)(columns - c0 < 32 ? columns - c0 : 32) * rank;
+    for (int i = threadIdx.x; i < n; i += 256)
+        G[(a * columns + c0) * rank + i] = (uint16_t)bf16_rne(tile[i % rank * 33 + i / rank]);
 }
 
 // B [count, out, rank] as [count, rank, width], width >= out, zeros beyond.
@@ -622,26 +928,26 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 
 
 constexpr int kTargetBlocks = 1024;
-constexpr int64_t kFewTokens = 64;
+constexpr int64_t kFewTokens = 64, kFewBlocks = 512;
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
 
 struct Low {
     int64_t k_split;
-    int splits, slots;
+    int splits;
 };
 
+// Ranks that a block of the product down to the rank takes.
+inline int rank_tile(int rank) { return rank <= 32 ? 32 : 64; }
+
 // Splits of k for the product down to the rank: as many as fill the chip, of
-// at least 256 k.
-inline Low low_plan(int64_t tokens, int64_t width, int count, int rank) {
+// at least 512 k.
+inline Low low_plan(int64_t tokens, int64_t width, int rank) {
     Low p;
-    const int64_t tiles = cdiv(tokens, 32) * (rank_pad(rank) / 32);
-    const int64_t fill = std::max<int64_t>(1, 4 * kTargetBlocks / tiles);
-    p.slots = (int)std::min<int64_t>(std::min<int64_t>(count, 8), std::min(tokens, fill));
-    const int64_t blocks = tiles * p.slots;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), cdiv(width, 256)));
-    p.k_split = cdiv(cdiv(width, want), 64) * 64;
+    const int64_t blocks = cdiv(tokens, 128) * cdiv(rank, rank_tile(rank));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kTargetBlocks / blocks, cdiv(width, 4 * kLowK)));
+    p.k_split = cdiv(cdiv(width, want), kLowK) * kLowK;
     p.splits = (int)cdiv(width, p.k_split);
     return p;
 }
@@ -662,11 +968,18 @@ struct Adapters {
 int shrink(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, const Adapters &ad, const Low &p,
            float *partial, hipStream_t stream) {
     const ShrinkArgs a{z, tokens, width, A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, p.k_split, partial};
-    const dim3 grid((unsigned)cdiv(tokens, 32), (unsigned)p.splits, (unsigned)(rank_pad(ad.rank) / 32 * p.slots));
-    if (z.scale)
-        hipLaunchKernelGGL((shrink_kernel<true>), grid, dim3(256), 0, stream, a, p.slots);
-    else
-        hipLaunchKernelGGL((shrink_kernel<false>), grid, dim3(256), 0, stream, a, p.slots);
+    const dim3 grid((unsigned)cdiv(tokens, 128), (unsigned)p.splits, (unsigned)cdiv(ad.rank, rank_tile(ad.rank)));
+#define SHRINK(c)                                                                    \
+    if (ad.rank <= 32)                                                               \
+        hipLaunchKernelGGL((shrink_kernel<c, 1>), grid, dim3(256), 0, stream, a);    \
+    else                                                                             \
+        hipLaunchKernelGGL((shrink_kernel<c, 2>), grid, dim3(256), 0, stream, a)
+    if (z.scale) {
+        SHRINK(true);
+    } else {
+        SHRINK(false);
+    }
+#undef SHRINK
     return launch_status();
 }
 
@@ -678,33 +991,49 @@ int shrink_to_low(const Rows &z, int64_t tokens, int64_t width, const uint16_t *
     return launch_status();
 }
 
-// The 256 x 256 tile where its blocks fill the chip at least once.
+inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
+    return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
+}
+
 template <Layout LW>
-int layer(LayerArgs a, hipStream_t stream) {
-    const int64_t m = a.W.rows, n = a.X.rows;
-    const int64_t large = cdiv(m, Large::kBM) * cdiv(n, Large::kBN);
-    if (large >= 256) {
-        a.mtiles = (unsigned)cdiv(m, Large::kBM);
-        hipLaunchKernelGGL((layer_kernel<Large, LW>), dim3((unsigned)large), dim3(Large::kThreads), 0, stream, a);
-    } else {
-        a.mtiles = (unsigned)cdiv(m, Small::kBM);
-        hipLaunchKernelGGL((layer_kernel<Small, LW>), dim3((unsigned)(a.mtiles * cdiv(n, Small::kBN))),
-                           dim3(Small::kThreads), 0, stream, a);
+int layer(LayerArgs a, const Split &p, float *sum, hipStream_t stream) {
+    const int64_t m = a.W.rows, n = a.X.rows, side = p.large ? 256 : 128;
+    a.mtiles = (unsigned)cdiv(m, side);
+    a.tiles = (unsigned)(a.mtiles * cdiv(n, side));
+    a.k_split = p.k;
+    a.sum = p.splits > 1 ? sum : nullptr;
+    const dim3 grid(a.tiles * (unsigned)p.splits);
+    if (p.large)
+        hipLaunchKernelGGL((layer_kernel<Large, LW>), grid, dim3(Large::kThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((layer_kernel<Small, LW>), grid, dim3(Small::kThreads), 0, stream, a);
+    if (const int st = launch_status()) return st;
+    if (p.splits == 1) return HSCALE_OK;
+    // rows of a grid's second dimension: at most 65535 tokens at a time
+    for (int64_t t = 0; t < n; t += 65535) {
+        const dim3 blocks((unsigned)cdiv(m, 1024), (unsigned)std::min<int64_t>(65535, n - t));
+        hipLaunchKernelGGL(layer_finish, blocks, dim3(256), 0, stream, sum + t * m, p.splits, n, m, a.scale,
+                           a.Y + t * a.ldy, a.ldy);
+        if (const int st = launch_status()) return st;
     }
-    return launch_status();
+    return HSCALE_OK;
 }
 
 struct FewPlan {
     int64_t k_split;
-    int splits;
+    int splits, low_splits, low_slots;
 };
 
-inline FewPlan few_plan(int64_t in, int64_t out) {
-    const int64_t blocks = cdiv(out, 64);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), cdiv(in, 512)));
+// Splits of k as far as they fill the chip once; every one costs its partial
+// sums once more.
+inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count) {
     FewPlan p;
-    p.k_split = cdiv(cdiv(in, want), 128) * 128;
+    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 64);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kFewBlocks / blocks, cdiv(in, kFewK)));
+    p.k_split = cdiv(cdiv(in, want), kFewK) * kFewK;
     p.splits = (int)cdiv(in, p.k_split);
+    p.low_splits = (int)cdiv(in, kFewLowK);
+    p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
     return p;
 }
 
@@ -721,6 +1050,7 @@ struct LinearPlan {
     bool few;
     FewPlan base;
     Low low;
+    Split tile;
     size_t weights, partial, low_partial, low_parts, total;
 };
 
@@ -728,15 +1058,18 @@ LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int r
     LinearPlan p{};
     p.few = tokens <= kFewTokens;
     if (p.few) {
-        p.base = few_plan(in, out);
+        p.base = few_plan(tokens, in, out, count);
         p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
+        if (count > 0) p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
     } else {
         p.weights = round_up((size_t)out * in * 2, 256);
-    }
-    if (count > 0) {
-        p.low = low_plan(tokens, in, count, rank);
-        p.low_partial = low_partial_bytes(p.low, tokens, rank);
-        if (!p.few) p.low_parts = low_bytes(tokens, rank);
+        p.tile = split_plan(out, tokens, in);
+        p.partial = sum_bytes(p.tile, out, tokens);
+        if (count > 0) {
+            p.low = low_plan(tokens, in, rank);
+            p.low_partial = low_partial_bytes(p.low, tokens, rank);
+            p.low_parts = low_bytes(tokens, rank);
+        }
     }
     p.total = p.weights + p.partial + p.low_partial + p.low_parts;
     return p;
@@ -748,12 +1081,13 @@ struct GradPlan {
     Low v, u;
     int64_t split_a, split_b;
     int splits_a, splits_b;
+    Split tile;
     size_t weights, dy, turned, low_partial, low, outer, total;
 };
 
 // Splits of the tokens for the adapters' gradients.
 inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
-    const int64_t blocks = cdiv(width, kOuterCols) * (rank_pad(rank) / 32) * count;
+    const int64_t blocks = cdiv(width, kOuterCols) * cdiv(rank, rank_tile(rank)) * count;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256)));
     split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
     splits = (int)cdiv(tokens, split);
@@ -766,13 +1100,15 @@ GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank,
     p.weights = round_up((size_t)out * in * 2, 256);
     p.dy = widen ? round_up((size_t)tokens * p.width * 2, 256) : 0;
     p.turned = round_up((size_t)count * rank * p.width * 2, 256);
-    p.v = low_plan(tokens, p.width, count, rank);
-    p.u = low_plan(tokens, in, count, rank);
+    p.v = low_plan(tokens, p.width, rank);
+    p.u = low_plan(tokens, in, rank);
     p.low_partial = std::max(low_partial_bytes(p.v, tokens, rank), low_partial_bytes(p.u, tokens, rank));
     p.low = low_bytes(tokens, rank);
     outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
     outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
     p.outer = round_up(std::max((size_t)p.splits_a * in, (size_t)p.splits_b * p.width) * count * rank * 4, 256);
+    p.tile = split_plan(in, tokens, p.width);
+    p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
     p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
     return p;
 }
@@ -835,7 +1171,7 @@ int hscale_pack_activations(const void *X, int64_t tokens, int64_t in, int64_t l
     if (!sizes_ok(tokens, in, 0) || (tokens > 1 && ldx < in)) return HSCALE_ERR_SHAPE;
     if (tokens == 0 || in == 0) return HSCALE_OK;
     if (!X || !q || !scale) return HSCALE_ERR_NULL;
-    if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(q, 8) || !aligned(scale, 4))
+    if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(q, 16) || !aligned(scale, 4))
         return HSCALE_ERR_ALIGN;
     const int64_t blocks = cdiv(in, kCkBlock);
     const Range w[] = {{q, (size_t)tokens * in}, {scale, (size_t)tokens * blocks * 4}};
@@ -851,7 +1187,7 @@ int hscale_unpack_activations(const int8_t *q, const float *scale, int64_t token
     if (!sizes_ok(tokens, in, 0) || (tokens > 1 && ldx < in)) return HSCALE_ERR_SHAPE;
     if (tokens == 0 || in == 0) return HSCALE_OK;
     if (!X || !q || !scale) return HSCALE_ERR_NULL;
-    if (!aligned(X, 2) || !aligned(q, 8) || !aligned(scale, 4)) return HSCALE_ERR_ALIGN;
+    if (!aligned(X, 2) || !aligned(q, 16) || !aligned(scale, 4)) return HSCALE_ERR_ALIGN;
     const int64_t blocks = cdiv(in, kCkBlock);
     const Range w[] = {{X, span(tokens, ldx, in, 2)}};
     const Range r[] = {{q, (size_t)tokens * in}, {scale, (size_t)tokens * blocks * 4}};
@@ -895,29 +1231,43 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     uint16_t *y = static_cast<uint16_t *>(Y);
     if (p.few) {
         float *partial = reinterpret_cast<float *>(ws), *low = reinterpret_cast<float *>(ws + p.partial);
-        if (ad.count)
-            if (const int st = shrink(x, tokens, in, ad.A, ad, p.low, low, stream)) return st;
-        const FewArgs a{scale_codes, packed_e2m1, out, in, static_cast<const uint16_t *>(X), tokens, ldx,
-                        p.base.k_split, partial};
-        const int nt = tokens <= 16 ? 1 : tokens <= 32 ? 2 : 4;
-        const dim3 grid((unsigned)cdiv(out, 64), (unsigned)p.base.splits, (unsigned)cdiv(tokens, 16 * nt));
-        if (nt == 1)
-            hipLaunchKernelGGL((few_kernel<1>), grid, dim3(256), 0, stream, a);
-        else if (nt == 2)
-            hipLaunchKernelGGL((few_kernel<2>), grid, dim3(256), 0, stream, a);
-        else
-            hipLaunchKernelGGL((few_kernel<4>), grid, dim3(256), 0, stream, a);
+        FewArgs a{scale_codes, packed_e2m1, out, in, static_cast<const uint16_t *>(X), tokens, ldx, p.base.k_split,
+                  (int)cdiv(out, kFewRows), p.base.splits, partial, 0, {}};
+        if (ad.count) {
+            a.low = FewLowArgs{a.X, tokens, ldx, in, ad.A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, low,
+                               p.base.low_splits, p.base.low_slots};
+            a.low_blocks = (int)cdiv(tokens, 32) * (rank_pad(ad.rank) / 32) * p.base.low_splits * p.base.low_slots;
+        }
+        const int nt = (int)std::min<int64_t>(cdiv(tokens, 16), 4);
+        const dim3 grid((unsigned)(a.low_blocks + (int64_t)a.row_blocks * a.splits * cdiv(tokens, 16 * nt)));
+        const bool even = in % 32 == 0 && aligned(scale_codes, 2);
+#define FEW(n)                                                                              \
+    if (even)                                                                               \
+        hipLaunchKernelGGL((few_kernel<n, true>), grid, dim3(512), 0, stream, a);           \
+    else                                                                                    \
+        hipLaunchKernelGGL((few_kernel<n, false>), grid, dim3(512), 0, stream, a)
+        if (nt == 1) {
+            FEW(1);
+        } else if (nt == 2) {
+            FEW(2);
+        } else if (nt == 3) {
+            FEW(3);
+        } else {
+            FEW(4);
+        }
+#undef FEW
         if (const int st = launch_status()) return st;
         const FewFinishArgs f{partial, p.base.splits, tokens, out, global_scale, ad.count ? low : nullptr,
-                              p.low.splits, ad.rank, rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
+                              p.base.low_splits, ad.rank, rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
         hipLaunchKernelGGL(few_finish, dim3((unsigned)cdiv(out, 256), (unsigned)tokens), dim3(256), 0, stream, f);
         return launch_status();
     }
     void *W = ws;
     float f, two_e;
     split_scale(global_scale, f, two_e);
-    float *partial = reinterpret_cast<float *>(ws + p.weights);
-    uint16_t *low = reinterpret_cast<uint16_t *>(ws + p.weights + p.low_partial);
+    float *sum = reinterpret_cast<float *>(ws += p.weights);
+    float *partial = reinterpret_cast<float *>(ws += p.partial);
+    uint16_t *low = reinterpret_cast<uint16_t *>(ws + p.low_partial);
     if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, two_e, W, stream)) return st;
     LayerArgs a{};
     if (ad.count) {
@@ -930,7 +1280,7 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     a.Y = y;
     a.ldy = ldy;
     a.wide = aligned(Y, 16) && (tokens == 1 || ldy % 8 == 0);
-    return layer<Along>(a, stream);
+    return layer<Along>(a, p.tile, sum, stream);
 }
 
 size_t hscale_adapted_linear_grad_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t count,
@@ -957,7 +1307,7 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
     GradPlan p{};
     if (tokens > 0) {
         if (!dY || !q || !scale || !scale_codes || !packed_e2m1 || !workspace) return HSCALE_ERR_NULL;
-        if (!aligned(dY, 2) || !aligned(q, 8) || !aligned(scale, 4) || !aligned(packed_e2m1, 8) || !aligned(dX, 2) ||
+        if (!aligned(dY, 2) || !aligned(q, 16) || !aligned(scale, 4) || !aligned(packed_e2m1, 8) || !aligned(dX, 2) ||
             !aligned(workspace, 256))
             return HSCALE_ERR_ALIGN;
         p = grad_plan(tokens, in, out, ad.count, ad.rank, needs_widening(dY, out, tokens > 1 ? lddy : 0));
@@ -1007,28 +1357,34 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
             a.Y = static_cast<uint16_t *>(dX);
             a.ldy = lddx;
             a.wide = aligned(dX, 16) && (tokens == 1 || lddx % 8 == 0);
-            if (const int st = layer<Across>(a, stream)) return st;
+            if (const int st = layer<Across>(a, p.tile, outer, stream)) return st;
         }
     }
     auto outer_of = [&](const Rows &z, int64_t width, int64_t columns, const uint16_t *low, int64_t split, int splits,
                         float by, void *G, bool transposed) {
         if (tokens > 0) {
             const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, split, outer};
-            const dim3 grid((unsigned)cdiv(width, kOuterCols), (unsigned)(rank_pad(ad.rank) / 32 * ad.count),
-                            (unsigned)splits);
-            if (z.scale)
-                hipLaunchKernelGGL((outer_kernel<true>), grid, dim3(256), 0, stream, a);
+            const dim3 grid((unsigned)cdiv(width, kOuterCols),
+                            (unsigned)(cdiv(ad.rank, rank_tile(ad.rank)) * ad.count), (unsigned)splits);
+            if (z.scale && ad.rank <= 32)
+                hipLaunchKernelGGL((outer_kernel<true, 1>), grid, dim3(256), 0, stream, a);
+            else if (z.scale)
+                hipLaunchKernelGGL((outer_kernel<true, 2>), grid, dim3(256), 0, stream, a);
+            else if (ad.rank <= 32)
+                hipLaunchKernelGGL((outer_kernel<false, 1>), grid, dim3(256), 0, stream, a);
             else
-                hipLaunchKernelGGL((outer_kernel<false>), grid, dim3(256), 0, stream, a);
+                hipLaunchKernelGGL((outer_kernel<false, 2>), grid, dim3(256), 0, stream, a);
             if (const int st = launch_status()) return st;
         }
-        const dim3 grid(grid_for((int64_t)ad.count * ad.rank * width, 256));
-        if (transposed)
-            hipLaunchKernelGGL((outer_finish<true>), grid, dim3(256), 0, stream, outer, splits, (int64_t)ad.count,
-                               ad.rank, width, columns, by, static_cast<uint16_t *>(G));
-        else
-            hipLaunchKernelGGL((outer_finish<false>), grid, dim3(256), 0, stream, outer, splits, (int64_t)ad.count,
-                               ad.rank, width, columns, by, static_cast<uint16_t *>(G));
+        if (transposed) {
+            hipLaunchKernelGGL(outer_finish_turned, dim3((unsigned)cdiv(columns, 32), (unsigned)ad.count), dim3(256),
+                               0, stream, outer, splits, (int64_t)ad.count, ad.rank, width, columns, by,
+                               static_cast<uint16_t *>(G));
+        } else {
+            const int64_t fours = (int64_t)ad.count * ad.rank * width / 4;
+            hipLaunchKernelGGL(outer_finish, dim3(grid_for(fours, 256)), dim3(256), 0, stream,
+                               reinterpret_cast<const float4 *>(outer), splits, fours, by, static_cast<uint16_t *>(G));
+        }
         return launch_status();
     };
     if (const int st = outer_of(x, in, in, v, p.split_a, p.splits_a, f, dA, false)) return st;

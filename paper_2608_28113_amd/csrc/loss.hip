@@ -172,28 +172,8 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dx_kernel(con
     const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.g.k ? k0 + a.k_split : a.g.k;
     Acc<T> acc;
     acc.clear();
-    if (k0 < k1) tile_product<T, Across, Along>(acc, lds, a.W, m0, a.g, n0, k0, k1);
-    const Place<T> at;
-    float *sum = a.sum + split * a.g.rows * a.W.rows;
-#pragma unroll
-    for (int j = 0; j < T::kNJ; ++j) {
-        const int64_t n = n0 + at.n(j);
-        if (n >= a.g.rows) continue;
-#pragma unroll
-        for (int i = 0; i < T::kMI; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t m = m0 + at.m(i, 4 * q);
-                if (m >= a.W.rows) continue;  // d % 16 == 0: whole fours
-                float4 *dst = reinterpret_cast<float4 *>(sum + n * a.W.rows + m);
-                float4 v = a.add ? *dst : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                v.x += acc.v[i][j][4 * q];
-                v.y += acc.v[i][j][4 * q + 1];
-                v.z += acc.v[i][j][4 * q + 2];
-                v.w += acc.v[i][j][4 * q + 3];
-                *dst = v;
-            }
-    }
+    if (k0 < k1) tile_product<T, Across, Along>(acc, lds, a.W, m0, a.g, n0, k0, k1);  // a last piece may have fewer splits
+    store_sum<T>(acc, a.sum + split * a.g.rows * a.W.rows, m0, a.W.rows, n0, a.g.rows, true, a.add);
 }
 
 __global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int splits, int64_t fours,
@@ -257,18 +237,17 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The 256 x 256 tile where its blocks fill the chip at least once.
-inline bool large_tiles(int64_t m, int64_t n) { return cdiv(m, Large::kBM) * cdiv(n, Large::kBN) >= 256; }
-inline int64_t tile_rows(int64_t m, int64_t n) { return large_tiles(m, n) ? Large::kBM : Small::kBM; }
-inline int64_t tile_cols(int64_t m, int64_t n) { return large_tiles(m, n) ? Large::kBN : Small::kBN; }
+// The tile of least estimated time for an m x n product over k.
+inline bool large_tiles(int64_t m, int64_t n, int64_t k) { return large_us(m, n, k) <= small_us(m, n, k, 1); }
+inline int64_t tile_side(int64_t m, int64_t n, int64_t k) { return large_tiles(m, n, k) ? 256 : 128; }
 
 struct LossPlan {
     size_t parts, at, total;
 };
 
-LossPlan loss_plan(int64_t tokens, int64_t vocab) {
+LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     LossPlan p;
-    p.parts = round_up((size_t)cdiv(vocab, tile_rows(vocab, tokens)) * tokens * sizeof(float2), 256);
+    p.parts = round_up((size_t)cdiv(vocab, tile_side(vocab, tokens, d)) * tokens * sizeof(float2), 256);
     p.at = round_up((size_t)tokens * 4, 256);
     p.total = p.parts + p.at;
     return p;
@@ -282,6 +261,7 @@ constexpr int64_t kPieceStep = 256;
 struct LossGradPlan {
     int64_t piece, pieces, k_split;
     int splits;
+    bool large_dx;
     size_t g, sum, rows, total;
 };
 
@@ -291,10 +271,10 @@ LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    const int64_t blocks = cdiv(d, tile_rows(d, tokens)) * cdiv(tokens, tile_cols(d, tokens));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / blocks, cdiv(p.piece, 512)));
-    p.k_split = cdiv(cdiv(p.piece, want), Large::kK) * Large::kK;
-    p.splits = (int)cdiv(p.piece, p.k_split);
+    const Split x = split_plan(d, tokens, p.piece);
+    p.large_dx = x.large;
+    p.k_split = x.k;
+    p.splits = x.splits;
     p.g = round_up((size_t)tokens * p.piece * 2, 256);
     p.sum = round_up((size_t)p.splits * tokens * d * 4, 256);
     p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
@@ -328,7 +308,7 @@ extern "C" {
 
 size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) {
     if (!loss_sizes_ok(tokens, d, vocab) || tokens == 0 || d == 0 || vocab == 0) return 0;
-    return loss_plan(tokens, vocab).total;
+    return loss_plan(tokens, d, vocab).total;
 }
 
 int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
@@ -341,7 +321,7 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
     if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(W, 16) || !aligned(target, 8) ||
         !aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 256))
         return HSCALE_ERR_ALIGN;
-    const LossPlan p = loss_plan(tokens, vocab);
+    const LossPlan p = loss_plan(tokens, d, vocab);
     if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
     const Range w[] = {{loss, (size_t)tokens * 4}, {lse, (size_t)tokens * 4}, {workspace, p.total}};
     const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8}};
@@ -353,9 +333,9 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
     a.parts = static_cast<float2 *>(workspace);
     a.at = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.parts);
     a.vocab = vocab;
-    a.mtiles = (unsigned)cdiv(vocab, tile_rows(vocab, tokens));
-    const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_cols(vocab, tokens))));
-    if (large_tiles(vocab, tokens))
+    a.mtiles = (unsigned)cdiv(vocab, tile_side(vocab, tokens, d));
+    const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_side(vocab, tokens, d))));
+    if (large_tiles(vocab, tokens, d))
         hipLaunchKernelGGL((loss_tile_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
     else
         hipLaunchKernelGGL((loss_tile_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
@@ -419,9 +399,9 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         a.weight = weight;
         a.g = g;
         a.ldg = ldg;
-        a.mtiles = (unsigned)(ldg / tile_rows(cols, tokens));
-        const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_cols(cols, tokens))));
-        if (large_tiles(cols, tokens))
+        a.mtiles = (unsigned)(ldg / tile_side(cols, tokens, d));
+        const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_side(cols, tokens, d))));
+        if (large_tiles(cols, tokens, d))
             hipLaunchKernelGGL((loss_slope_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
         else
             hipLaunchKernelGGL((loss_slope_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
@@ -430,13 +410,14 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             DxArgs x{};
             x.W = Operand{Wp, d, d, cols};
             x.g = Operand{g, ldg, tokens, ldg};
-            x.mtiles = (unsigned)cdiv(d, tile_rows(d, tokens));
-            x.tiles = (unsigned)(x.mtiles * cdiv(tokens, tile_cols(d, tokens)));
+            const int64_t side = p.large_dx ? Large::kBM : Small::kBM;
+            x.mtiles = (unsigned)cdiv(d, side);
+            x.tiles = (unsigned)(x.mtiles * cdiv(tokens, side));
             x.k_split = p.k_split;
             x.add = v0 > 0;
             x.sum = sum;
             const dim3 blocks(x.tiles * (unsigned)p.splits);
-            if (large_tiles(d, tokens))
+            if (p.large_dx)
                 hipLaunchKernelGGL((loss_dx_kernel<Large>), blocks, dim3(Large::kThreads), 0, stream, x);
             else
                 hipLaunchKernelGGL((loss_dx_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, x);
@@ -446,12 +427,12 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             DwArgs b{};
             b.X = Operand{rows, d, d, tokens};
             b.g = Operand{g, ldg, ldg, tokens};
-            b.mtiles = (unsigned)cdiv(d, tile_rows(d, cols));
+            b.mtiles = (unsigned)cdiv(d, tile_side(d, cols, tokens));
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;
             b.wide = aligned(dW, 16);
-            const dim3 blocks((unsigned)(b.mtiles * cdiv(cols, tile_cols(d, cols))));
-            if (large_tiles(d, cols))
+            const dim3 blocks((unsigned)(b.mtiles * cdiv(cols, tile_side(d, cols, tokens))));
+            if (large_tiles(d, cols, tokens))
                 hipLaunchKernelGGL((loss_dw_kernel<LargeAcross>), blocks, dim3(LargeAcross::kThreads), 0, stream, b);
             else
                 hipLaunchKernelGGL((loss_dw_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, b);

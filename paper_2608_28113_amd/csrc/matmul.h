@@ -201,7 +201,40 @@ struct Tile {
 
 typedef Tile<2, 2, 4, 4, 64, 2, 2> Large;        // 256 x 256
 typedef Tile<2, 4, 4, 2, 32, 4, 2> LargeAcross;  // the same, for two operands across
-typedef Tile<2, 2, 2, 2, 64, 2, 2> Small;        // 128 x 128, two blocks on a CU
+typedef Tile<2, 2, 2, 2, 64, 4, 2> Small;        // 128 x 128, for fewer blocks than CUs: its ring hides latency
+
+// Estimated time in us of a product in 256 x 256 or in 128 x 128 tiles and
+// `splits` of k, whose partial sums are written and read again: rounds of 256
+// blocks, each with its stages and a start and an end.
+inline double large_us(int64_t m, int64_t n, int64_t k) {
+    const int64_t rounds = ((m + 255) / 256 * ((n + 255) / 256) + 255) / 256;
+    return rounds * ((k + 63) / 64 * 1.02 + 8.0);
+}
+inline double small_us(int64_t m, int64_t n, int64_t k, int64_t splits) {
+    const int64_t rounds = ((m + 127) / 128 * ((n + 127) / 128) * splits + 255) / 256;
+    const double sums = splits > 1 ? 4.0 + splits * m * n * 8 / 5.0e6 : 0.0;
+    return rounds * (((k + 63) / 64 + splits - 1) / splits * 0.27 + 4.0) + sums;
+}
+
+struct Split {
+    bool large;
+    int64_t k;   // of a split, a multiple of 64
+    int splits;
+};
+
+// The tile, and for the small one the splits of at least 256 k, of the least
+// estimated time.
+inline Split split_plan(int64_t m, int64_t n, int64_t k) {
+    int64_t best = 1;
+    for (int64_t s = 2; s <= 32 && (k + s - 1) / s >= 256; ++s)
+        if (small_us(m, n, k, s) < small_us(m, n, k, best)) best = s;
+    Split p;
+    p.large = large_us(m, n, k) <= small_us(m, n, k, best);
+    const int64_t each = p.large ? k : (k + best - 1) / best;
+    p.k = (each + 63) / 64 * 64;
+    p.splits = (int)((k + p.k - 1) / p.k);
+    return p;
+}
 
 template <class T>
 struct Acc {
@@ -443,6 +476,36 @@ __device__ __forceinline__ void store_bf16(const Acc<T> &acc, uint8_t *lds, uint
             for (int e = 0; e < 16; ++e) {
                 const int64_t m = m0 + at.m(i, e);
                 if (m < rows) row[m] = (uint16_t)bf16_rne(acc.v[i][j][e] * scale);
+            }
+    }
+}
+
+// Writes a tile to a partial sum S[n, rows], or adds it to what is there.
+// `fours`: rows is a multiple of 4.
+template <class T>
+__device__ __forceinline__ void store_sum(const Acc<T> &acc, float *S, int64_t m0, int64_t rows, int64_t n0,
+                                          int64_t cols, bool fours, bool add) {
+    const Place<T> at;
+#pragma unroll
+    for (int j = 0; j < T::kNJ; ++j) {
+        const int64_t n = n0 + at.n(j);
+        if (n >= cols) continue;
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t m = m0 + at.m(i, 4 * q);
+                float *dst = S + n * rows + m;
+                const f32x16 &a = acc.v[i][j];
+                if (fours && m < rows) {
+                    float4 v = add ? *reinterpret_cast<float4 *>(dst) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    v.x += a[4 * q], v.y += a[4 * q + 1], v.z += a[4 * q + 2], v.w += a[4 * q + 3];
+                    *reinterpret_cast<float4 *>(dst) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (m + e < rows) dst[e] = (add ? dst[e] : 0.0f) + a[4 * q + e];
+                }
             }
     }
 }
