@@ -89,15 +89,17 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
     }
 }
 
-// Eight checkpointed values restored: bf16(q s), one rounding.
-__device__ __forceinline__ u32x4 restore8(uint2 q, float s) {
+// Eight checkpointed values restored: bf16(fp32(q s)).  A byte becomes a float
+// in one operation if it is unsigned, and (q + 128) s - 128 s in one fma rounds
+// to the same fp32(q s), as 128 s is exact.
+__device__ __forceinline__ u32x4 restore8(uint32_t lo, uint32_t hi, float s) {
+    const float less = -128.0f * s;
     u32x4 r;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t w = k < 2 ? q.x : q.y;
-        const float a = (float)(int8_t)(w >> (16 * (k & 1))) * s;
-        const float b = (float)(int8_t)(w >> (16 * (k & 1) + 8)) * s;
-        r[k] = bf16_pair(a, b);
+        const uint32_t w = (k < 2 ? lo : hi) ^ 0x80808080u;
+        r[k] = bf16_pair(fmaf((float)(w >> (16 * (k & 1)) & 0xFF), s, less),
+                         fmaf((float)(w >> (16 * (k & 1) + 8) & 0xFF), s, less));
     }
     return r;
 }
@@ -140,7 +142,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint2 *__restrict__ q
         const int64_t blk = id >> 4, t = blk / blocks, b = blk - t * blocks;
         const int64_t c = b * kCkBlock + (id & 15) * 8;
         if (c >= in) continue;
-        const u32x4 v = restore8(q[(t * in + c) >> 3], scale[blk]);
+        const uint2 w = q[(t * in + c) >> 3];
+        const u32x4 v = restore8(w.x, w.y, scale[blk]);
         uint16_t *x = X + t * ldx + c;
         if (wide) {
             *reinterpret_cast<u32x4 *>(x) = v;
@@ -155,6 +158,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint2 *__restrict__ q
 // Down to the rank: p[t, j] = sum_k z[t, k] A_a[j, k]
 // ---------------------------------------------------------------------------
 
+constexpr int kLowStep = 256;  // k of a split: a multiple of it
+
 // Activations as bf16 rows, or as a checkpoint.
 struct Rows {
     const void *p;       // bf16 [tokens, width] at ld, or int8 [tokens, width]
@@ -168,64 +173,77 @@ struct ShrinkArgs {
     const uint16_t *A;      // [count, rank, width]
     int count, rank, rank_pad;
     const int32_t *ids;
-    int64_t k_split;        // of a split, a multiple of kLowK
+    int64_t k_split;        // of a split, a multiple of kLowStep
+    int slots;
     float *partial;         // [splits, tokens, rank_pad]
 };
 
 // 128 tokens (32 a wave) x 32 kMI ranks x one split of k per block, 128 k at a
 // time; one pass for each adapter that the 128 tokens have, which reads and
-// stores only the rows of its own tokens.  Reading z bounds it: a lane takes
+// stores only the rows of its own tokens (the nth adapter by the blocks of slot
+// n modulo `slots`; a wave without such a token only keeps step).  Reading z
+// bounds it: a lane takes
 // its token's k straight into registers while the 128 k before multiply, 16
 // bytes at a time (two lanes 32 consecutive ones); the adapter's rows, the
 // same for all waves, come through LDS, 16-byte chunk c of row j at c ^ (j % 16).
-constexpr int kLowK = 128;
-
+// Checkpoints are taken 256 k at a time, so that as many bytes are under way.
 template <bool kCheckpoint, int kMI>
 __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
-    constexpr int kABytes = 32 * kMI * kLowK * 2;
-    constexpr int kLoads = kCheckpoint ? 4 : 8;  // 16 bytes a lane: 16 or 8 of the 64 k that it takes of 128
+    constexpr int kK = kCheckpoint ? 256 : 128, kARow = kK * 2, kABytes = 32 * kMI * kARow;
+    constexpr int kLoads = 8;  // 16 bytes a lane: 8 or 16 of the kK / 2 k that it takes
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kABytes];
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t t0 = (int64_t)blockIdx.x * 128, t1 = t0 + 128 < a.tokens ? t0 + 128 : a.tokens;
-    const int64_t k0 = (int64_t)blockIdx.y * a.k_split;
-    const int64_t k1 = k0 + a.k_split < a.width ? k0 + a.k_split : a.width;
-    const int stages = (int)((k1 - k0 + kLowK - 1) / kLowK);
-    const int j0 = (int)blockIdx.z * 32 * kMI, ranks = a.rank - j0 < 32 * kMI ? a.rank - j0 : 32 * kMI;
-    const int64_t t = t0 + wave * 32 + (lane & 31);
+    const int k0 = (int)(blockIdx.y * a.k_split);
+    const int k1 = (int)(k0 + a.k_split < a.width ? k0 + a.k_split : a.width), width = (int)a.width;
+    const int stages = (k1 - k0 + kK - 1) / kK;
+    const int j0 = (int)(blockIdx.z / a.slots) * 32 * kMI, ranks = a.rank - j0 < 32 * kMI ? a.rank - j0 : 32 * kMI;
+    const int trow = wave * 32 + (lane & 31);
+    const int64_t t = t0 + trow;
     const int own = t < t1 ? adapter_of(a.ids, a.count, t) : kNoAdapter;
-    const int64_t blocks = (a.width + kCkBlock - 1) / kCkBlock;
-    const char *zrow = reinterpret_cast<const char *>(a.z.p) + (kCheckpoint ? t * a.width : t * a.z.ld * 2);
+    const int blocks = (width + kCkBlock - 1) / kCkBlock;
+    const int64_t zrow = kCheckpoint ? a.width : a.z.ld * 2;  // bytes
+    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char *>(reinterpret_cast<const char *>(a.z.p)) + t0 * zrow, 0,
+        (int)((t1 - t0 - 1) * zrow + (kCheckpoint ? a.width : a.width * 2)), kRawWord3);
     const float *srow = kCheckpoint ? a.z.scale + t * blocks : nullptr;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
 
     struct Taken {
         u32x4 v[kLoads];
-        float s;
+        float s[2];
     } z[2];
-    for (int adapter = next_adapter(a.ids, a.count, t0, t1, -1); adapter != INT_MAX;
-         adapter = next_adapter(a.ids, a.count, t0, t1, adapter)) {
-        const bool mine = own == adapter;
+    int adapter = -1;
+    for (int nth = 0;; ++nth) {
+        adapter = next_adapter(a.ids, a.count, t0, t1, adapter);
+        if (adapter == INT_MAX) break;
+        if (nth % a.slots != (int)(blockIdx.z % a.slots)) continue;
+        const bool mine = own == adapter, some = __any(mine);
         const u32x4 ra = raw_buffer(a.A + ((int64_t)adapter * a.rank + j0) * a.width, ranks * a.width * 2);
         auto copy_a = [&](int stage) {
-            const int64_t k = k0 + (int64_t)stage * kLowK;
+            const int k = k0 + stage * kK;
+            constexpr int kLanes = kARow / 16, kRows = 64 / kLanes;  // of a row, in a copy
 #pragma unroll
-            for (int i = 0; i < 2 * kMI; ++i) {
-                const int row = (wave + 4 * i) * 4 + (lane >> 4);
-                const int64_t c = k + ((lane & 15) ^ (row & 15)) * 8;
-                copy_to_lds(ra, row < ranks && c < k1 ? (uint32_t)((row * a.width + c) * 2) : kNoRead,
+            for (int i = 0; i < kABytes / 4096; ++i) {
+                const int row = (wave + 4 * i) * kRows + lane / kLanes;
+                const int c = k + ((lane % kLanes) ^ (row & 15)) * 8;
+                copy_to_lds(ra, row < ranks && c < k1 ? (uint32_t)((row * width + c) * 2) : kNoRead,
                             lds0 + (stage & 1) * kABytes + i * 4096);
             }
         };
         auto take = [&](Taken &r, int stage) {
-            const int64_t k = k0 + (int64_t)stage * kLowK;
+            const int k = k0 + stage * kK;
 #pragma unroll
             for (int p = 0; p < kLoads; ++p) {
-                const int64_t c = k + (kCheckpoint ? p * 32 + h * 16 : p * 16 + h * 8);
-                r.v[p] = u32x4{0, 0, 0, 0};
-                if (mine && c < k1) r.v[p] = *reinterpret_cast<const u32x4 *>(zrow + (kCheckpoint ? c : 2 * c));
+                const int c = k + (kCheckpoint ? p * 32 + h * 16 : p * 16 + h * 8);
+                r.v[p] = __builtin_amdgcn_raw_buffer_load_b128(
+                    rz, mine && c < k1 ? (uint32_t)(trow * zrow + (kCheckpoint ? c : 2 * c)) : kNoRead, 0, 0);
             }
-            if (kCheckpoint) r.s = mine ? srow[k / kCkBlock] : 0.0f;
+            if (kCheckpoint) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) r.s[p] = mine && k + p * kCkBlock < k1 ? srow[k / kCkBlock + p] : 0.0f;
+            }
         };
         f32x16 acc[kMI];
 #pragma unroll
@@ -233,27 +251,25 @@ __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
         auto multiply = [&](const Taken &r, int stage) {
-            const uint8_t *buf = lds + (stage & 1) * kABytes + (lane & 31) * (kLowK * 2);
+            const uint8_t *buf = lds + (stage & 1) * kABytes + (lane & 31) * kARow;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
+            for (int q = 0; q < kK / 16; ++q) {
                 const int chunk = kCheckpoint ? 4 * (q >> 1) + 2 * h + (q & 1) : 2 * q + h;
-                u32x4 x;
-                if (kCheckpoint) {
-                    const u32x4 w = r.v[q >> 1 & 3];
-                    x = restore8(q & 1 ? make_uint2(w[2], w[3]) : make_uint2(w[0], w[1]), r.s);
-                } else {
-                    x = r.v[q & (kLoads - 1)];
-                }
+                const u32x4 w = r.v[kCheckpoint ? q >> 1 : q];
+                const u32x4 x = !kCheckpoint ? w
+                                : q & 1      ? restore8(w[2], w[3], r.s[q >> 3])
+                                             : restore8(w[0], w[1], r.s[q >> 3]);
 #pragma unroll
                 for (int i = 0; i < kMI; ++i) {
-                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(buf + i * 32 * (kLowK * 2) +
+                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(buf + i * 32 * kARow +
                                                                        ((chunk ^ (lane & 15)) << 4));
                     acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, __builtin_bit_cast(bf16x8, x), acc[i], 0, 0, 0);
                 }
+                if (q & 1) __builtin_amdgcn_sched_barrier(0);
             }
         };
         copy_a(0);
-        take(z[0], 0);
+        if (some) take(z[0], 0);
         for (int s = 0; s < stages; s += 2) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -261,9 +277,9 @@ __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
                     wait_and_barrier();
                     if (s + b + 1 < stages) {
                         copy_a(s + b + 1);
-                        take(z[1 - b], s + b + 1);
+                        if (some) take(z[1 - b], s + b + 1);
                     }
-                    multiply(z[b], s + b);
+                    if (some) multiply(z[b], s + b);
                 }
         }
         wait_and_barrier();
@@ -751,57 +767,72 @@ struct OuterArgs {
     float *partial;       // [splits, count, rank, width]
 };
 
-constexpr int kOuterCols = 128, kOuterTokens = 64;
+constexpr int kOuterCols = 256, kOuterTokens = 64, kOuterThreads = 512;
 
-// 128 columns x 32 kRT ranks of one adapter x one split of the tokens.  Stages
+// 256 columns x 32 kRT ranks of one adapter x one split of the tokens.  Stages
 // of 64 tokens through LDS, laid out as Stage<Across>; the next stage's rows
 // are under way to registers while one multiplies.  Tokens of other adapters
-// are not read and enter as zeros, stages without any are passed over.
+// are not read and enter as zeros, stages without any are passed over: which
+// ones have some is found for many stages at a time, so that a stage's rows
+// do not wait for its adapters' numbers.
+constexpr int kOuterMasks = 256;
+
 template <bool kCheckpoint, int kRT>
-__global__ __launch_bounds__(256, 2) void outer_kernel(const OuterArgs a) {
-    using SZ = Stage<Across, kOuterCols, 4, kOuterTokens>;
-    using SL = Stage<Across, 64, 4, kOuterTokens>;  // of 32 ranks: both parts
-    constexpr int kZ = kCheckpoint ? 2 : 4, kL = 2 * kRT;  // 16-byte words a thread
+__global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs a) {
+    using SZ = Stage<Across, kOuterCols, 8, kOuterTokens>;
+    using SL = Stage<Across, 64, 8, kOuterTokens>;  // of 32 ranks: both parts
+    constexpr int kZ = kCheckpoint ? 2 : 4;         // 16-byte words a thread
     __shared__ __attribute__((aligned(16))) uint8_t lds[SZ::kBytes + kRT * SL::kBytes];
+    __shared__ uint64_t masks[kOuterMasks];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
-    const int64_t c0 = (int64_t)blockIdx.x * kOuterCols;
+    const int c0 = (int)blockIdx.x * kOuterCols, width = (int)a.width;
     const int groups = (a.rank_pad / 32 + kRT - 1) / kRT;
     const int j0 = (int)(blockIdx.y % groups) * 32 * kRT, adapter = blockIdx.y / groups;
     const int64_t t0 = (int64_t)blockIdx.z * a.t_split;
     const int64_t t1 = t0 + a.t_split < a.tokens ? t0 + a.t_split : a.tokens;
-    const int64_t blocks = (a.width + kCkBlock - 1) / kCkBlock;
+    const int blocks = (width + kCkBlock - 1) / kCkBlock;
+    const int64_t zrow = kCheckpoint ? a.width : a.z.ld * 2;  // bytes
+    const int lrow = a.rank_pad * 4;
 
-    u32x4 z[kZ], l[kL];
+    u32x4 z[kZ], l[kRT];
     float scale[kZ];
-    // The next stage from s on that has a token of the adapter; its rows.
-    auto fetch = [&](int64_t s) {
+    // Where a thread's words lie: 16 (bf16: 32) threads to a token's columns,
+    // 8 to its 32 ranks, of which 4 to each part.
+    auto z_row = [&](int i) { return kCheckpoint ? i * 32 + (tid >> 4) : i * 16 + (tid >> 5); };
+    const int zc = kCheckpoint ? (tid & 15) * 16 : (tid & 31) * 8, l_row = tid >> 3, part = (tid >> 2) & 1;
+
+    // The next stage of a run of stages from `base` that has a token of the
+    // adapter, from the gth on: its number, and its rows under way.
+    auto fetch = [&](int64_t base, int g, int count) {
         uint64_t mask = 0;
-        for (; s < t1; s += kOuterTokens) {
-            mask = __ballot(s + lane < t1 && adapter_of(a.ids, a.count, s + lane) == adapter);
+        for (; g < count; ++g) {
+            mask = masks[g];
             if (mask) break;
         }
-        if (!mask) return t1;
+        if (g >= count) return count;
+        const int64_t s = base + (int64_t)g * kOuterTokens;
+        const int64_t rows = t1 - s < kOuterTokens ? t1 - s : kOuterTokens;
+        const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char *>(reinterpret_cast<const char *>(a.z.p)) + s * zrow, 0,
+            (int)((rows - 1) * zrow + (kCheckpoint ? a.width : a.width * 2)), kRawWord3);
+        const __amdgpu_buffer_rsrc_t rl = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint16_t *>(a.low) + s * 2 * a.rank_pad, 0, (int)(rows * lrow), kRawWord3);
 #pragma unroll
-        for (int i = 0; i < kZ; ++i) {  // 8 or 16 threads to a token, 16 or 8 columns each
-            const int row = kCheckpoint ? i * 32 + (tid >> 3) : i * 16 + (tid >> 4);
-            const int64_t t = s + row, c = c0 + (kCheckpoint ? (tid & 7) * 16 : (tid & 15) * 8);
-            const bool some = (mask >> row & 1) && c < a.width;
-            z[i] = u32x4{0, 0, 0, 0};
-            if (kCheckpoint) {
-                if (some) z[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const int8_t *>(a.z.p) + t * a.width + c);
-                scale[i] = some ? a.z.scale[t * blocks + blockIdx.x] : 0.0f;
-            } else if (some) {
-                z[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(a.z.p) + t * a.z.ld + c);
-            }
+        for (int i = 0; i < kZ; ++i) {
+            const int row = z_row(i), c = c0 + zc;
+            const bool some = (mask >> row & 1) && c < width;
+            z[i] = __builtin_amdgcn_raw_buffer_load_b128(
+                rz, some ? (uint32_t)(row * zrow + (kCheckpoint ? c : 2 * c)) : kNoRead, 0, 0);
+            if (kCheckpoint) scale[i] = some ? a.z.scale[(s + row) * blocks + c / kCkBlock] : 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < kL; ++i) {  // 8 threads to a token's 32 ranks: 4 to each part
-            const int row = (i & 1) * 32 + (tid >> 3), part = (tid >> 2) & 1, j = j0 + (i >> 1) * 32 + (tid & 3) * 8;
-            l[i] = u32x4{0, 0, 0, 0};
-            if ((mask >> row & 1) && j < a.rank_pad)
-                l[i] = *reinterpret_cast<const u32x4 *>(a.low + (s + row) * 2 * a.rank_pad + part * a.rank_pad + j);
+        for (int r = 0; r < kRT; ++r) {
+            const int j = j0 + r * 32 + (tid & 3) * 8;
+            const bool some = (mask >> l_row & 1) && j < a.rank_pad;
+            l[r] = __builtin_amdgcn_raw_buffer_load_b128(
+                rl, some ? (uint32_t)(l_row * lrow + (part * a.rank_pad + j) * 2) : kNoRead, 0, 0);
         }
-        return s;
+        return g;
     };
     auto put = [&](int row, int col, u32x4 v) {
         *reinterpret_cast<u32x4 *>(lds + row * SZ::kRowBytes + (((col >> 5) ^ SZ::across_swizzle(row)) << 6) +
@@ -813,37 +844,44 @@ __global__ __launch_bounds__(256, 2) void outer_kernel(const OuterArgs a) {
     for (int r = 0; r < kRT; ++r)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[r][e] = 0.0f;
-    static_assert(kCkBlock == kOuterCols, "a block's columns have one scale a token");
-    for (int64_t s = fetch(t0); s < t1;) {
+    for (int64_t base = t0; base < t1; base += kOuterMasks * kOuterTokens) {
+        const int64_t left = (t1 - base + kOuterTokens - 1) / kOuterTokens;
+        const int count = left < kOuterMasks ? (int)left : kOuterMasks;
         __syncthreads();
+        for (int g = wave; g < count; g += 8) {
+            const int64_t t = base + (int64_t)g * kOuterTokens + lane;
+            const uint64_t mask = __ballot(t < t1 && adapter_of(a.ids, a.count, t) == adapter);
+            if (lane == 0) masks[g] = mask;
+        }
+        __syncthreads();
+        for (int g = fetch(base, 0, count); g < count;) {
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kZ; ++i) {
-            if (kCheckpoint) {
-                const int row = i * 32 + (tid >> 3), col = (tid & 7) * 16;
-                put(row, col, restore8(make_uint2(z[i][0], z[i][1]), scale[i]));
-                put(row, col + 8, restore8(make_uint2(z[i][2], z[i][3]), scale[i]));
-            } else {
-                put(i * 16 + (tid >> 4), (tid & 15) * 8, z[i]);
+            for (int i = 0; i < kZ; ++i) {
+                if (kCheckpoint) {
+                    put(z_row(i), zc, restore8(z[i][0], z[i][1], scale[i]));
+                    put(z_row(i), zc + 8, restore8(z[i][2], z[i][3], scale[i]));
+                } else {
+                    put(z_row(i), zc, z[i]);
+                }
             }
-        }
-#pragma unroll
-        for (int i = 0; i < kL; ++i) {
-            const int row = (i & 1) * 32 + (tid >> 3), part = (tid >> 2) & 1;
-            *reinterpret_cast<u32x4 *>(lds + SZ::kBytes + (i >> 1) * SL::kBytes + row * SL::kRowBytes +
-                                       ((part ^ SL::across_swizzle(row)) << 6) + (tid & 3) * 16) = l[i];
-        }
-        __syncthreads();
-        s = fetch(s + kOuterTokens);
-#pragma unroll
-        for (int kk = 0; kk < kOuterTokens / 16; ++kk) {
-            const bf16x8 fz = SZ::read(lds, SZ::read_offset(wave * 32, kk, lane));
 #pragma unroll
             for (int r = 0; r < kRT; ++r)
+                *reinterpret_cast<u32x4 *>(lds + SZ::kBytes + r * SL::kBytes + l_row * SL::kRowBytes +
+                                           ((part ^ SL::across_swizzle(l_row)) << 6) + (tid & 3) * 16) = l[r];
+            __syncthreads();
+            g = fetch(base, g + 1, count);
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const bf16x8 fl = SL::read(lds + SZ::kBytes + r * SL::kBytes, SL::read_offset(part * 32, kk, lane));
-                    acc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fz, fl, acc[r], 0, 0, 0);
-                }
+            for (int kk = 0; kk < kOuterTokens / 16; ++kk) {
+                const bf16x8 fz = SZ::read(lds, SZ::read_offset(wave * 32, kk, lane));
+#pragma unroll
+                for (int r = 0; r < kRT; ++r)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const bf16x8 fl = SL::read(lds + SZ::kBytes + r * SL::kBytes, SL::read_offset(p * 32, kk, lane));
+                        acc[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fz, fl, acc[r], 0, 0, 0);
+                    }
+            }
         }
     }
 #pragma unroll
@@ -853,8 +891,8 @@ __global__ __launch_bounds__(256, 2) void outer_kernel(const OuterArgs a) {
         float *dst = a.partial + (((int64_t)blockIdx.z * a.count + adapter) * a.rank + j) * a.width;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int64_t c = c0 + wave * 32 + 8 * q + 4 * (lane >> 5);
-            if (c < a.width)
+            const int c = c0 + wave * 32 + 8 * q + 4 * (lane >> 5);
+            if (c < width)
                 *reinterpret_cast<float4 *>(dst + c) =
                     make_float4(acc[r][4 * q], acc[r][4 * q + 1], acc[r][4 * q + 2], acc[r][4 * q + 3]);
         }
@@ -935,7 +973,7 @@ inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
 
 struct Low {
     int64_t k_split;
-    int splits;
+    int splits, slots;
 };
 
 // Ranks that a block of the product down to the rank takes.
@@ -943,12 +981,14 @@ inline int rank_tile(int rank) { return rank <= 32 ? 32 : 64; }
 
 // Splits of k for the product down to the rank: as many as fill the chip, of
 // at least 512 k.
-inline Low low_plan(int64_t tokens, int64_t width, int rank) {
+inline Low low_plan(int64_t tokens, int64_t width, int count, int rank) {
     Low p;
     const int64_t blocks = cdiv(tokens, 128) * cdiv(rank, rank_tile(rank));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kTargetBlocks / blocks, cdiv(width, 4 * kLowK)));
-    p.k_split = cdiv(cdiv(width, want), kLowK) * kLowK;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kTargetBlocks / blocks, cdiv(width, 2 * kLowStep)));
+    p.k_split = cdiv(cdiv(width, want), kLowStep) * kLowStep;
     p.splits = (int)cdiv(width, p.k_split);
+    // a slot more costs blocks that find no adapter; few tiles leave room for them
+    p.slots = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(count, 8), 2 * kTargetBlocks / (blocks * p.splits)));
     return p;
 }
 
@@ -967,8 +1007,10 @@ struct Adapters {
 
 int shrink(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, const Adapters &ad, const Low &p,
            float *partial, hipStream_t stream) {
-    const ShrinkArgs a{z, tokens, width, A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, p.k_split, partial};
-    const dim3 grid((unsigned)cdiv(tokens, 128), (unsigned)p.splits, (unsigned)cdiv(ad.rank, rank_tile(ad.rank)));
+    const ShrinkArgs a{z, tokens, width, A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, p.k_split, p.slots,
+                       partial};
+    const dim3 grid((unsigned)cdiv(tokens, 128), (unsigned)p.splits,
+                    (unsigned)(cdiv(ad.rank, rank_tile(ad.rank)) * p.slots));
 #define SHRINK(c)                                                                    \
     if (ad.rank <= 32)                                                               \
         hipLaunchKernelGGL((shrink_kernel<c, 1>), grid, dim3(256), 0, stream, a);    \
@@ -1066,7 +1108,7 @@ LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int r
         p.tile = split_plan(out, tokens, in);
         p.partial = sum_bytes(p.tile, out, tokens);
         if (count > 0) {
-            p.low = low_plan(tokens, in, rank);
+            p.low = low_plan(tokens, in, count, rank);
             p.low_partial = low_partial_bytes(p.low, tokens, rank);
             p.low_parts = low_bytes(tokens, rank);
         }
@@ -1100,8 +1142,8 @@ GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank,
     p.weights = round_up((size_t)out * in * 2, 256);
     p.dy = widen ? round_up((size_t)tokens * p.width * 2, 256) : 0;
     p.turned = round_up((size_t)count * rank * p.width * 2, 256);
-    p.v = low_plan(tokens, p.width, rank);
-    p.u = low_plan(tokens, in, rank);
+    p.v = low_plan(tokens, p.width, count, rank);
+    p.u = low_plan(tokens, in, count, rank);
     p.low_partial = std::max(low_partial_bytes(p.v, tokens, rank), low_partial_bytes(p.u, tokens, rank));
     p.low = low_bytes(tokens, rank);
     outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
@@ -1367,13 +1409,13 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
             const dim3 grid((unsigned)cdiv(width, kOuterCols),
                             (unsigned)(cdiv(ad.rank, rank_tile(ad.rank)) * ad.count), (unsigned)splits);
             if (z.scale && ad.rank <= 32)
-                hipLaunchKernelGGL((outer_kernel<true, 1>), grid, dim3(256), 0, stream, a);
+                hipLaunchKernelGGL((outer_kernel<true, 1>), grid, dim3(kOuterThreads), 0, stream, a);
             else if (z.scale)
-                hipLaunchKernelGGL((outer_kernel<true, 2>), grid, dim3(256), 0, stream, a);
+                hipLaunchKernelGGL((outer_kernel<true, 2>), grid, dim3(kOuterThreads), 0, stream, a);
             else if (ad.rank <= 32)
-                hipLaunchKernelGGL((outer_kernel<false, 1>), grid, dim3(256), 0, stream, a);
+                hipLaunchKernelGGL((outer_kernel<false, 1>), grid, dim3(kOuterThreads), 0, stream, a);
             else
-                hipLaunchKernelGGL((outer_kernel<false, 2>), grid, dim3(256), 0, stream, a);
+                hipLaunchKernelGGL((outer_kernel<false, 2>), grid, dim3(kOuterThreads), 0, stream, a);
             if (const int st = launch_status()) return st;
         }
         if (transposed) {

@@ -53,7 +53,11 @@ __device__ __forceinline__ uint32_t bf16_rne(float f) {  // NaN stays NaN
     return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return bf16_rne(a) | (bf16_rne(b) << 16); }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {  // one conversion
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
 
