@@ -35,22 +35,54 @@ __device__ __forceinline__ int adapter_of(const int32_t *ids, int count, int64_t
     return a >= 0 && a < count ? a : kNoAdapter;
 }
 
-// The smallest adapter above `after` among tokens t0 .. t1 - 1, INT_MAX when
-// there is none; the same in all lanes of a wave.
-__device__ __forceinline__ int next_adapter(const int32_t *ids, int count, int64_t t0, int64_t t1, int after) {
-    int least = INT_MAX;
-    for (int64_t t = t0 + (threadIdx.x & 63); t < t1; t += 64) {
-        const int a = adapter_of(ids, count, t);
-        if (a > after && a < least) least = a;
-    }
+// Tells the compiler that loads to `v` are done, where wait_and_barrier() has
+// waited for them.  It does not see that wait, nor the copies to LDS issued
+// behind the loads, and its own wait before v's use would be for those.
+__device__ __forceinline__ void landed(u32x4 &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void landed(uint32_t &v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void landed(float &v) { asm volatile("" : "+v"(v)); }
+
+// The adapters that up to 64 kN tokens have, one after another, in the order
+// in which they come first; the same in all lanes of a wave.
+template <int kN>
+struct Distinct {
+    int id[kN];          // of token 64 i + lane
+    uint64_t left[kN];   // tokens whose adapter is still to come
+    __device__ __forceinline__ void read(const int32_t *ids, int count, int64_t t0, int64_t t1) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-    return __builtin_amdgcn_readfirstlane(least);
-}
+        for (int i = 0; i < kN; ++i) {
+            const int64_t t = t0 + i * 64 + lane;
+            id[i] = t < t1 ? adapter_of(ids, count, t) : kNoAdapter;
+        }
+        restart();
+    }
+    __device__ __forceinline__ void restart() {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) left[i] = __ballot(id[i] != kNoAdapter);
+    }
+    __device__ __forceinline__ int next() {  // kNoAdapter when there are no more
+        int a = kNoAdapter;
+#pragma unroll
+        for (int i = kN - 1; i >= 0; --i)
+            if (left[i]) a = __builtin_amdgcn_readlane(id[i], __builtin_ctzll(left[i]));
+        if (a == kNoAdapter) return a;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) left[i] &= ~__ballot(id[i] == a);
+        return a;
+    }
+};
 
 // ---------------------------------------------------------------------------
 // Stored weights as bf16
 // ---------------------------------------------------------------------------
+
+// The E4M3 value of a scale code times 2^e, exact and without a branch: the
+// code's fields moved to those of an fp32 stand for the value times 2^-120, the
+// subnormal ones among them.
+__device__ __forceinline__ float scale_value(uint32_t code, int e) {
+    return ldexpf(__uint_as_float(code << 20), 120 + e);
+}
 
 // Two E2M1 values of byte K of `src` times l, as a pair of bf16: exact.
 template <int K>
@@ -65,11 +97,11 @@ __device__ __forceinline__ u32x4 stored_eight(uint32_t src, float l) {
 
 // W^ [groups * 16] with 2^e in place of s_g, one group per thread.
 __global__ __launch_bounds__(256) void stored_to_bf16(const uint8_t *__restrict__ codes,
-                                                      const uint2 *__restrict__ packed, int64_t groups, float two_e,
+                                                      const uint2 *__restrict__ packed, int64_t groups, int e,
                                                       u32x4 *__restrict__ W) {
     const int64_t stride = (int64_t)gridDim.x * 256;
     for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += stride) {
-        const float l = e4m3fn_value(codes[g]) * two_e;
+        const float l = scale_value(codes[g] & 0x7F, e);
         const uint2 p = packed[g];
         W[2 * g] = stored_eight(p.x, l);
         W[2 * g + 1] = stored_eight(p.y, l);
@@ -214,10 +246,11 @@ __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
         u32x4 v[kLoads];
         float s[2];
     } z[2];
-    int adapter = -1;
+    Distinct<2> adapters;
+    adapters.read(a.ids, a.count, t0, t1);
     for (int nth = 0;; ++nth) {
-        adapter = next_adapter(a.ids, a.count, t0, t1, adapter);
-        if (adapter == INT_MAX) break;
+        const int adapter = adapters.next();
+        if (adapter == kNoAdapter) break;
         if (nth % a.slots != (int)(blockIdx.z % a.slots)) continue;
         const bool mine = own == adapter, some = __any(mine);
         const u32x4 ra = raw_buffer(a.A + ((int64_t)adapter * a.rank + j0) * a.width, ranks * a.width * 2);
@@ -275,6 +308,11 @@ __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
             for (int b = 0; b < 2; ++b)
                 if (s + b < stages) {
                     wait_and_barrier();
+                    if (some) {
+#pragma unroll
+                        for (int p = 0; p < kLoads; ++p) landed(z[b].v[p]);
+                        if (kCheckpoint) landed(z[b].s[0]), landed(z[b].s[1]);
+                    }
                     if (s + b + 1 < stages) {
                         copy_a(s + b + 1);
                         if (some) take(z[1 - b], s + b + 1);
@@ -296,6 +334,19 @@ __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
     }
 }
 
+// The sum over the splits in order, 8 loads under way at a time.
+__device__ __forceinline__ float sum_splits(const float *__restrict__ p, int splits, int64_t plane) {
+    float v = 0.0f;
+    for (int s = 0; s < splits; s += 8) {
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = s + k < splits ? p[(s + k) * plane] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += w[k];
+    }
+    return v;
+}
+
 // alpha / f times the sum of the splits (f multiplies the result that takes it),
 // or alpha times it, as two bf16 parts: low[t, j] and
 // low[t, rank_pad + j].  Tokens without an adapter are left as they are; what
@@ -312,7 +363,7 @@ __global__ __launch_bounds__(256) void shrink_finish(const float *__restrict__ p
         if (a == kNoAdapter) continue;
         float v = 0.0f;
         if (j < rank) {
-            for (int s = 0; s < splits; ++s) v += partial[(int64_t)s * total + id];
+            v = sum_splits(partial + id, splits, total);
             if (alpha) v *= alpha[a];
             v /= f;
         }
@@ -348,9 +399,9 @@ struct LowRankStages {
     const LowRank &w;
     int64_t m0, prows, n0, n1;
     int wave, lane;
-    int tile[T::kBN / 64];       // adapters of the tile's tokens, over the wave
+    Distinct<T::kBN / 64> adapters;
     int copied[SQ::kCopies];     // of the rows that this lane copies
-    int adapter = -1, step = 0;  // of the next stage
+    int adapter = kNoAdapter, step = 0;  // of the next stage
 
     __device__ __forceinline__ LowRankStages(const LowRank &low, bool some, int64_t m, int64_t rows, int64_t n,
                                              int64_t tokens)
@@ -360,25 +411,16 @@ struct LowRankStages {
         wave = at.wm + at.wn * T::kWM;
         lane = at.lane;
         if (!w.low || !some) return;
+        adapters.read(w.ids, w.count, n0, n1);
 #pragma unroll
-        for (int i = 0; i < T::kBN / 64; ++i) tile[i] = of(i * 64 + lane);
-#pragma unroll
-        for (int i = 0; i < SQ::kCopies; ++i) copied[i] = of(SQ::row_of(i, wave, lane));
-        for (int a = next(-1); a != INT_MAX; a = next(a)) stages += per_adapter();
-    }
-    __device__ __forceinline__ int of(int row) const {
-        return n0 + row < n1 ? adapter_of(w.ids, w.count, n0 + row) : kNoAdapter;
+        for (int i = 0; i < SQ::kCopies; ++i) {
+            const int row = SQ::row_of(i, wave, lane);
+            copied[i] = n0 + row < n1 ? adapter_of(w.ids, w.count, n0 + row) : kNoAdapter;
+        }
+        while (adapters.next() != kNoAdapter) stages += per_adapter();
+        adapters.restart();
     }
     __device__ __forceinline__ int per_adapter() const { return (2 * w.rank_pad + T::kK - 1) / T::kK; }
-    __device__ __forceinline__ int next(int after) const {
-        int least = INT_MAX;
-#pragma unroll
-        for (int i = 0; i < T::kBN / 64; ++i)
-            if (tile[i] > after) least = min(least, tile[i]);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-        return __builtin_amdgcn_readfirstlane(least);
-    }
     // Column of the adapter's rank that k of its stages stands for, or none.
     __device__ __forceinline__ int column(int k) const {
         const int j = k >= w.rank_pad ? k - w.rank_pad : k;
@@ -389,7 +431,7 @@ struct LowRankStages {
             sp.left = sq.left = 0;
             return;
         }
-        if (step == 0) adapter = next(adapter);
+        if (step == 0) adapter = adapters.next();
         const int k0 = step * T::kK, deep = 2 * w.rank_pad;
         step = step + 1 == per_adapter() ? 0 : step + 1;
         const uint16_t *P = w.other + (int64_t)adapter * w.other_size + (LP == Along ? m0 * w.ld : m0);
@@ -501,14 +543,11 @@ __device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t 
     const int64_t t0 = (int64_t)(rest / rank_tiles) * 32, t1 = t0 + 32 < a.tokens ? t0 + 32 : a.tokens;
     const int64_t t = t0 + (lane & 31);
     const int own = t < t1 ? adapter_of(a.ids, a.count, t) : kNoAdapter;
-    bool first = lane < 32 && own != kNoAdapter;
-#pragma unroll
-    for (int k = 0; k < 31; ++k)
-        if (__builtin_amdgcn_readlane(own, k) == own && lane > k) first = false;
-    uint64_t mask = __ballot(first);
-    for (int nth = 0; nth < slot; ++nth) mask &= mask - 1;
-    if (mask == 0) return;
-    const int adapter = __builtin_amdgcn_readlane(own, __builtin_ctzll(mask));
+    Distinct<1> adapters;
+    adapters.read(a.ids, a.count, t0, t1);
+    int adapter = adapters.next();
+    for (int nth = 0; nth < slot && adapter != kNoAdapter; ++nth) adapter = adapters.next();
+    if (adapter == kNoAdapter) return;
     const uint16_t *Arow = a.A + ((int64_t)adapter * a.rank + j) * a.in;
     const uint16_t *Xrow = a.X + t * a.ldx;
     const int64_t c0 = (int64_t)split * kFewLowK + wave * (kFewLowK / 8) + 8 * (lane >> 5);
@@ -545,13 +584,13 @@ __device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t 
 }
 
 // W^ against few tokens: 128 output rows x 16 kNT tokens x one split of k per
-// block.  8 waves: 32 rows each, and each half of a 256-k chunk its own four.
+// block.  8 waves: 32 rows each, and each half of a chunk of k its own four.
 // HBM bounds it for few tokens, the conversion of the weights (about 11 cycles
 // for two per lane) and LDS reads of X for 64.  A wave's MFMA operand of
 // weights comes straight from memory, 32 consecutive weights a lane: which k
 // meets which place in a step does not matter, as both operands agree.  X goes
 // through LDS, 16 bytes a lane, row t's 16-byte chunk c at c ^ (t % 16).
-constexpr int kFewK = 256, kFewRows = 128;
+constexpr int kFewK = 512, kFewRows = 128;  // a split is a multiple of kFewK
 
 struct FewArgs {
     const uint8_t *codes;
@@ -561,34 +600,56 @@ struct FewArgs {
     int64_t tokens, ldx;
     int64_t k_split;  // a multiple of kFewK
     int row_blocks, splits;
-    float *partial;   // [splits, tokens, out]
-    int low_blocks;   // the first blocks go down to the rank
+    int e;            // 2^e in place of s_g = f 2^e
+    float *partial;   // [splits, tokens, out]; NULL: one split, f times it written to Y
+    float f;
+    uint16_t *Y;
+    int64_t ldy;
+    bool wide;        // rows of Y are 8-byte aligned
+    int low_blocks;   // the first blocks go down to the rank (then the adapters' part is few_finish's)
     FewLowArgs low;
+    LowRank rank;     // or it is added here: rank.low not NULL
 };
 
-template <bool kEven>  // in % 32 == 0: a lane's two scales are one aligned word
+template <bool kEven, int kNF, int kDepth>  // kEven: in % 32 == 0, a lane's two scales are one aligned word
 struct FewWeights {
-    u32x4 p[2];
-    uint32_t c[2];
-    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t rp, const __amdgpu_buffer_rsrc_t rc,
-                                         uint32_t prow, uint32_t crow, uint32_t p16, uint32_t c16, uint32_t k) {
+    u32x4 p[kNF][kDepth];
+    uint32_t c[kNF][kDepth];
+    __device__ __forceinline__ void landed_all() {
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            p[f] = __builtin_amdgcn_raw_buffer_load_b128(rp, prow + f * p16 + k / 2, 0, 0);
-            if (kEven) {
-                c[f] = __builtin_amdgcn_raw_buffer_load_b16(rc, crow + f * c16 + k / 16, 0, 0);
-            } else {
-                c[f] = __builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16, 0, 0);
-                c[f] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16 + 1, 0, 0) << 8;
+        for (int f = 0; f < kNF; ++f)
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                landed(p[f][d]);
+                landed(c[f][d]);
             }
-        }
+    }
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t rp, const __amdgpu_buffer_rsrc_t rc,
+                                         uint32_t prow, uint32_t crow, uint32_t p16, uint32_t c16, uint32_t k0) {
+#pragma unroll
+        for (int f = 0; f < kNF; ++f)
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                const uint32_t k = k0 + d * 128;
+                p[f][d] = __builtin_amdgcn_raw_buffer_load_b128(rp, prow + f * p16 + k / 2, 0, 0);
+                if (kEven) {
+                    c[f][d] = __builtin_amdgcn_raw_buffer_load_b16(rc, crow + f * c16 + k / 16, 0, 0);
+                } else {
+                    c[f][d] = __builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16, 0, 0);
+                    c[f][d] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rc, crow + f * c16 + k / 16 + 1, 0, 0)
+                               << 8;
+                }
+            }
     }
 };
 
 template <int kNT, bool kEven>
-__global__ __launch_bounds__(512, 4) void few_kernel(const FewArgs a) {
-    constexpr int kXBytes = 16 * kNT * kFewK * 2;
-    constexpr int kLdsBytes = 2 * kXBytes > 8 * 4096 ? 2 * kXBytes : 8 * 4096;
+__global__ __launch_bounds__(512, kNT <= 4 ? 4 : 2) void few_kernel(const FewArgs a) {
+    constexpr int kNF = kFewRows / 64;
+    constexpr int kDepth = kNT <= 2 ? 2 : 1;  // 128 k of a half at a time
+    constexpr int kK = 256 * kDepth, kXRow = kK * 2, kXBytes = 16 * kNT * kXRow;
+    constexpr int kRedBytes = 4 * kNF * kNT * 1024;
+    constexpr int kLdsBytes = std::max(std::max(2 * kXBytes, kRedBytes), 8 * 4096);
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
     if ((int)blockIdx.x < a.low_blocks) {
         few_low(a.low, blockIdx.x, lds);
@@ -603,7 +664,7 @@ __global__ __launch_bounds__(512, 4) void few_kernel(const FewArgs a) {
     const int64_t t0 = (int64_t)(block / a.row_blocks / a.splits) * 16 * kNT;
     const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.in ? k0 + a.k_split : a.in;
     const int64_t rows = a.out - r0 < kFewRows ? a.out - r0 : kFewRows;
-    const int chunks = (int)((k1 - k0 + kFewK - 1) / kFewK);
+    const int chunks = (int)((k1 - k0 + kK - 1) / kK);
 
     // Weights past a row's end are the next row's, and meet zeros of X; past
     // the block's last row they read as zeros.
@@ -611,92 +672,146 @@ __global__ __launch_bounds__(512, 4) void few_kernel(const FewArgs a) {
         const_cast<uint8_t *>(a.packed + r0 * (a.in / 2)), 0, (int)(rows * (a.in / 2)), kRawWord3);
     const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint8_t *>(a.codes + r0 * (a.in / kGroup)), 0, (int)(rows * (a.in / kGroup)), kRawWord3);
-    const uint32_t row = rg * 32 + l16;
+    const uint32_t row = rg * 16 * kNF + l16;
     const uint32_t prow = row * (uint32_t)(a.in / 2), crow = row * (uint32_t)(a.in / kGroup);
     const uint32_t p16 = 16 * (uint32_t)(a.in / 2), c16 = 16 * (uint32_t)(a.in / kGroup);
-    const uint32_t kl = (uint32_t)k0 + half * 128 + g * 32;
+    const uint32_t kl = (uint32_t)k0 + half * 128 * kDepth + g * 32;
 
     const int64_t toks = a.tokens - t0 < 16 * kNT ? a.tokens - t0 : 16 * kNT;
     const u32x4 rx = raw_buffer(a.X + t0 * a.ldx, ((toks - 1) * a.ldx + a.in) * 2);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * 1024;
-    auto copy_x = [&](int chunk) {  // copy i: rows 2 (wave + 8 i) and the next
-        const int64_t k = k0 + (int64_t)chunk * kFewK;
+    auto copy_x = [&](int chunk, int buf) {  // a copy: 2 or 1 rows
+        const int64_t k = k0 + (int64_t)chunk * kK;
+        constexpr int kLanes = kXRow / 16, kRows = 64 / kLanes;
 #pragma unroll
-        for (int i = 0; i < kNT; ++i) {
-            const int t = 2 * (wave + 8 * i) + (lane >> 5), c = (lane & 31) ^ (t & 15);
+        for (int i = 0; i < kXBytes / 8192; ++i) {
+            const int t = (wave + 8 * i) * kRows + lane / kLanes, c = (lane % kLanes) ^ (t & 15);
             const uint32_t off = t < toks && k + c * 8 < k1 ? (uint32_t)((t * a.ldx + k + c * 8) * 2) : kNoRead;
-            copy_to_lds(rx, off, lds0 + (chunk & 1) * kXBytes + i * 8192);
+            copy_to_lds(rx, off, lds0 + buf * kXBytes + i * 8192);
         }
     };
 
-    f32x4 acc[2][kNT];
+    f32x4 acc[kNF][kNT];
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < kNF; ++f)
 #pragma unroll
         for (int n = 0; n < kNT; ++n) acc[f][n] = f32x4{0, 0, 0, 0};
-    FewWeights<kEven> w[2];
-    auto compute = [&](const FewWeights<kEven> &v, int chunk) {
-        const uint8_t *x = lds + (chunk & 1) * kXBytes + l16 * (kFewK * 2);
-        float l[2][2];
+    FewWeights<kEven, kNF, kDepth> w[2];
+    auto compute = [&](const FewWeights<kEven, kNF, kDepth> &v, int buf) {
+        const uint8_t *x = lds + buf * kXBytes + l16 * kXRow;
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            l[f][0] = e4m3fn_value(v.c[f] & 0xFF);
-            l[f][1] = e4m3fn_value(v.c[f] >> 8 & 0xFF);
-        }
+        for (int d = 0; d < kDepth; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            bf16x8 fx[kNT], fw[2];
-#pragma unroll
-            for (int n = 0; n < kNT; ++n)
-                fx[n] = *reinterpret_cast<const bf16x8 *>(x + n * 16 * (kFewK * 2) +
-                                                          (((half * 16 + g * 4 + q) ^ l16) << 4));
-#pragma unroll
-            for (int f = 0; f < 2; ++f) fw[f] = __builtin_bit_cast(bf16x8, stored_eight(v.p[f][q], l[f][q >> 1]));
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
+            for (int q = 0; q < 4; ++q) {
+                bf16x8 fx[kNT], fw[kNF];
 #pragma unroll
                 for (int n = 0; n < kNT; ++n)
-                    acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[f], fx[n], acc[f][n], 0, 0, 0);
-        }
+                    fx[n] = *reinterpret_cast<const bf16x8 *>(
+                        x + n * 16 * kXRow + (((half * 16 * kDepth + d * 16 + g * 4 + q) ^ l16) << 4));
+#pragma unroll
+                for (int f = 0; f < kNF; ++f)
+                    fw[f] = __builtin_bit_cast(
+                        bf16x8,
+                        stored_eight(v.p[f][d][q], scale_value(v.c[f][d] >> (8 * (q >> 1)) & 0x7F, a.e)));
+#pragma unroll
+                for (int f = 0; f < kNF; ++f)
+#pragma unroll
+                    for (int n = 0; n < kNT; ++n)
+                        acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[f], fx[n], acc[f][n], 0, 0, 0);
+                if (kNF * kNT > 8) __builtin_amdgcn_sched_barrier(0);  // one step's operands at a time
+            }
     };
-    // A chunk's weights and X come while the chunk before it multiplies.
-    copy_x(0);
+    // A chunk's weights and X come while the one before it multiplies.  (Two
+    // chunks ahead is slower: the LDS for a third takes the second block from
+    // the CU.)
+    copy_x(0, 0);
     w[0].load(rp, rc, prow, crow, p16, c16, kl);
     for (int i = 0; i < chunks; i += 2) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (i + h < chunks) {
                 wait_and_barrier();
+                w[h].landed_all();
                 if (i + h + 1 < chunks) {
-                    copy_x(i + h + 1);
-                    w[1 - h].load(rp, rc, prow, crow, p16, c16, kl + (i + h + 1) * kFewK);
+                    copy_x(i + h + 1, 1 - h);
+                    w[1 - h].load(rp, rc, prow, crow, p16, c16, kl + (i + h + 1) * kK);
                 }
-                compute(w[h], i + h);
+                compute(w[h], h);
             }
         }
     }
-    __syncthreads();
+    wait_and_barrier();
+
+    // The adapters' part, once: for each adapter that the tokens have, its rows
+    // of B against both parts of low; tokens of others enter as zeros.
+    if (a.rank.low && split == 0 && half == 0) {
+        const LowRank &w = a.rank;
+        int own[kNT];
+#pragma unroll
+        for (int n = 0; n < kNT; ++n)
+            own[n] = n * 16 + l16 < toks ? adapter_of(w.ids, w.count, t0 + n * 16 + l16) : kNoAdapter;
+        Distinct<(kNT + 3) / 4> adapters;
+        adapters.read(w.ids, w.count, t0, t0 + toks);
+        for (int adapter = adapters.next(); adapter != kNoAdapter; adapter = adapters.next()) {
+            const uint16_t *B = w.other + adapter * w.other_size + (r0 + row) * w.rank;
+            for (int k = g * 8; k < 2 * w.rank_pad; k += 32) {
+                const int j = k >= w.rank_pad ? k - w.rank_pad : k;
+                u32x4 fw[kNF], fx[kNT];
+#pragma unroll
+                for (int f = 0; f < kNF; ++f) {
+                    fw[f] = u32x4{0, 0, 0, 0};
+                    if (j < w.rank && (int64_t)row + f * 16 < rows)
+                        fw[f] = *reinterpret_cast<const u32x4 *>(B + f * 16 * w.rank + j);
+                }
+#pragma unroll
+                for (int n = 0; n < kNT; ++n) {
+                    fx[n] = u32x4{0, 0, 0, 0};
+                    if (own[n] == adapter)
+                        fx[n] = *reinterpret_cast<const u32x4 *>(w.low + (t0 + n * 16 + l16) * 2 * w.rank_pad + k);
+                }
+#pragma unroll
+                for (int f = 0; f < kNF; ++f)
+#pragma unroll
+                    for (int n = 0; n < kNT; ++n)
+                        acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[f]),
+                                                                            __builtin_bit_cast(bf16x8, fx[n]),
+                                                                            acc[f][n], 0, 0, 0);
+            }
+        }
+    }
 
     // The two halves of k, then out: a lane holds four consecutive rows of a token.
-    float4 *red = reinterpret_cast<float4 *>(lds);  // [4 row groups][2][kNT][64]
+    float4 *red = reinterpret_cast<float4 *>(lds);  // [4 row groups][kNF][kNT][64]
     if (half == 1) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < kNF; ++f)
 #pragma unroll
             for (int n = 0; n < kNT; ++n)
-                red[((rg * 2 + f) * kNT + n) * 64 + lane] =
+                red[((rg * kNF + f) * kNT + n) * 64 + lane] =
                     make_float4(acc[f][n][0], acc[f][n][1], acc[f][n][2], acc[f][n][3]);
     }
     __syncthreads();
     if (half == 1) return;
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < kNF; ++f)
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
-            const float4 o = red[((rg * 2 + f) * kNT + n) * 64 + lane];
+            const float4 o = red[((rg * kNF + f) * kNT + n) * 64 + lane];
             const float v[4] = {acc[f][n][0] + o.x, acc[f][n][1] + o.y, acc[f][n][2] + o.z, acc[f][n][3] + o.w};
-            const int64_t t = n * 16 + l16, m = rg * 32 + f * 16 + 4 * g;
+            const int64_t t = n * 16 + l16, m = (rg * kNF + f) * 16 + 4 * g;
             if (t >= toks) continue;
+            if (!a.partial) {
+                uint16_t *dst = a.Y + (t0 + t) * a.ldy + r0 + m;
+                const uint32_t lo = bf16_pair(v[0] * a.f, v[1] * a.f), hi = bf16_pair(v[2] * a.f, v[3] * a.f);
+                if (m + 4 <= rows && a.wide) {
+                    *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (m + e < rows) dst[e] = (uint16_t)((e < 2 ? lo : hi) >> (16 * (e & 1)));
+                }
+                continue;
+            }
             float *dst = a.partial + ((int64_t)split * a.tokens + t0 + t) * a.out + r0 + m;
             if (m + 4 <= rows && (a.out & 3) == 0) {
                 *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
@@ -712,7 +827,7 @@ struct FewFinishArgs {
     const float *partial;  // [splits, tokens, out]
     int splits;
     int64_t tokens, out;
-    float s_g;
+    float f;
     const float *low;      // [low_splits, tokens, rank_pad], NULL: no adapters
     int low_splits, rank, rank_pad, count;
     const uint16_t *B;     // [count, out, rank]
@@ -727,18 +842,13 @@ __global__ __launch_bounds__(256) void few_finish(const FewFinishArgs a) {
     __shared__ float u[kMaxRank];
     const int64_t t = blockIdx.y, m = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int id = a.low ? adapter_of(a.ids, a.count, t) : kNoAdapter;
-    float y = 0.0f;
-    if (m < a.out)
-        for (int s = 0; s < a.splits; ++s) y += a.partial[((int64_t)s * a.tokens + t) * a.out + m];
-    y *= a.s_g;
+    const int64_t plane = a.tokens * a.out, low_plane = a.tokens * a.rank_pad;
+    float y = m < a.out ? sum_splits(a.partial + t * a.out + m, a.splits, plane) * a.f : 0.0f;
     if (id != kNoAdapter) {
         const uint16_t *b = a.B + ((int64_t)id * a.out + (m < a.out ? m : 0)) * a.rank;
         u32x4 next = *reinterpret_cast<const u32x4 *>(b);
         if ((int)threadIdx.x < a.rank) {
-            float v = 0.0f;
-#pragma unroll 4
-            for (int s = 0; s < a.low_splits; ++s)
-                v += a.low[((int64_t)s * a.tokens + t) * a.rank_pad + threadIdx.x];
+            const float v = sum_splits(a.low + t * a.rank_pad + threadIdx.x, a.low_splits, low_plane);
             u[threadIdx.x] = a.alpha ? v * a.alpha[id] : v;
         }
         __syncthreads();
@@ -929,9 +1039,7 @@ __global__ __launch_bounds__(256) void outer_finish_turned(const float *__restri
     const int64_t c0 = (int64_t)blockIdx.x * 32, a = blockIdx.y, plane = count * rank * width;
     const int64_t c = c0 + (threadIdx.x & 31);
     for (int r = threadIdx.x >> 5; r < rank; r += 8) {
-        float v = 0.0f;
-        if (c < columns)
-            for (int s = 0; s < splits; ++s) v += partial[s * plane + (a * rank + r) * width + c];
+        const float v = c < columns ? sum_splits(partial + (a * rank + r) * width + c, splits, plane) : 0.0f;
         tile[r * 33 + (threadIdx.x & 31)] = v * scale;
     }
     __syncthreads();
@@ -966,7 +1074,7 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 
 
 constexpr int kTargetBlocks = 1024;
-constexpr int64_t kFewTokens = 64, kFewBlocks = 512;
+constexpr int64_t kFewTokens = 1024, kFewFused = 128;
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
@@ -1037,9 +1145,20 @@ inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
     return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
 }
 
+int sum_of_splits(const float *sum, int splits, int64_t tokens, int64_t m, float scale, uint16_t *Y, int64_t ldy,
+                  hipStream_t stream) {
+    for (int64_t t = 0; t < tokens; t += 65535) {  // as many rows has a grid
+        const dim3 blocks((unsigned)cdiv(m, 1024), (unsigned)std::min<int64_t>(65535, tokens - t));
+        hipLaunchKernelGGL(layer_finish, blocks, dim3(256), 0, stream, sum + t * m, splits, tokens, m, scale,
+                           Y + t * ldy, ldy);
+        if (const int st = launch_status()) return st;
+    }
+    return HSCALE_OK;
+}
+
 template <Layout LW>
 int layer(LayerArgs a, const Split &p, float *sum, hipStream_t stream) {
-    const int64_t m = a.W.rows, n = a.X.rows, side = p.large ? 256 : 128;
+    const int64_t m = a.W.rows, n = a.X.rows, side = p.side();
     a.mtiles = (unsigned)cdiv(m, side);
     a.tiles = (unsigned)(a.mtiles * cdiv(n, side));
     a.k_split = p.k;
@@ -1050,28 +1169,24 @@ int layer(LayerArgs a, const Split &p, float *sum, hipStream_t stream) {
     else
         hipLaunchKernelGGL((layer_kernel<Small, LW>), grid, dim3(Small::kThreads), 0, stream, a);
     if (const int st = launch_status()) return st;
-    if (p.splits == 1) return HSCALE_OK;
-    // rows of a grid's second dimension: at most 65535 tokens at a time
-    for (int64_t t = 0; t < n; t += 65535) {
-        const dim3 blocks((unsigned)cdiv(m, 1024), (unsigned)std::min<int64_t>(65535, n - t));
-        hipLaunchKernelGGL(layer_finish, blocks, dim3(256), 0, stream, sum + t * m, p.splits, n, m, a.scale,
-                           a.Y + t * a.ldy, a.ldy);
-        if (const int st = launch_status()) return st;
-    }
-    return HSCALE_OK;
+    return p.splits > 1 ? sum_of_splits(sum, p.splits, n, m, a.scale, a.Y, a.ldy, stream) : HSCALE_OK;
 }
 
 struct FewPlan {
     int64_t k_split;
     int splits, low_splits, low_slots;
+    bool fused;  // the adapters' part beside the weights' and in the end, not before and with them
+    int tile;    // tokens a block, in sixteens
 };
 
 // Splits of k as far as they fill the chip once; every one costs its partial
 // sums once more.
 inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count) {
     FewPlan p;
-    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 64);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kFewBlocks / blocks, cdiv(in, kFewK)));
+    p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
+    p.fused = tokens <= kFewFused;
+    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), room = p.tile > 4 ? kCUs : 2 * kCUs;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(room / blocks, cdiv(in, kFewK)));
     p.k_split = cdiv(cdiv(in, want), kFewK) * kFewK;
     p.splits = (int)cdiv(in, p.k_split);
     p.low_splits = (int)cdiv(in, kFewLowK);
@@ -1101,17 +1216,18 @@ LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int r
     p.few = tokens <= kFewTokens;
     if (p.few) {
         p.base = few_plan(tokens, in, out, count);
-        p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
-        if (count > 0) p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
+        if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
     } else {
         p.weights = round_up((size_t)out * in * 2, 256);
-        p.tile = split_plan(out, tokens, in);
+        p.tile = split_plan(out, tokens, in, true);
         p.partial = sum_bytes(p.tile, out, tokens);
-        if (count > 0) {
-            p.low = low_plan(tokens, in, count, rank);
-            p.low_partial = low_partial_bytes(p.low, tokens, rank);
-            p.low_parts = low_bytes(tokens, rank);
-        }
+    }
+    if (count > 0 && p.few && p.base.fused) {
+        p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
+    } else if (count > 0) {
+        p.low = low_plan(tokens, in, count, rank);
+        p.low_partial = low_partial_bytes(p.low, tokens, rank);
+        p.low_parts = low_bytes(tokens, rank);
     }
     p.total = p.weights + p.partial + p.low_partial + p.low_parts;
     return p;
@@ -1149,7 +1265,7 @@ GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank,
     outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
     outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
     p.outer = round_up(std::max((size_t)p.splits_a * in, (size_t)p.splits_b * p.width) * count * rank * 4, 256);
-    p.tile = split_plan(in, tokens, p.width);
+    p.tile = split_plan(in, tokens, p.width, true);
     p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
     p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
     return p;
@@ -1174,10 +1290,9 @@ int check_adapters(const hscale_adapters *w, Adapters &ad) {
 }
 
 // s = f 2^e with 1 <= f < 2.
-inline void split_scale(float s, float &f, float &two_e) {
-    int e;
+inline void split_scale(float s, float &f, int &e) {
     f = 2.0f * std::frexp(s, &e);
-    two_e = std::ldexp(1.0f, e - 1);
+    --e;
 }
 
 struct Range {
@@ -1196,11 +1311,11 @@ bool any_overlap(const Range *w, int nw, const Range *r, int nr) {
     return false;
 }
 
-int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, float two_e, void *W,
+int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, int e, void *W,
                    hipStream_t stream) {
     const int64_t groups = out * (in / kGroup);
     hipLaunchKernelGGL(stored_to_bf16, dim3(grid_for(groups, 256)), dim3(256), 0, stream, codes,
-                       reinterpret_cast<const uint2 *>(packed), groups, two_e, static_cast<u32x4 *>(W));
+                       reinterpret_cast<const uint2 *>(packed), groups, e, static_cast<u32x4 *>(W));
     return launch_status();
 }
 
@@ -1255,11 +1370,11 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     if (!scale_ok(global_scale)) return HSCALE_ERR_SCALE;
     Adapters ad;
     if (const int st = check_adapters(adapters, ad)) return st;
-    if (!X || !scale_codes || !packed_e2m1 || !Y || !workspace) return HSCALE_ERR_NULL;
+    const LinearPlan p = linear_plan(tokens, in, out, ad.count, ad.rank);
+    if (!X || !scale_codes || !packed_e2m1 || !Y || (!workspace && p.total)) return HSCALE_ERR_NULL;
     if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(packed_e2m1, 8) || !aligned(Y, 2) ||
         !aligned(workspace, 256))
         return HSCALE_ERR_ALIGN;
-    const LinearPlan p = linear_plan(tokens, in, out, ad.count, ad.rank);
     if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
     const size_t low_size = (size_t)ad.count * ad.rank * 2;
     const Range w[] = {{Y, span(tokens, ldy, out, 2)}, {workspace, p.total}};
@@ -1271,16 +1386,38 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     char *ws = static_cast<char *>(workspace);
     const Rows x{X, nullptr, ldx};
     uint16_t *y = static_cast<uint16_t *>(Y);
+    float f;
+    int e;
+    split_scale(global_scale, f, e);
+    void *W = ws;
+    float *sum = reinterpret_cast<float *>(ws += p.weights);
+    float *low_sum = reinterpret_cast<float *>(ws += p.partial);
+    uint16_t *low = reinterpret_cast<uint16_t *>(ws + p.low_partial);
+    LowRank rank{};
+    if (p.low_parts) {
+        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.low, f, low_sum, low, stream)) return st;
+        rank = LowRank{low, ad.B, out * ad.rank, ad.rank, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
+    }
     if (p.few) {
-        float *partial = reinterpret_cast<float *>(ws), *low = reinterpret_cast<float *>(ws + p.partial);
-        FewArgs a{scale_codes, packed_e2m1, out, in, static_cast<const uint16_t *>(X), tokens, ldx, p.base.k_split,
-                  (int)cdiv(out, kFewRows), p.base.splits, partial, 0, {}};
-        if (ad.count) {
-            a.low = FewLowArgs{a.X, tokens, ldx, in, ad.A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, low,
+        FewArgs a{};
+        a.codes = scale_codes;
+        a.packed = packed_e2m1;
+        a.out = out, a.in = in;
+        a.X = static_cast<const uint16_t *>(X);
+        a.tokens = tokens, a.ldx = ldx;
+        a.k_split = p.base.k_split;
+        a.row_blocks = (int)cdiv(out, kFewRows);
+        a.splits = p.base.splits;
+        a.e = e, a.f = f;
+        a.partial = p.partial ? sum : nullptr;
+        a.Y = y, a.ldy = ldy, a.wide = aligned(Y, 8) && (tokens == 1 || ldy % 4 == 0);
+        a.rank = rank;
+        if (ad.count && p.base.fused) {
+            a.low = FewLowArgs{a.X, tokens, ldx, in, ad.A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, low_sum,
                                p.base.low_splits, p.base.low_slots};
             a.low_blocks = (int)cdiv(tokens, 32) * (rank_pad(ad.rank) / 32) * p.base.low_splits * p.base.low_slots;
         }
-        const int nt = (int)std::min<int64_t>(cdiv(tokens, 16), 4);
+        const int nt = p.base.tile;
         const dim3 grid((unsigned)(a.low_blocks + (int64_t)a.row_blocks * a.splits * cdiv(tokens, 16 * nt)));
         const bool even = in % 32 == 0 && aligned(scale_codes, 2);
 #define FEW(n)                                                                              \
@@ -1294,28 +1431,22 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
             FEW(2);
         } else if (nt == 3) {
             FEW(3);
-        } else {
+        } else if (nt == 4) {
             FEW(4);
+        } else {
+            FEW(8);
         }
 #undef FEW
         if (const int st = launch_status()) return st;
-        const FewFinishArgs f{partial, p.base.splits, tokens, out, global_scale, ad.count ? low : nullptr,
-                              p.base.low_splits, ad.rank, rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
-        hipLaunchKernelGGL(few_finish, dim3((unsigned)cdiv(out, 256), (unsigned)tokens), dim3(256), 0, stream, f);
+        if (!p.base.fused) return p.partial ? sum_of_splits(sum, p.base.splits, tokens, out, f, y, ldy, stream) : HSCALE_OK;
+        const FewFinishArgs last{sum, p.base.splits, tokens, out, f, ad.count ? low_sum : nullptr, p.base.low_splits,
+                              ad.rank, rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
+        hipLaunchKernelGGL(few_finish, dim3((unsigned)cdiv(out, 256), (unsigned)tokens), dim3(256), 0, stream, last);
         return launch_status();
     }
-    void *W = ws;
-    float f, two_e;
-    split_scale(global_scale, f, two_e);
-    float *sum = reinterpret_cast<float *>(ws += p.weights);
-    float *partial = reinterpret_cast<float *>(ws += p.partial);
-    uint16_t *low = reinterpret_cast<uint16_t *>(ws + p.low_partial);
-    if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, two_e, W, stream)) return st;
+    if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, e, W, stream)) return st;
     LayerArgs a{};
-    if (ad.count) {
-        if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.low, f, partial, low, stream)) return st;
-        a.low = LowRank{low, ad.B, out * ad.rank, ad.rank, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
-    }
+    a.low = rank;
     a.W = Operand{W, in, out, in};
     a.X = Operand{X, ldx, tokens, in};
     a.scale = f;
@@ -1367,8 +1498,9 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
 
     char *ws = static_cast<char *>(workspace);
     void *W = ws;
-    float f, two_e;
-    split_scale(global_scale, f, two_e);
+    float f;
+    int e;
+    split_scale(global_scale, f, e);
     uint16_t *wide_dy = reinterpret_cast<uint16_t *>(ws += p.weights);
     uint16_t *turned = reinterpret_cast<uint16_t *>(ws += p.dy);
     float *partial = reinterpret_cast<float *>(ws += p.turned);
@@ -1390,7 +1522,7 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
         if (const int st = shrink_to_low(dy, tokens, p.width, turned, ad, p.v, f, partial, v, stream)) return st;
         if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.u, 1.0f, partial, u, stream)) return st;
         if (dX) {
-            if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, two_e, W, stream)) return st;
+            if (const int st = stored_weights(scale_codes, packed_e2m1, out, in, e, W, stream)) return st;
             LayerArgs a{};
             a.W = Operand{W, in, in, out};
             a.X = Operand{dy.p, dy.ld, tokens, p.width};

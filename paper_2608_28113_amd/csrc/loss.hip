@@ -237,9 +237,9 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The tile of least estimated time for an m x n product over k.
-inline bool large_tiles(int64_t m, int64_t n, int64_t k) { return large_us(m, n, k) <= small_us(m, n, k, 1); }
-inline int64_t tile_side(int64_t m, int64_t n, int64_t k) { return large_tiles(m, n, k) ? 256 : 128; }
+// The tile of least estimated time for an m x n product over k that is not split.
+inline bool large_tiles(int64_t m, int64_t n, int64_t k) { return split_plan(m, n, k, false).large; }
+inline int64_t tile_side(int64_t m, int64_t n, int64_t k) { return split_plan(m, n, k, false).side(); }
 
 struct LossPlan {
     size_t parts, at, total;
@@ -271,7 +271,7 @@ LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    const Split x = split_plan(d, tokens, p.piece);
+    const Split x = split_plan(d, tokens, p.piece, true);
     p.large_dx = x.large;
     p.k_split = x.k;
     p.splits = x.splits;

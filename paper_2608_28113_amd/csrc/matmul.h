@@ -139,7 +139,7 @@ struct Stage {
     // into reads of nothing (a row's next values are not read).  Stages past
     // the last are all nothing: zeros, and no memory traffic.
     __device__ __forceinline__ u32x4 begin() {
-        if (L == Along && k_left < kK) {
+        if (L == Along && __builtin_amdgcn_readfirstlane(k_left < kK)) {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i)
                 if (chunk * 8 >= k_left) off[i] = kNoRead;
@@ -204,38 +204,45 @@ struct Tile {
 };
 
 typedef Tile<2, 2, 4, 4, 64, 2, 2> Large;        // 256 x 256
-typedef Tile<2, 4, 4, 2, 32, 4, 2> LargeAcross;  // the same, for two operands across
 typedef Tile<2, 2, 2, 2, 64, 4, 2> Small;        // 128 x 128, for fewer blocks than CUs: its ring hides latency
+typedef Tile<2, 4, 4, 2, 32, 4, 2> LargeAcross;  // 256 x 256 for two operands across, in eight waves: four run out of registers
+constexpr int kCUs = 256;
 
-// Estimated time in us of a product in 256 x 256 or in 128 x 128 tiles and
-// `splits` of k, whose partial sums are written and read again: rounds of 256
-// blocks, each with its stages and a start and an end.
-inline double large_us(int64_t m, int64_t n, int64_t k) {
-    const int64_t rounds = ((m + 255) / 256 * ((n + 255) / 256) + 255) / 256;
-    return rounds * ((k + 63) / 64 * 1.02 + 8.0);
-}
-inline double small_us(int64_t m, int64_t n, int64_t k, int64_t splits) {
-    const int64_t rounds = ((m + 127) / 128 * ((n + 127) / 128) * splits + 255) / 256;
-    const double sums = splits > 1 ? 4.0 + splits * m * n * 8 / 5.0e6 : 0.0;
-    return rounds * (((k + 63) / 64 + splits - 1) / splits * 0.27 + 4.0) + sums;
-}
-
+// A product in 256 x 256 or 128 x 128 tiles and splits of k, whose partial
+// sums are written and read again.
 struct Split {
     bool large;
     int64_t k;   // of a split, a multiple of 64
     int splits;
+    int64_t side() const { return large ? 256 : 128; }
 };
 
-// The tile, and for the small one the splits of at least 256 k, of the least
-// estimated time.
-inline Split split_plan(int64_t m, int64_t n, int64_t k) {
-    int64_t best = 1;
-    for (int64_t s = 2; s <= 32 && (k + s - 1) / s >= 256; ++s)
-        if (small_us(m, n, k, s) < small_us(m, n, k, best)) best = s;
-    Split p;
-    p.large = large_us(m, n, k) <= small_us(m, n, k, best);
-    const int64_t each = p.large ? k : (k + best - 1) / best;
-    p.k = (each + 63) / 64 * 64;
+// Estimated time of it in us: rounds of up to 256 blocks; a stage of 64 k takes
+// what its matrix instructions do, or what its 64 or 32 KB per block take out
+// of the L2s at 15 TB/s in all; a round starts and ends; sums at 5 TB/s.
+// Measured at 8192^3 and 2048 x 4096 x 4096: 1.0 and 0.6 us a stage.
+inline double split_us(int64_t m, int64_t n, int64_t k, bool large, int64_t splits) {
+    const int64_t side = large ? 256 : 128, units = (m + side - 1) / side * ((n + side - 1) / side) * splits;
+    const int64_t rounds = (units + kCUs - 1) / kCUs, blocks = units < kCUs ? units : kCUs;
+    const double work = large ? 0.9 : 0.27, bytes = side * 256.0 * blocks / 15.0e6;
+    const double stages = (double)(((k + 63) / 64 + splits - 1) / splits);
+    return rounds * (stages * (work > bytes ? work : bytes) + 3.0) + 3.0 +
+           (splits > 1 ? 3.0 + splits * m * n * 8 / 5.0e6 : 0.0);
+}
+
+// The tile and, if it may, the splits of at least 256 k of the least estimated time.
+inline Split split_plan(int64_t m, int64_t n, int64_t k, bool may_split) {
+    Split p{true, k, 1};
+    double best = split_us(m, n, k, true, 1);
+    for (int large = 0; large < 2; ++large)
+        for (int64_t s = 1; s == 1 || (may_split && s <= 32 && (k + s - 1) / s >= 256); ++s) {
+            const double us = split_us(m, n, k, large, s);
+            if (us < best) {
+                best = us;
+                p = Split{large != 0, (k + s - 1) / s, (int)s};
+            }
+        }
+    p.k = (p.k + 63) / 64 * 64;
     p.splits = (int)((k + p.k - 1) / p.k);
     return p;
 }
@@ -364,7 +371,6 @@ __device__ __forceinline__ void tile_product(Acc<T> &acc, uint8_t *lds, const Op
             const bool last = kk == kSteps - 1;
             if (last) {
                 wait_copies_and_barrier<(R - 2) * kCopies>();
-                begin();
             }
             // after the last stage: old values that nothing uses
             const uint8_t *from = lds + (last ? next : cur) * kStageBytes;
@@ -375,9 +381,10 @@ __device__ __forceinline__ void tile_product(Acc<T> &acc, uint8_t *lds, const Op
                 const int i = q % T::kMI, j = q / T::kMI;
                 acc.v[i][j] =
                     __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[kk & 1][i], fq[kk & 1][j], acc.v[i][j], 0, 0, 0);
+                if (last && q == 0) begin();  // behind an MFMA, not before it
 #pragma unroll
                 for (int u = 0; u < kUnits; ++u)
-                    if (u * kMfmas / kUnits == q) read_unit(from, last ? 0 : kk + 1, u);
+                    if (u * kMfmas / (2 * kUnits) == q) read_unit(from, last ? 0 : kk + 1, u);
 #pragma unroll
                 for (int c = 0; c < kCopies; ++c)
                     if (c >= c0 && c < c1 && (2 * (c - c0) + 1) * kMfmas / (2 * (c1 - c0)) == q)
