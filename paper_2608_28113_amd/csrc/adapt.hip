@@ -348,28 +348,28 @@ __device__ __forceinline__ float sum_splits(const float *__restrict__ p, int spl
 }
 
 // alpha / f times the sum of the splits (f multiplies the result that takes it),
-// or alpha times it, as two bf16 parts: low[t, j] and
-// low[t, rank_pad + j].  Tokens without an adapter are left as they are; what
+// or alpha times it, as two bf16 parts: low[t, j] and low[t, pad + j].  Tokens without an adapter are left as they are; what
 // reads `low` skips them.
 __global__ __launch_bounds__(256) void shrink_finish(const float *__restrict__ partial, int splits, int64_t tokens,
-                                                     int rank, int rank_pad, const float *__restrict__ alpha, float f,
+                                                     int rank, int rank_pad, int pad, const float *__restrict__ alpha,
+                                                     float f,
                                                      const int32_t *__restrict__ ids, int count,
                                                      uint16_t *__restrict__ low) {
-    const int64_t total = tokens * rank_pad, stride = (int64_t)gridDim.x * 256;
+    const int64_t total = tokens * pad, stride = (int64_t)gridDim.x * 256;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
-        const int64_t t = id / rank_pad;
-        const int j = (int)(id - t * rank_pad);
+        const int64_t t = id / pad;
+        const int j = (int)(id - t * pad);
         const int a = adapter_of(ids, count, t);
         if (a == kNoAdapter) continue;
         float v = 0.0f;
         if (j < rank) {
-            v = sum_splits(partial + id, splits, total);
+            v = sum_splits(partial + t * rank_pad + j, splits, tokens * rank_pad);
             if (alpha) v *= alpha[a];
             v /= f;
         }
         const uint32_t hi = bf16_rne(v);
-        low[t * 2 * rank_pad + j] = (uint16_t)hi;
-        low[t * 2 * rank_pad + rank_pad + j] = (uint16_t)bf16_rne(v - bf16_value(hi));
+        low[t * 2 * pad + j] = (uint16_t)hi;
+        low[t * 2 * pad + pad + j] = (uint16_t)bf16_rne(v - bf16_value(hi));
     }
 }
 
@@ -378,11 +378,11 @@ __global__ __launch_bounds__(256) void shrink_finish(const float *__restrict__ p
 // ---------------------------------------------------------------------------
 
 struct LowRank {
-    const uint16_t *low;    // [tokens, 2 rank_pad]: two bf16 parts
+    const uint16_t *low;    // [tokens, 2 pad]: two bf16 parts
     const uint16_t *other;  // forward: B [count, out, rank]; backward: A [count, rank, in]
     int64_t other_size;     // elements of one adapter
     int64_t ld;
-    int count, rank, rank_pad;
+    int count, rank, pad;
     const int32_t *ids;
 };
 
@@ -420,11 +420,11 @@ struct LowRankStages {
         while (adapters.next() != kNoAdapter) stages += per_adapter();
         adapters.restart();
     }
-    __device__ __forceinline__ int per_adapter() const { return (2 * w.rank_pad + T::kK - 1) / T::kK; }
+    __device__ __forceinline__ int per_adapter() const { return (2 * w.pad + T::kK - 1) / T::kK; }
     // Column of the adapter's rank that k of its stages stands for, or none.
     __device__ __forceinline__ int column(int k) const {
-        const int j = k >= w.rank_pad ? k - w.rank_pad : k;
-        return k < 2 * w.rank_pad && j < w.rank ? j : -1;
+        const int j = k >= w.pad ? k - w.pad : k;
+        return k < 2 * w.pad && j < w.rank ? j : -1;
     }
     __device__ __forceinline__ void set(SP &sp, SQ &sq, bool some) {
         if (!some) {  // stages past the last
@@ -432,7 +432,7 @@ struct LowRankStages {
             return;
         }
         if (step == 0) adapter = adapters.next();
-        const int k0 = step * T::kK, deep = 2 * w.rank_pad;
+        const int k0 = step * T::kK, deep = 2 * w.pad;
         step = step + 1 == per_adapter() ? 0 : step + 1;
         const uint16_t *P = w.other + (int64_t)adapter * w.other_size + (LP == Along ? m0 * w.ld : m0);
         sp.base = reinterpret_cast<const char *>(P);
@@ -495,10 +495,15 @@ __global__ __launch_bounds__(256) void layer_finish(const float *__restrict__ su
     const float *src = sum + t * m + c;
     uint16_t *dst = Y + t * ldy + c;
     if (m % 4 == 0) {
-        float4 v = *reinterpret_cast<const float4 *>(src);
-        for (int s = 1; s < splits; ++s) {
-            const float4 o = *reinterpret_cast<const float4 *>(src + s * plane);
-            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int s = 0; s < splits; s += 4) {  // 4 loads under way
+            float4 o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                o[k] = s + k < splits ? *reinterpret_cast<const float4 *>(src + (s + k) * plane)
+                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v.x += o[k].x, v.y += o[k].y, v.z += o[k].z, v.w += o[k].w;
         }
         const uint32_t lo = bf16_pair(v.x * scale, v.y * scale), hi = bf16_pair(v.z * scale, v.w * scale);
         if ((reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
@@ -743,8 +748,9 @@ __global__ __launch_bounds__(512, kNT <= 4 ? 4 : 2) void few_kernel(const FewArg
     wait_and_barrier();
 
     // The adapters' part, once: for each adapter that the tokens have, its rows
-    // of B against both parts of low; tokens of others enter as zeros.
-    if (a.rank.low && split == 0 && half == 0) {
+    // of B against both parts of low; tokens of others enter as zeros.  The
+    // halves take every other adapter.
+    if (a.rank.low && split == 0) {
         const LowRank &w = a.rank;
         int own[kNT];
 #pragma unroll
@@ -752,10 +758,12 @@ __global__ __launch_bounds__(512, kNT <= 4 ? 4 : 2) void few_kernel(const FewArg
             own[n] = n * 16 + l16 < toks ? adapter_of(w.ids, w.count, t0 + n * 16 + l16) : kNoAdapter;
         Distinct<(kNT + 3) / 4> adapters;
         adapters.read(w.ids, w.count, t0, t0 + toks);
+        int nth = 0;
         for (int adapter = adapters.next(); adapter != kNoAdapter; adapter = adapters.next()) {
+            if ((nth++ & 1) != half) continue;
             const uint16_t *B = w.other + adapter * w.other_size + (r0 + row) * w.rank;
-            for (int k = g * 8; k < 2 * w.rank_pad; k += 32) {
-                const int j = k >= w.rank_pad ? k - w.rank_pad : k;
+            for (int k = g * 8; k < 2 * w.pad; k += 32) {
+                const int j = k >= w.pad ? k - w.pad : k;
                 u32x4 fw[kNF], fx[kNT];
 #pragma unroll
                 for (int f = 0; f < kNF; ++f) {
@@ -767,7 +775,7 @@ __global__ __launch_bounds__(512, kNT <= 4 ? 4 : 2) void few_kernel(const FewArg
                 for (int n = 0; n < kNT; ++n) {
                     fx[n] = u32x4{0, 0, 0, 0};
                     if (own[n] == adapter)
-                        fx[n] = *reinterpret_cast<const u32x4 *>(w.low + (t0 + n * 16 + l16) * 2 * w.rank_pad + k);
+                        fx[n] = *reinterpret_cast<const u32x4 *>(w.low + (t0 + n * 16 + l16) * 2 * w.pad + k);
                 }
 #pragma unroll
                 for (int f = 0; f < kNF; ++f)
@@ -870,8 +878,8 @@ __global__ __launch_bounds__(256) void few_finish(const FewFinishArgs a) {
 struct OuterArgs {
     Rows z;
     int64_t tokens, width;
-    const uint16_t *low;  // [tokens, 2 rank_pad]
-    int count, rank, rank_pad;
+    const uint16_t *low;  // [tokens, 2 pad]
+    int count, rank, pad;
     const int32_t *ids;
     int64_t t_split;      // of a split, a multiple of 64
     float *partial;       // [splits, count, rank, width]
@@ -896,13 +904,13 @@ __global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs
     __shared__ uint64_t masks[kOuterMasks];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     const int c0 = (int)blockIdx.x * kOuterCols, width = (int)a.width;
-    const int groups = (a.rank_pad / 32 + kRT - 1) / kRT;
+    const int groups = (a.rank + 32 * kRT - 1) / (32 * kRT);
     const int j0 = (int)(blockIdx.y % groups) * 32 * kRT, adapter = blockIdx.y / groups;
     const int64_t t0 = (int64_t)blockIdx.z * a.t_split;
     const int64_t t1 = t0 + a.t_split < a.tokens ? t0 + a.t_split : a.tokens;
     const int blocks = (width + kCkBlock - 1) / kCkBlock;
     const int64_t zrow = kCheckpoint ? a.width : a.z.ld * 2;  // bytes
-    const int lrow = a.rank_pad * 4;
+    const int lrow = a.pad * 4;
 
     u32x4 z[kZ], l[kRT];
     float scale[kZ];
@@ -926,7 +934,7 @@ __global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs
             const_cast<char *>(reinterpret_cast<const char *>(a.z.p)) + s * zrow, 0,
             (int)((rows - 1) * zrow + (kCheckpoint ? a.width : a.width * 2)), kRawWord3);
         const __amdgpu_buffer_rsrc_t rl = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t *>(a.low) + s * 2 * a.rank_pad, 0, (int)(rows * lrow), kRawWord3);
+            const_cast<uint16_t *>(a.low) + s * 2 * a.pad, 0, (int)(rows * lrow), kRawWord3);
 #pragma unroll
         for (int i = 0; i < kZ; ++i) {
             const int row = z_row(i), c = c0 + zc;
@@ -938,9 +946,9 @@ __global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs
 #pragma unroll
         for (int r = 0; r < kRT; ++r) {
             const int j = j0 + r * 32 + (tid & 3) * 8;
-            const bool some = (mask >> l_row & 1) && j < a.rank_pad;
+            const bool some = (mask >> l_row & 1) && j < a.pad;
             l[r] = __builtin_amdgcn_raw_buffer_load_b128(
-                rl, some ? (uint32_t)(l_row * lrow + (part * a.rank_pad + j) * 2) : kNoRead, 0, 0);
+                rl, some ? (uint32_t)(l_row * lrow + (part * a.pad + j) * 2) : kNoRead, 0, 0);
         }
         return g;
     };
@@ -1074,10 +1082,11 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 
 
 constexpr int kTargetBlocks = 1024;
-constexpr int64_t kFewTokens = 1024, kFewFused = 128;
+constexpr int64_t kFewTokens = 1024, kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
+inline int low_pad(int rank) { return (rank + 15) / 16 * 16; }
 
 struct Low {
     int64_t k_split;
@@ -1104,7 +1113,7 @@ inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
     return round_up((size_t)p.splits * tokens * rank_pad(rank) * 4, 256);
 }
 
-inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * rank_pad(rank) * 2, 256); }
+inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * low_pad(rank) * 2, 256); }
 
 struct Adapters {
     int count, rank;
@@ -1136,8 +1145,8 @@ int shrink(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, cons
 int shrink_to_low(const Rows &z, int64_t tokens, int64_t width, const uint16_t *A, const Adapters &ad, const Low &p,
                   float f, float *partial, uint16_t *low, hipStream_t stream) {
     if (const int st = shrink(z, tokens, width, A, ad, p, partial, stream)) return st;
-    hipLaunchKernelGGL(shrink_finish, dim3(grid_for(tokens * rank_pad(ad.rank), 256)), dim3(256), 0, stream, partial,
-                       p.splits, tokens, ad.rank, rank_pad(ad.rank), ad.alpha, f, ad.ids, ad.count, low);
+    hipLaunchKernelGGL(shrink_finish, dim3(grid_for(tokens * low_pad(ad.rank), 256)), dim3(256), 0, stream, partial,
+                       p.splits, tokens, ad.rank, rank_pad(ad.rank), low_pad(ad.rank), ad.alpha, f, ad.ids, ad.count, low);
     return launch_status();
 }
 
@@ -1179,16 +1188,26 @@ struct FewPlan {
     int tile;    // tokens a block, in sixteens
 };
 
-// Splits of k as far as they fill the chip once; every one costs its partial
-// sums once more.
-inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count) {
+// The splits of k of the least estimated time in us: rounds of one or two
+// blocks a CU, 256 k of a block in 1.2 to 2.4 us by its tokens (128 tokens
+// 2.3, measured at 512 tokens, 4096 -> 14336), partial sums at 5 TB/s.
+inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
     FewPlan p;
     p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
-    p.fused = tokens <= kFewFused;
-    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), room = p.tile > 4 ? kCUs : 2 * kCUs;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(room / blocks, cdiv(in, kFewK)));
-    p.k_split = cdiv(cdiv(in, want), kFewK) * kFewK;
-    p.splits = (int)cdiv(in, p.k_split);
+    p.fused = tokens <= kFewTile ||
+              (count > 0 && tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork);
+    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
+    double least = 0.0;
+    for (int64_t s = 1; s <= 32 && s <= cdiv(in, kFewK); ++s) {
+        const int64_t k = cdiv(cdiv(in, s), kFewK) * kFewK, n = cdiv(in, k);
+        const double each = p.tile > 4 ? 2.3 : 0.9 + 0.35 * p.tile;
+        const double us = cdiv(blocks * n, slots) * (k / 256 * each + 2.0) +
+                          (n > 1 || p.fused ? 3.0 + n * tokens * out * 8 / 5.0e6 : 0.0);
+        if (s > 1 && us >= least) continue;
+        least = us;
+        p.k_split = k;
+        p.splits = (int)n;
+    }
     p.low_splits = (int)cdiv(in, kFewLowK);
     p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
     return p;
@@ -1215,7 +1234,7 @@ LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int r
     LinearPlan p{};
     p.few = tokens <= kFewTokens;
     if (p.few) {
-        p.base = few_plan(tokens, in, out, count);
+        p.base = few_plan(tokens, in, out, count, rank);
         if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
     } else {
         p.weights = round_up((size_t)out * in * 2, 256);
@@ -1396,7 +1415,7 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     LowRank rank{};
     if (p.low_parts) {
         if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.low, f, low_sum, low, stream)) return st;
-        rank = LowRank{low, ad.B, out * ad.rank, ad.rank, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
+        rank = LowRank{low, ad.B, out * ad.rank, ad.rank, ad.count, ad.rank, low_pad(ad.rank), ad.ids};
     }
     if (p.few) {
         FewArgs a{};
@@ -1527,7 +1546,7 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
             a.W = Operand{W, in, in, out};
             a.X = Operand{dy.p, dy.ld, tokens, p.width};
             a.scale = f;
-            a.low = LowRank{v, ad.A, in * ad.rank, in, ad.count, ad.rank, rank_pad(ad.rank), ad.ids};
+            a.low = LowRank{v, ad.A, in * ad.rank, in, ad.count, ad.rank, low_pad(ad.rank), ad.ids};
             a.Y = static_cast<uint16_t *>(dX);
             a.ldy = lddx;
             a.wide = aligned(dX, 16) && (tokens == 1 || lddx % 8 == 0);
@@ -1537,7 +1556,7 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
     auto outer_of = [&](const Rows &z, int64_t width, int64_t columns, const uint16_t *low, int64_t split, int splits,
                         float by, void *G, bool transposed) {
         if (tokens > 0) {
-            const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, split, outer};
+            const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, low_pad(ad.rank), ad.ids, split, outer};
             const dim3 grid((unsigned)cdiv(width, kOuterCols),
                             (unsigned)(cdiv(ad.rank, rank_tile(ad.rank)) * ad.count), (unsigned)splits);
             if (z.scale && ad.rank <= 32)
