@@ -1167,16 +1167,14 @@ int sum_of_splits(const float *sum, int splits, int64_t tokens, int64_t m, float
 
 template <Layout LW>
 int layer(LayerArgs a, const Split &p, float *sum, hipStream_t stream) {
-    const int64_t m = a.W.rows, n = a.X.rows, side = p.side();
-    a.mtiles = (unsigned)cdiv(m, side);
-    a.tiles = (unsigned)(a.mtiles * cdiv(n, side));
+    const int64_t m = a.W.rows, n = a.X.rows;
+    a.mtiles = (unsigned)cdiv(m, p.side_m());
+    a.tiles = (unsigned)p.units(m, n);
     a.k_split = p.k;
     a.sum = p.splits > 1 ? sum : nullptr;
-    const dim3 grid(a.tiles * (unsigned)p.splits);
-    if (p.large)
-        hipLaunchKernelGGL((layer_kernel<Large, LW>), grid, dim3(Large::kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((layer_kernel<Small, LW>), grid, dim3(Small::kThreads), 0, stream, a);
+#define LAYER(T) layer_kernel<T, LW>
+    LAUNCH_TILES(LAYER, Large, p.size, a.tiles * (unsigned)p.splits, stream, a);
+#undef LAYER
     if (const int st = launch_status()) return st;
     return p.splits > 1 ? sum_of_splits(sum, p.splits, n, m, a.scale, a.Y, a.ldy, stream) : HSCALE_OK;
 }

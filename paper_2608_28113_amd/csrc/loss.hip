@@ -237,17 +237,20 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The tile of least estimated time for an m x n product over k that is not split.
-inline bool large_tiles(int64_t m, int64_t n, int64_t k) { return split_plan(m, n, k, false).large; }
-inline int64_t tile_side(int64_t m, int64_t n, int64_t k) { return split_plan(m, n, k, false).side(); }
+#define loss_tile_kernel_of(T) loss_tile_kernel<T>
+#define loss_slope_kernel_of(T) loss_slope_kernel<T>
+#define loss_dx_kernel_of(T) loss_dx_kernel<T>
+#define loss_dw_kernel_of(T) loss_dw_kernel<T>
 
 struct LossPlan {
+    Split tile;
     size_t parts, at, total;
 };
 
 LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     LossPlan p;
-    p.parts = round_up((size_t)cdiv(vocab, tile_side(vocab, tokens, d)) * tokens * sizeof(float2), 256);
+    p.tile = split_plan(vocab, tokens, d, false);
+    p.parts = round_up((size_t)cdiv(vocab, p.tile.side_m()) * tokens * sizeof(float2), 256);
     p.at = round_up((size_t)tokens * 4, 256);
     p.total = p.parts + p.at;
     return p;
@@ -259,9 +262,8 @@ constexpr int64_t kLeastPiece = 2048;
 constexpr int64_t kPieceStep = 256;
 
 struct LossGradPlan {
-    int64_t piece, pieces, k_split;
-    int splits;
-    bool large_dx;
+    int64_t piece, pieces;
+    Split dx;
     size_t g, sum, rows, total;
 };
 
@@ -271,12 +273,9 @@ LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    const Split x = split_plan(d, tokens, p.piece, true);
-    p.large_dx = x.large;
-    p.k_split = x.k;
-    p.splits = x.splits;
+    p.dx = split_plan(d, tokens, p.piece, true);
     p.g = round_up((size_t)tokens * p.piece * 2, 256);
-    p.sum = round_up((size_t)p.splits * tokens * d * 4, 256);
+    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
     p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
     p.total = p.g + p.sum + p.rows;
     return p;
@@ -333,12 +332,8 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
     a.parts = static_cast<float2 *>(workspace);
     a.at = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.parts);
     a.vocab = vocab;
-    a.mtiles = (unsigned)cdiv(vocab, tile_side(vocab, tokens, d));
-    const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_side(vocab, tokens, d))));
-    if (large_tiles(vocab, tokens, d))
-        hipLaunchKernelGGL((loss_tile_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((loss_tile_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
+    a.mtiles = (unsigned)cdiv(vocab, p.tile.side_m());
+    LAUNCH_TILES(loss_tile_kernel_of, Large, p.tile.size, p.tile.units(vocab, tokens), stream, a);
     if (const int st = launch_status()) return st;
     hipLaunchKernelGGL(loss_finish, dim3((unsigned)cdiv(tokens, 64)), dim3(256), 0, stream, a.parts,
                        (int64_t)a.mtiles, tokens, target, vocab, a.at, loss, lse);
@@ -399,50 +394,39 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         a.weight = weight;
         a.g = g;
         a.ldg = ldg;
-        a.mtiles = (unsigned)(ldg / tile_side(cols, tokens, d));
-        const dim3 grid((unsigned)(a.mtiles * cdiv(tokens, tile_side(cols, tokens, d))));
-        if (large_tiles(cols, tokens, d))
-            hipLaunchKernelGGL((loss_slope_kernel<Large>), grid, dim3(Large::kThreads), 0, stream, a);
-        else
-            hipLaunchKernelGGL((loss_slope_kernel<Small>), grid, dim3(Small::kThreads), 0, stream, a);
+        const Split logits = split_plan(ldg, tokens, d, false);
+        a.mtiles = (unsigned)(ldg / logits.side_m());
+        LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
         if (const int st = launch_status()) return st;
         if (dX) {
             DxArgs x{};
             x.W = Operand{Wp, d, d, cols};
             x.g = Operand{g, ldg, tokens, ldg};
-            const int64_t side = p.large_dx ? Large::kBM : Small::kBM;
-            x.mtiles = (unsigned)cdiv(d, side);
-            x.tiles = (unsigned)(x.mtiles * cdiv(tokens, side));
-            x.k_split = p.k_split;
+            x.mtiles = (unsigned)cdiv(d, p.dx.side_m());
+            x.tiles = (unsigned)p.dx.units(d, tokens);
+            x.k_split = p.dx.k;
             x.add = v0 > 0;
             x.sum = sum;
-            const dim3 blocks(x.tiles * (unsigned)p.splits);
-            if (p.large_dx)
-                hipLaunchKernelGGL((loss_dx_kernel<Large>), blocks, dim3(Large::kThreads), 0, stream, x);
-            else
-                hipLaunchKernelGGL((loss_dx_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, x);
+            LAUNCH_TILES(loss_dx_kernel_of, Large, p.dx.size, x.tiles * (unsigned)p.dx.splits, stream, x);
             if (const int st = launch_status()) return st;
         }
         if (dW) {
             DwArgs b{};
             b.X = Operand{rows, d, d, tokens};
             b.g = Operand{g, ldg, ldg, tokens};
-            b.mtiles = (unsigned)cdiv(d, tile_side(d, cols, tokens));
+            const Split rows_of = split_plan(d, cols, tokens, false);
+            b.mtiles = (unsigned)cdiv(d, rows_of.side_m());
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;
             b.wide = aligned(dW, 16);
-            const dim3 blocks((unsigned)(b.mtiles * cdiv(cols, tile_side(d, cols, tokens))));
-            if (large_tiles(d, cols, tokens))
-                hipLaunchKernelGGL((loss_dw_kernel<LargeAcross>), blocks, dim3(LargeAcross::kThreads), 0, stream, b);
-            else
-                hipLaunchKernelGGL((loss_dw_kernel<Small>), blocks, dim3(Small::kThreads), 0, stream, b);
+            LAUNCH_TILES(loss_dw_kernel_of, LargeAcross, rows_of.size, rows_of.units(d, cols), stream, b);
             if (const int st = launch_status()) return st;
         }
     }
     if (dX) {
         const int64_t fours = tokens * d / 4;
         hipLaunchKernelGGL(loss_dx_finish, dim3(grid_for(fours, 256)), dim3(256), 0, stream,
-                           reinterpret_cast<const float4 *>(sum), p.splits, fours, d, static_cast<uint16_t *>(dX),
+                           reinterpret_cast<const float4 *>(sum), p.dx.splits, fours, d, static_cast<uint16_t *>(dX),
                            lddx);
         return launch_status();
     }
