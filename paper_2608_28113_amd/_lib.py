@@ -260,64 +260,63 @@ def hscale_output_error(X: int, tokens: int, in_: int, W: int, out: int, global_
                                       stream or None)
 
 
+# The entry points of a stored layer in use.  They are called once a layer and
+# token, where microseconds count: pointers go as they are (c_void_p takes 0 for
+# NULL).
+
+
 def _adapters(adapters):
     """A pointer to struct hscale_adapters of (count, rank, A, B, alpha, adapter), or NULL for None."""
-    if adapters is None:
-        return None
-    count, rank, *ptrs = adapters
-    return ctypes.byref(HScaleAdapters(count, rank, *(p or None for p in ptrs)))
+    return None if adapters is None else ctypes.byref(HScaleAdapters(*adapters))
 
 
 def hscale_adapted_linear_workspace_bytes(tokens: int, in_: int, out: int, count: int, rank: int) -> int:
-    return int(load().hscale_adapted_linear_workspace_bytes(tokens, in_, out, count, rank))
+    return (_lib or load()).hscale_adapted_linear_workspace_bytes(tokens, in_, out, count, rank)
 
 
 def hscale_adapted_linear(X: int, tokens: int, in_: int, ldx: int, out: int, global_scale: float, scale_codes: int,
                           packed_e2m1: int, adapters, Y: int, ldy: int, workspace: int, workspace_bytes: int,
                           stream: int) -> int:
-    return load().hscale_adapted_linear(X or None, tokens, in_, ldx, out, global_scale, scale_codes or None,
-                                        packed_e2m1 or None, _adapters(adapters), Y or None, ldy, workspace or None,
-                                        workspace_bytes, stream or None)
+    return (_lib or load()).hscale_adapted_linear(X, tokens, in_, ldx, out, global_scale, scale_codes, packed_e2m1,
+                                                  _adapters(adapters), Y, ldy, workspace, workspace_bytes, stream)
 
 
 def hscale_pack_activations(X: int, tokens: int, in_: int, ldx: int, q: int, scale: int, stream: int) -> int:
-    return load().hscale_pack_activations(X or None, tokens, in_, ldx, q or None, scale or None, stream or None)
+    return (_lib or load()).hscale_pack_activations(X, tokens, in_, ldx, q, scale, stream)
 
 
 def hscale_unpack_activations(q: int, scale: int, tokens: int, in_: int, X: int, ldx: int, stream: int) -> int:
-    return load().hscale_unpack_activations(q or None, scale or None, tokens, in_, X or None, ldx, stream or None)
+    return (_lib or load()).hscale_unpack_activations(q, scale, tokens, in_, X, ldx, stream)
 
 
 def hscale_adapted_linear_grad_workspace_bytes(tokens: int, in_: int, out: int, count: int, rank: int) -> int:
-    return int(load().hscale_adapted_linear_grad_workspace_bytes(tokens, in_, out, count, rank))
+    return (_lib or load()).hscale_adapted_linear_grad_workspace_bytes(tokens, in_, out, count, rank)
 
 
 def hscale_adapted_linear_grad(dY: int, tokens: int, out: int, lddy: int, q: int, scale: int, in_: int,
                                global_scale: float, scale_codes: int, packed_e2m1: int, adapters, dX: int, lddx: int,
                                dA: int, dB: int, workspace: int, workspace_bytes: int, stream: int) -> int:
-    return load().hscale_adapted_linear_grad(dY or None, tokens, out, lddy, q or None, scale or None, in_,
-                                             global_scale, scale_codes or None, packed_e2m1 or None,
-                                             _adapters(adapters), dX or None, lddx, dA or None, dB or None,
-                                             workspace or None, workspace_bytes, stream or None)
+    return (_lib or load()).hscale_adapted_linear_grad(dY, tokens, out, lddy, q, scale, in_, global_scale,
+                                                       scale_codes, packed_e2m1, _adapters(adapters), dX, lddx, dA,
+                                                       dB, workspace, workspace_bytes, stream)
 
 
 def hscale_token_loss_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
-    return int(load().hscale_token_loss_workspace_bytes(tokens, d, vocab))
+    return (_lib or load()).hscale_token_loss_workspace_bytes(tokens, d, vocab)
 
 
 def hscale_token_loss(X: int, tokens: int, d: int, ldx: int, W: int, vocab: int, target: int, loss: int, lse: int,
                       workspace: int, workspace_bytes: int, stream: int) -> int:
-    return load().hscale_token_loss(X or None, tokens, d, ldx, W or None, vocab, target or None, loss or None,
-                                    lse or None, workspace or None, workspace_bytes, stream or None)
+    return (_lib or load()).hscale_token_loss(X, tokens, d, ldx, W, vocab, target, loss, lse, workspace,
+                                              workspace_bytes, stream)
 
 
 def hscale_token_loss_grad_workspace_bytes(tokens: int, d: int, vocab: int) -> int:
-    return int(load().hscale_token_loss_grad_workspace_bytes(tokens, d, vocab))
+    return (_lib or load()).hscale_token_loss_grad_workspace_bytes(tokens, d, vocab)
 
 
 def hscale_token_loss_grad(X: int, tokens: int, d: int, ldx: int, W: int, vocab: int, target: int, lse: int,
                            weight: int, dX: int, lddx: int, dW: int, workspace: int, workspace_bytes: int,
                            stream: int) -> int:
-    return load().hscale_token_loss_grad(X or None, tokens, d, ldx, W or None, vocab, target or None, lse or None,
-                                         weight or None, dX or None, lddx, dW or None, workspace or None,
-                                         workspace_bytes, stream or None)
+    return (_lib or load()).hscale_token_loss_grad(X, tokens, d, ldx, W, vocab, target, lse, weight, dX, lddx, dW,
+                                                   workspace, workspace_bytes, stream)

@@ -105,7 +105,14 @@ __global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ pa
     const int64_t t = (int64_t)blockIdx.x * 64 + lane;
     float2 p = make_float2(-INFINITY, 0.0f);
     if (t < tokens)
-        for (int64_t k = w; k < tiles; k += 4) p = join(p, parts[k * tokens + t]);
+        for (int64_t k = w; k < tiles; k += 32) {  // 8 loads under way
+            float2 q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                q[i] = k + 4 * i < tiles ? parts[(k + 4 * i) * tokens + t] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p = join(p, q[i]);
+        }
     red[w][lane] = p;
     __syncthreads();
     if (w != 0 || t >= tokens) return;

@@ -395,9 +395,13 @@ CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
 
 def _rows_in(t, name: str) -> int:
     """t is a 2-D bf16 CUDA view with unit column stride; its row stride."""
-    if not _on_device(t) or t.dtype != torch.bfloat16 or t.dim() != 2:
+    if not _on_device(t) or t.dtype is not torch.bfloat16 or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D bf16 CUDA tensor")
-    return _row_view(t, torch.bfloat16, t.shape, t.device, name)
+    row, col = t.stride()
+    rows, cols = t.shape
+    if col != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return row if rows > 1 else cols
 
 
 def _rows_out(t, name: str, shape, device) -> tuple[torch.Tensor, int]:
