@@ -561,9 +561,10 @@ size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t
  * that hscale_token_loss wrote: with
  *   g[t, v] = weight[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),
  * dX = g W and dW = g^T X.  The logits are computed again, a piece of the
- * vocabulary at a time; g is rounded to bf16 for the two products, whose sums
- * are fp32.  Tokens that are not scored (target or weight 0) get dX = 0 and
- * add nothing to dW, whatever their X and lse hold.
+ * vocabulary at a time; g is rounded for the two products, relative to the
+ * largest weight, to bf16 (to two bf16 parts for up to 64 tokens), and their
+ * sums are fp32.  Tokens that are not scored (target or weight 0) get dX = 0
+ * and add nothing to dW, whatever their X and lse hold.
  *
  * weight     fp32 [tokens]: d(total) / d(loss[t]); 1 / n for a mean over n
  * dX         bf16 [tokens, d], rows lddx apart (8-byte aligned rows); NULL:

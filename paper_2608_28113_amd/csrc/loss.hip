@@ -7,6 +7,17 @@
 // The loss takes one pass of matrix products whose tiles end as a maximum and
 // a sum of exponentials per token; the gradient computes the logits again, a
 // piece of the vocabulary at a time, and only that piece of g is held.
+//
+// g meets the products as bf16.  A weight like 1 / n that is rounded with it
+// errs alike in all tokens' terms, which no sum evens out.  So the largest
+// weight c stays out, and equal weights are exact:
+//
+//   h_tv = weight_t / c (exp(l_tv - lse_t) - [v = target]), rounded,
+//   dX = c (h W),  dW = c (h^T X).
+//
+// For up to 64 tokens h is kept as two bf16 parts: a gradient of few terms is
+// not averaged over many roundings, and twice 64 rows fill no more than the
+// smallest tile.
 
 #include "matmul.h"
 
@@ -31,6 +42,10 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
     return make_float2(m, a.y * exp_of(a.x - m) + b.y * exp_of(b.x - m));
 }
 
+// The two bf16 values of a word.
+__device__ __forceinline__ float low_half(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high_half(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
 struct LogitArgs {
     Operand W, X;            // [vocab, d], [tokens, d]
     const int64_t *target;   // [tokens]
@@ -40,9 +55,11 @@ struct LogitArgs {
     float *at;               // [tokens]: the target's logit
     // gradient: vocabulary from v0 on
     int64_t v0, vocab;       // of the whole
-    const float *lse, *weight;
-    uint16_t *g;             // [tokens, ldg]
+    const float *lse;
+    const float *factor;     // [tokens]: weight_t / c, 0 if not scored
+    uint16_t *g;             // [tokens, ldg]; the second parts follow
     int64_t ldg;
+    bool two;
 };
 
 template <class T>
@@ -124,7 +141,7 @@ __global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ pa
     loss[t] = y >= 0 && y < vocab ? l - at[t] : 0.0f;
 }
 
-// g of a piece of the vocabulary, bf16; zeros where a token is not scored and
+// h of a piece of the vocabulary, bf16; zeros where a token is not scored and
 // beyond the vocabulary.
 template <class T>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(const LogitArgs a) {
@@ -145,7 +162,7 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(
         const bool in = t < a.X.rows;
         const int64_t y = in ? a.target[t] : -1;
         const bool scored = y >= 0 && y < a.vocab;
-        const float w = scored ? a.weight[t] : 0.0f, l = in ? a.lse[t] : 0.0f;
+        const float w = in ? a.factor[t] : 0.0f, l = in ? a.lse[t] : 0.0f;
         const int64_t yl = y - a.v0 - m0;
         const int own = scored && yl >= 0 && yl < words ? (int)yl - first : -1;
         const int some = w != 0.0f ? words - first : 0;
@@ -159,14 +176,66 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(
             }
     }
     store_bf16<T>(acc, lds, a.g, a.ldg, m0, a.ldg, n0, a.X.rows, true);
+    if constexpr (T::kBN > 128) return;  // up to 64 tokens: a narrower tile is taken
+    if (!a.two) return;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::kNJ; ++j)
+#pragma unroll
+        for (int i = 0; i < T::kMI; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const uint32_t r = bf16_pair(acc.v[i][j][e], acc.v[i][j][e + 1]);
+                acc.v[i][j][e] -= low_half(r);
+                acc.v[i][j][e + 1] -= high_half(r);
+            }
+    store_bf16<T>(acc, lds, a.g + a.X.rows * a.ldg, a.ldg, m0, a.ldg, n0, a.X.rows, true);
+}
+
+// The largest finite |weight| of the scored tokens, a part of it per block.
+constexpr int kMost = 256;
+
+__device__ __forceinline__ float block_max(float v, float *red) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    __syncthreads();
+    return v;
+}
+
+__global__ __launch_bounds__(256) void weight_most(const int64_t *__restrict__ target,
+                                                   const float *__restrict__ weight, int64_t tokens, int64_t vocab,
+                                                   float *__restrict__ most) {
+    __shared__ float red[4];
+    float v = 0.0f;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < tokens; t += kMost * 256) {
+        const int64_t y = target[t];
+        const float w = fabsf(weight[t]);
+        if (y >= 0 && y < vocab && w < INFINITY) v = fmaxf(v, w);
+    }
+    v = block_max(v, red);
+    if (threadIdx.x == 0) most[blockIdx.x] = v;
+}
+
+// Their largest, in a block of 256; 1 where no weight counts.
+__device__ __forceinline__ float largest(const float *most) {
+    __shared__ float red[4];
+    const float c = block_max(most[threadIdx.x], red);
+    return c == 0.0f ? 1.0f : c;
+}
+
+__device__ __forceinline__ float factor_of(int64_t y, float w, int64_t vocab, float c) {
+    return y < 0 || y >= vocab ? 0.0f : w / c;
 }
 
 struct DxArgs {
-    Operand W, g;    // W [vocab piece, d] across, g [tokens, piece]
+    Operand W, g;    // W [vocab piece, d] across, g [parts of tokens, piece]
     unsigned mtiles, tiles;
     int64_t k_split;
     bool add;
-    float *sum;      // [splits, tokens, d]
+    float *sum;      // [splits, parts of tokens, d]
 };
 
 template <class T>
@@ -183,33 +252,43 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dx_kernel(con
     store_sum<T>(acc, a.sum + split * a.g.rows * a.W.rows, m0, a.W.rows, n0, a.g.rows, true, a.add);
 }
 
-__global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int splits, int64_t fours,
-                                                      int64_t d, uint16_t *__restrict__ dX, int64_t lddx) {
+// Adds the splits, and the parts of a token, and rounds.
+__global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int parts, int64_t fours,
+                                                      int64_t d, const float *__restrict__ most,
+                                                      uint16_t *__restrict__ dX, int64_t lddx) {
     const int64_t stride = (int64_t)gridDim.x * 256;
+    const float c = largest(most);
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
         float4 v = sum[id];
-        for (int s = 1; s < splits; ++s) {
+        for (int s = 1; s < parts; ++s) {
             const float4 o = sum[(int64_t)s * fours + id];
             v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
         }
-        const int64_t t = id / (d / 4), c = id % (d / 4) * 4;
-        *reinterpret_cast<uint2 *>(dX + t * lddx + c) = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+        const int64_t t = id / (d / 4), m = id % (d / 4) * 4;
+        *reinterpret_cast<uint2 *>(dX + t * lddx + m) =
+            make_uint2(bf16_pair(v.x * c, v.y * c), bf16_pair(v.z * c, v.w * c));
     }
 }
 
-// X with zeros in the rows that are not scored, so that what lies there does
-// not meet the zeros of g in a product.
+// Every token's weight / c, and X with zeros in the rows that are not scored,
+// so that what lies there does not meet the zeros of h in a product; once for
+// each part of h.
 __global__ __launch_bounds__(256) void scored_rows(const uint16_t *__restrict__ X, int64_t ldx, int64_t tokens,
                                                    int64_t d, const int64_t *__restrict__ target,
                                                    const float *__restrict__ weight, int64_t vocab,
-                                                   u32x4 *__restrict__ S) {
-    const int64_t words = d / 8, total = tokens * words, stride = (int64_t)gridDim.x * 256;
-    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
-        const int64_t t = id / words, c = id - t * words;
+                                                   const float *__restrict__ most, float *__restrict__ factor,
+                                                   u32x4 *__restrict__ S, int parts) {
+    const int64_t stride = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const float c = largest(most);
+    for (int64_t t = first; t < tokens; t += stride) factor[t] = factor_of(target[t], weight[t], vocab, c);
+    if (!S) return;
+    const int64_t words = d / 8, total = tokens * words;
+    for (int64_t id = first; id < total; id += stride) {
+        const int64_t t = id / words, k = id - t * words;
         const int64_t y = target[t];
         u32x4 v = {0, 0, 0, 0};
-        if (y >= 0 && y < vocab && weight[t] != 0.0f) v = *reinterpret_cast<const u32x4 *>(X + t * ldx + c * 8);
-        S[id] = v;
+        if (y >= 0 && y < vocab && weight[t] != 0.0f) v = *reinterpret_cast<const u32x4 *>(X + t * ldx + k * 8);
+        for (int p = 0; p < parts; ++p) S[p * total + id] = v;
     }
 }
 
@@ -219,7 +298,8 @@ __global__ __launch_bounds__(256) void clear_kernel(uint2 *__restrict__ p, int64
 }
 
 struct DwArgs {
-    Operand X, g;    // X [tokens, d] across, g [tokens, piece] across
+    Operand X, g;    // X [parts of tokens, d] across, g [parts of tokens, piece] across
+    const float *most;
     unsigned mtiles;
     int64_t cols;    // rows of dW in this piece
     uint16_t *dW;    // [cols, d]
@@ -235,7 +315,11 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
     Acc<T> acc;
     acc.clear();
     tile_product<T, Across, Across>(acc, lds, a.X, m0, a.g, n0, 0, a.g.k);
-    store_bf16<T>(acc, lds, a.dW, a.X.rows, m0, a.X.rows, n0, a.cols, a.wide);
+    float c = a.most[threadIdx.x & 63];
+    for (int i = 64; i < kMost; i += 64) c = fmaxf(c, a.most[i + (threadIdx.x & 63)]);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) c = fmaxf(c, __shfl_xor(c, o, 64));
+    store_bf16<T>(acc, lds, a.dW, a.X.rows, m0, a.X.rows, n0, a.cols, a.wide, c == 0.0f ? 1.0f : c);
 }
 
 // ---------------------------------------------------------------------------
@@ -267,24 +351,29 @@ LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kLeastPiece = 2048;
 constexpr int64_t kPieceStep = 256;
+constexpr int64_t kTwoParts = 64;  // tokens up to which h is kept as two parts
 
 struct LossGradPlan {
+    int64_t parts;  // of h
     int64_t piece, pieces;
     Split dx;
-    size_t g, sum, rows, total;
+    size_t g, sum, rows, factor, total;
 };
 
 LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     LossGradPlan p;
-    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (2 * tokens) / kPieceStep * kPieceStep);
+    p.parts = tokens <= kTwoParts ? 2 : 1;
+    const int64_t rows = p.parts * tokens;
+    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (2 * rows) / kPieceStep * kPieceStep);
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    p.dx = split_plan(d, tokens, p.piece, true);
-    p.g = round_up((size_t)tokens * p.piece * 2, 256);
-    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
-    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
-    p.total = p.g + p.sum + p.rows;
+    p.dx = split_plan(d, rows, p.piece, true);
+    p.g = round_up((size_t)rows * p.piece * 2, 256);
+    p.sum = round_up((size_t)p.dx.splits * rows * d * 4, 256);
+    p.rows = dw ? round_up((size_t)rows * d * 2, 256) : 0;
+    p.factor = round_up((size_t)tokens * sizeof(float), 256);
+    p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
     return p;
 }
 
@@ -382,12 +471,15 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
     char *ws = static_cast<char *>(workspace);
     uint16_t *g = reinterpret_cast<uint16_t *>(ws);
     float *sum = reinterpret_cast<float *>(ws + p.g);
-    u32x4 *rows = reinterpret_cast<u32x4 *>(ws + p.g + p.sum);
-    if (dW) {
-        hipLaunchKernelGGL(scored_rows, dim3(grid_for(tokens * d / 8, 256)), dim3(256), 0, stream,
-                           static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, rows);
-        if (const int st = launch_status()) return st;
-    }
+    u32x4 *rows = dW ? reinterpret_cast<u32x4 *>(ws + p.g + p.sum) : nullptr;
+    float *factor = reinterpret_cast<float *>(ws + p.g + p.sum + p.rows);
+    float *most = reinterpret_cast<float *>(ws + p.g + p.sum + p.rows + p.factor);
+    hipLaunchKernelGGL(weight_most, dim3(kMost), dim3(256), 0, stream, target, weight, tokens, vocab, most);
+    if (const int st = launch_status()) return st;
+    hipLaunchKernelGGL(scored_rows, dim3(grid_for(dW ? tokens * d / 8 : tokens, 256)), dim3(256), 0, stream,
+                       static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, most, factor, rows,
+                       (int)p.parts);
+    if (const int st = launch_status()) return st;
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t cols = std::min(p.piece, vocab - v0), ldg = cdiv(cols, kPieceStep) * kPieceStep;
         const uint16_t *Wp = static_cast<const uint16_t *>(W) + v0 * d;
@@ -398,19 +490,21 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         a.v0 = v0;
         a.vocab = vocab;
         a.lse = lse;
-        a.weight = weight;
+        a.factor = factor;
+        a.two = p.parts == 2;
         a.g = g;
         a.ldg = ldg;
-        const Split logits = split_plan(ldg, tokens, d, false);
+        Split logits = split_plan(ldg, tokens, d, false);
+        if (a.two && logits.size == kLarge) logits.size = kMiddle;
         a.mtiles = (unsigned)(ldg / logits.side_m());
         LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
         if (const int st = launch_status()) return st;
         if (dX) {
             DxArgs x{};
             x.W = Operand{Wp, d, d, cols};
-            x.g = Operand{g, ldg, tokens, ldg};
+            x.g = Operand{g, ldg, p.parts * tokens, ldg};
             x.mtiles = (unsigned)cdiv(d, p.dx.side_m());
-            x.tiles = (unsigned)p.dx.units(d, tokens);
+            x.tiles = (unsigned)p.dx.units(d, p.parts * tokens);
             x.k_split = p.dx.k;
             x.add = v0 > 0;
             x.sum = sum;
@@ -419,9 +513,10 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         }
         if (dW) {
             DwArgs b{};
-            b.X = Operand{rows, d, d, tokens};
-            b.g = Operand{g, ldg, ldg, tokens};
-            const Split rows_of = split_plan(d, cols, tokens, false);
+            b.X = Operand{rows, d, d, p.parts * tokens};
+            b.g = Operand{g, ldg, ldg, p.parts * tokens};
+            b.most = most;
+            const Split rows_of = split_plan(d, cols, p.parts * tokens, false);
             b.mtiles = (unsigned)cdiv(d, rows_of.side_m());
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;
@@ -433,8 +528,8 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
     if (dX) {
         const int64_t fours = tokens * d / 4;
         hipLaunchKernelGGL(loss_dx_finish, dim3(grid_for(fours, 256)), dim3(256), 0, stream,
-                           reinterpret_cast<const float4 *>(sum), p.dx.splits, fours, d, static_cast<uint16_t *>(dX),
-                           lddx);
+                           reinterpret_cast<const float4 *>(sum), p.dx.splits * (int)p.parts, fours, d, most,
+                           static_cast<uint16_t *>(dX), lddx);
         return launch_status();
     }
     return HSCALE_OK;
