@@ -205,17 +205,22 @@ __device__ __forceinline__ float block_max(float v, float *red) {
     return v;
 }
 
-__global__ __launch_bounds__(256) void weight_most(const int64_t *__restrict__ target,
-                                                   const float *__restrict__ weight, int64_t tokens, int64_t vocab,
-                                                   float *__restrict__ most) {
+__device__ __forceinline__ float scored_most(const int64_t *target, const float *weight, int64_t first, int64_t tokens,
+                                             int64_t step, int64_t vocab) {
     __shared__ float red[4];
     float v = 0.0f;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < tokens; t += kMost * 256) {
+    for (int64_t t = first; t < tokens; t += step) {
         const int64_t y = target[t];
         const float w = fabsf(weight[t]);
         if (y >= 0 && y < vocab && w < INFINITY) v = fmaxf(v, w);
     }
-    v = block_max(v, red);
+    return block_max(v, red);
+}
+
+__global__ __launch_bounds__(256) void weight_most(const int64_t *__restrict__ target,
+                                                   const float *__restrict__ weight, int64_t tokens, int64_t vocab,
+                                                   float *__restrict__ most) {
+    const float v = scored_most(target, weight, (int64_t)blockIdx.x * 256 + threadIdx.x, tokens, kMost * 256, vocab);
     if (threadIdx.x == 0) most[blockIdx.x] = v;
 }
 
@@ -272,14 +277,23 @@ __global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__
 
 // Every token's weight / c, and X with zeros in the rows that are not scored,
 // so that what lies there does not meet the zeros of h in a product; once for
-// each part of h.
+// each part of h.  Of few tokens each block finds the largest weight itself and
+// the first leaves it in `most`, which saves a launch.
+template <bool few>
 __global__ __launch_bounds__(256) void scored_rows(const uint16_t *__restrict__ X, int64_t ldx, int64_t tokens,
                                                    int64_t d, const int64_t *__restrict__ target,
                                                    const float *__restrict__ weight, int64_t vocab,
-                                                   const float *__restrict__ most, float *__restrict__ factor,
+                                                   float *__restrict__ most, float *__restrict__ factor,
                                                    u32x4 *__restrict__ S, int parts) {
     const int64_t stride = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const float c = largest(most);
+    float c;
+    if constexpr (few) {
+        c = scored_most(target, weight, threadIdx.x, tokens, 256, vocab);
+        if (blockIdx.x == 0) most[threadIdx.x] = threadIdx.x == 0 ? c : 0.0f;
+        c = c == 0.0f ? 1.0f : c;
+    } else {
+        c = largest(most);
+    }
     for (int64_t t = first; t < tokens; t += stride) factor[t] = factor_of(target[t], weight[t], vocab, c);
     if (!S) return;
     const int64_t words = d / 8, total = tokens * words;
@@ -351,6 +365,7 @@ LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kLeastPiece = 2048;
 constexpr int64_t kPieceStep = 256;
+constexpr int64_t kFewWeights = 4096;  // tokens whose weights each block reads: 16 loads of a thread
 constexpr int64_t kTwoParts = 64;  // tokens up to which h is kept as two parts
 
 struct LossGradPlan {
@@ -474,9 +489,11 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
     u32x4 *rows = dW ? reinterpret_cast<u32x4 *>(ws + p.g + p.sum) : nullptr;
     float *factor = reinterpret_cast<float *>(ws + p.g + p.sum + p.rows);
     float *most = reinterpret_cast<float *>(ws + p.g + p.sum + p.rows + p.factor);
-    hipLaunchKernelGGL(weight_most, dim3(kMost), dim3(256), 0, stream, target, weight, tokens, vocab, most);
-    if (const int st = launch_status()) return st;
-    hipLaunchKernelGGL(scored_rows, dim3(grid_for(dW ? tokens * d / 8 : tokens, 256)), dim3(256), 0, stream,
+    if (tokens > kFewWeights) {
+        hipLaunchKernelGGL(weight_most, dim3(kMost), dim3(256), 0, stream, target, weight, tokens, vocab, most);
+        if (const int st = launch_status()) return st;
+    }
+    hipLaunchKernelGGL(tokens > kFewWeights ? scored_rows<false> : scored_rows<true>, dim3(grid_for(dW ? tokens * d / 8 : tokens, 256)), dim3(256), 0, stream,
                        static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, most, factor, rows,
                        (int)p.parts);
     if (const int st = launch_status()) return st;
