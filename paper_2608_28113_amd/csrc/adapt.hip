@@ -10,9 +10,12 @@
 //
 // An E2M1 value has 2 significant bits and an E4M3 scale 4, so with the power
 // of two of s_g = f 2^e (1 <= f < 2) W^ is exact in bf16: the products with W^
-// are bf16 products accumulated in fp32, and f multiplies the sum.  u and v are kept as two bf16 parts
-// (within 2^-16), so that nothing of the adapters' part is rounded to 8 bits
-// before the result is.
+// are bf16 products accumulated in fp32, and f multiplies the sum.  u and v are
+// kept as two bf16 parts (within 2^-16), so that nothing of the adapters' part
+// is rounded to 8 bits before the result is.
+//
+// Times below are of one MI355X, whose large copies reach 4.9 TB/s, streaming
+// reads 6.9 TB/s and large bf16 products 1.4 to 1.5 PFLOP/s.
 
 #include "matmul.h"
 
@@ -95,7 +98,10 @@ __device__ __forceinline__ u32x4 stored_eight(uint32_t src, float l) {
     return u32x4{stored_pair<0>(src, l), stored_pair<1>(src, l), stored_pair<2>(src, l), stored_pair<3>(src, l)};
 }
 
-// W^ [groups * 16] with 2^e in place of s_g, one group per thread.
+// W^ [groups * 16] with 2^e in place of s_g, one group per thread.  HBM bounds
+// it: 14336 x 4096 in 31 us, 4.8 TB/s of 33 MB read and 117 MB written.  For
+// many tokens that is less than converting in every tile of the product, whose
+// matrix cores would wait for it.
 __global__ __launch_bounds__(256) void stored_to_bf16(const uint8_t *__restrict__ codes,
                                                       const uint2 *__restrict__ packed, int64_t groups, int e,
                                                       u32x4 *__restrict__ W) {
@@ -138,7 +144,8 @@ __device__ __forceinline__ u32x4 restore8(uint32_t lo, uint32_t hi, float s) {
 
 // A thread per 8 values, 16 threads per block of 128 (the last of a row may
 // be shorter): s = fp32(m fp32(1/127)) with m = max(|x|, 2^-100), and
-// q = rint(fp32(x fp32(127 / m))).
+// q = rint(fp32(x fp32(127 / m))).  HBM bounds this and the way back: 16384 x
+// 14336 in 136 and 109 us, 5.2 and 6.5 TB/s.
 __global__ __launch_bounds__(256) void pack_kernel(const uint16_t *__restrict__ X, int64_t tokens, int64_t in,
                                                    int64_t ldx, uint2 *__restrict__ q, float *__restrict__ scale) {
     const int64_t blocks = (in + kCkBlock - 1) / kCkBlock, total = tokens * blocks * 16;
@@ -219,6 +226,9 @@ struct ShrinkArgs {
 // bytes at a time (two lanes 32 consecutive ones); the adapter's rows, the
 // same for all waves, come through LDS, 16-byte chunk c of row j at c ^ (j % 16).
 // Checkpoints are taken 256 k at a time, so that as many bytes are under way.
+// 8192 x 4096 at rank 16 in 17 us (3.9 TB/s); a checkpoint of 8192 x 14336 at
+// rank 64 in 85 us (1.4 TB/s of 121 MB; MFMA 0.07 and VALU 0.18 busy): few and
+// short stages, each of which waits for its loads and for the block's barrier.
 template <bool kCheckpoint, int kMI>
 __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
     constexpr int kK = kCheckpoint ? 256 : 128, kARow = kK * 2, kABytes = 32 * kMI * kARow;
@@ -470,6 +480,9 @@ struct LayerArgs {
 
 template <class T, Layout LW>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void layer_kernel(const LayerArgs a) {
+    // 8192 tokens of 4096 -> 14336 with adapters of rank 16: 790 us, 1.22 PFLOP/s
+    // at MFMA 0.63 busy and 1.87 GHz; the plain product in the same tiles reaches
+    // 1.25 to 1.35 as the chip's power lets its clock.
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
@@ -595,6 +608,10 @@ __device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t 
 // weights comes straight from memory, 32 consecutive weights a lane: which k
 // meets which place in a step does not matter, as both operands agree.  X goes
 // through LDS, 16 bytes a lane, row t's 16-byte chunk c at c ^ (t % 16).
+// 1 token of 4096 -> 1024 in 6.7 us, latency alone; 48 of 4096 -> 14336 in 24 us
+// (33 MB of weights, 8 of 24 us by HBM; VALU 0.20 busy, half the time waiting);
+// 515 of 14336 -> 4096 in 104 us, 0.58 PFLOP/s: MFMA 0.31, LDS 0.31, VALU 0.33
+// busy, which two blocks' waves overlap only in part.
 constexpr int kFewK = 512, kFewRows = 128;  // a split is a multiple of kFewK
 
 struct FewArgs {
@@ -883,6 +900,10 @@ struct OuterArgs {
     const int32_t *ids;
     int64_t t_split;      // of a split, a multiple of 64
     float *partial;       // [splits, count, rank, width]
+    // of a single split: the result, `by` times the sums, in place of `partial`
+    uint16_t *G;          // dA [count, rank, width], dB [count, columns, rank]
+    int64_t columns;
+    float by;
 };
 
 constexpr int kOuterCols = 256, kOuterTokens = 64, kOuterThreads = 512;
@@ -892,8 +913,21 @@ constexpr int kOuterCols = 256, kOuterTokens = 64, kOuterThreads = 512;
 // are under way to registers while one multiplies.  Tokens of other adapters
 // are not read and enter as zeros, stages without any are passed over: which
 // ones have some is found for many stages at a time, so that a stage's rows
-// do not wait for its adapters' numbers.
+// do not wait for its adapters' numbers.  A checkpoint of 8192 x 14336 (two
+// parts of rank 64, four adapters) takes 85 us, dY of 8192 x 4096 46: the
+// blocks that have tokens of their adapter are not many more than run at once,
+// and the longest last.  Sharing out the stages evenly cost more than that (121
+// and 78 us: every block then visits every part of the tokens).
 constexpr int kOuterMasks = 256;
+
+// Four bf16 values to where they may not be aligned together.
+__device__ __forceinline__ void store_four(uint16_t *dst, uint32_t lo, uint32_t hi) {
+    if ((reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+    } else {
+        dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16), dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
+    }
+}
 
 template <bool kCheckpoint, int kRT>
 __global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs a) {
@@ -1006,6 +1040,24 @@ __global__ __launch_bounds__(kOuterThreads, 4) void outer_kernel(const OuterArgs
     for (int r = 0; r < kRT; ++r) {
         const int j = j0 + r * 32 + (lane & 31);
         if (j >= a.rank) continue;
+        if (a.G) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = c0 + wave * 32 + 8 * q + 4 * (lane >> 5);
+                const uint32_t lo = bf16_pair(acc[r][4 * q] * a.by, acc[r][4 * q + 1] * a.by);
+                const uint32_t hi = bf16_pair(acc[r][4 * q + 2] * a.by, acc[r][4 * q + 3] * a.by);
+                if constexpr (kCheckpoint) {
+                    if (c < width) store_four(a.G + ((int64_t)adapter * a.rank + j) * width + c, lo, hi);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < a.columns)
+                            a.G[((int64_t)adapter * a.columns + c + e) * a.rank + j] =
+                                (uint16_t)((e < 2 ? lo : hi) >> (16 * (e & 1)));
+                }
+            }
+            continue;
+        }
         float *dst = a.partial + (((int64_t)blockIdx.z * a.count + adapter) * a.rank + j) * a.width;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -1029,12 +1081,7 @@ __global__ __launch_bounds__(256) void outer_finish(const float4 *__restrict__ p
             v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
         }
         const uint32_t lo = bf16_pair(v.x * scale, v.y * scale), hi = bf16_pair(v.z * scale, v.w * scale);
-        uint16_t *dst = G + id * 4;
-        if ((reinterpret_cast<uintptr_t>(G) & 7) == 0) {
-            *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
-        } else {
-            dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16), dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
-        }
+        store_four(G + id * 4, lo, hi);
     }
 }
 
@@ -1056,14 +1103,26 @@ __global__ __launch_bounds__(256) void outer_finish_turned(const float *__restri
         G[(a * columns + c0) * rank + i] = (uint16_t)bf16_rne(tile[i % rank * 33 + i / rank]);
 }
 
-// B [count, out, rank] as [count, rank, width], width >= out, zeros beyond.
-__global__ __launch_bounds__(256) void turn_kernel(const uint16_t *__restrict__ B, int64_t count, int64_t out,
-                                                   int rank, int64_t width, uint16_t *__restrict__ T) {
-    const int64_t total = count * rank * width, stride = (int64_t)gridDim.x * 256;
-    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += stride) {
-        const int64_t c = id % width, aj = id / width, a = aj / rank, j = aj % rank;
-        T[id] = c < out ? B[(a * out + c) * rank + j] : (uint16_t)0;
+// B [count, out, rank] as [count, rank, width], width >= out, zeros beyond: 32
+// columns of one adapter a block, whole rows in and runs of columns out.
+__global__ __launch_bounds__(256) void turn_kernel(const uint16_t *__restrict__ B, int64_t out, int rank, int64_t width,
+                                                   uint16_t *__restrict__ T) {
+    __shared__ uint16_t tile[32 * (kMaxRank + 2)];
+    const int64_t c0 = (int64_t)blockIdx.x * 32, a = blockIdx.y;
+    const int row = rank + 2, words = rank / 8;
+    for (int i = threadIdx.x; i < 32 * words; i += 256) {
+        const int c = i / words, k = i - c * words;
+        u32x4 v = {0, 0, 0, 0};
+        if (c0 + c < out) v = *reinterpret_cast<const u32x4 *>(B + (a * out + c0 + c) * rank + k * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t *>(tile + c * row + k * 8 + 2 * e) = v[e];
     }
+    __syncthreads();
+    const int c = (threadIdx.x & 15) * 2;
+    if (c0 + c >= width) return;
+    for (int j = threadIdx.x >> 4; j < rank; j += 16)
+        *reinterpret_cast<uint32_t *>(T + (a * rank + j) * width + c0 + c) =
+            (uint32_t)tile[c * row + j] | (uint32_t)tile[(c + 1) * row + j] << 16;
 }
 
 // Rows of `width` >= out columns, zeros beyond.
@@ -1281,7 +1340,9 @@ GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank,
     p.low = low_bytes(tokens, rank);
     outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
     outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
-    p.outer = round_up(std::max((size_t)p.splits_a * in, (size_t)p.splits_b * p.width) * count * rank * 4, 256);
+    const size_t cols_a = p.splits_a > 1 ? (size_t)p.splits_a * in : 0;
+    const size_t cols_b = p.splits_b > 1 ? (size_t)p.splits_b * p.width : 0;
+    p.outer = round_up(std::max(cols_a, cols_b) * count * rank * 4, 256);
     p.tile = split_plan(in, tokens, p.width, true);
     p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
     p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
@@ -1533,8 +1594,8 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
             if (const int st = launch_status()) return st;
             dy = Rows{wide_dy, nullptr, p.width};
         }
-        hipLaunchKernelGGL(turn_kernel, dim3(grid_for(ad.count * ad.rank * p.width, 256)), dim3(256), 0, stream, ad.B,
-                           (int64_t)ad.count, out, ad.rank, p.width, turned);
+        hipLaunchKernelGGL(turn_kernel, dim3((unsigned)cdiv(p.width, 32), (unsigned)ad.count), dim3(256), 0, stream,
+                           ad.B, out, ad.rank, p.width, turned);
         if (const int st = launch_status()) return st;
         if (const int st = shrink_to_low(dy, tokens, p.width, turned, ad, p.v, f, partial, v, stream)) return st;
         if (const int st = shrink_to_low(x, tokens, in, ad.A, ad, p.u, 1.0f, partial, u, stream)) return st;
@@ -1554,7 +1615,8 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
     auto outer_of = [&](const Rows &z, int64_t width, int64_t columns, const uint16_t *low, int64_t split, int splits,
                         float by, void *G, bool transposed) {
         if (tokens > 0) {
-            const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, low_pad(ad.rank), ad.ids, split, outer};
+            const OuterArgs a{z, tokens, width, low, ad.count, ad.rank, low_pad(ad.rank), ad.ids, split, outer,
+                              splits == 1 ? static_cast<uint16_t *>(G) : nullptr, columns, by};
             const dim3 grid((unsigned)cdiv(width, kOuterCols),
                             (unsigned)(cdiv(ad.rank, rank_tile(ad.rank)) * ad.count), (unsigned)splits);
             if (z.scale && ad.rank <= 32)
@@ -1565,7 +1627,8 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
                 hipLaunchKernelGGL((outer_kernel<false, 1>), grid, dim3(kOuterThreads), 0, stream, a);
             else
                 hipLaunchKernelGGL((outer_kernel<false, 2>), grid, dim3(kOuterThreads), 0, stream, a);
-            if (const int st = launch_status()) return st;
+            const int st = launch_status();
+            if (st || splits == 1) return st;
         }
         if (transposed) {
             hipLaunchKernelGGL(outer_finish_turned, dim3((unsigned)cdiv(columns, 32), (unsigned)ad.count), dim3(256),
