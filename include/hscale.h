@@ -460,8 +460,8 @@ typedef struct hscale_adapters {
                                outside 0 .. count - 1 for none; NULL: all use 0 */
 } hscale_adapters;
 
-/* Workspace bytes hscale_adapted_linear needs (0 when a size is 0 or invalid;
- * count = 0 without adapters). */
+/* Workspace bytes hscale_adapted_linear needs (0 when none, or when a size is
+ * 0 or invalid; count = 0 without adapters). */
 size_t hscale_adapted_linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t count, int32_t rank);
 
 /*

@@ -6,6 +6,13 @@ H-Scale refines NVFP4 per-group scales with a diagonal second-order proxy:
 neighbours of the max-abs scale that minimises the h-weighted reconstruction
 error, returning NVFP4 scale bytes and packed E2M1 codes.
 
+The stored layer is then served and trained through: ``adapted_linear``
+applies it to the tokens of many requests, each with a low-rank adapter of its
+own or none; ``pack_activations`` keeps its input in 8 bits for the backward
+pass, ``token_loss`` and ``token_loss_grad`` are the cross entropy over a large
+vocabulary and its gradient without stored logits, and ``adapted_linear_grad``
+returns the gradients of the adapters and of the layer's input.
+
 The compute is in ``libhscale.so`` (hand-written HIP, C ABI in
 ``include/hscale.h``); this package is its thin Python binding.
 """

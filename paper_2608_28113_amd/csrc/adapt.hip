@@ -1141,7 +1141,20 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 
 
 constexpr int kTargetBlocks = 1024;
-constexpr int64_t kFewTokens = 1024, kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
+
+// Up to 1024 tokens the stored weights go straight into the product; above,
+// they are converted once and multiplied in tiles.  That way (and the other),
+// us: 512 tokens of 4096 -> 14336 75 (151); 1040 of 4096 -> 14336 153 (161),
+// of 14336 -> 4096 191 (169), of 4096 -> 4096 71 (65), of 4096 -> 1024 27 (29);
+// 2040 of 4096 -> 14336 274 (243).
+constexpr int64_t kFewTokens = 1024;
+// Up to 64 tokens a block takes them all, in sixteens, and the adapters' part
+// is computed beside the product and added at its end (fused); above, a block
+// takes 128, and that is done while tokens x outputs x rank are few.  64 and 80 tokens of
+// 4096 -> 14336 with eight adapters of rank 16: 27 and 38 us, of 4096 -> 1024
+// 11.5 and 13; reading B per token, as the end does, grows with tokens and
+// outputs, where the product's own stages read it once per 128 tokens.
+constexpr int64_t kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
@@ -1320,9 +1333,14 @@ struct GradPlan {
 };
 
 // Splits of the tokens for the adapters' gradients.
+// Up to 512 tokens are not split, which saves the partial sums and the kernels
+// that add them: 500 tokens of 1024 -> 4096, eight adapters of rank 32, 70 us
+// so and 79 in two splits; 512 of 8192 -> 1024, one of rank 64, 83 and 82.
+constexpr int64_t kOuterWhole = 512;
+
 inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
     const int64_t blocks = cdiv(width, kOuterCols) * cdiv(rank, rank_tile(rank)) * count;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256)));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), tokens <= kOuterWhole ? 1 : cdiv(tokens, 256)));
     split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
     splits = (int)cdiv(tokens, split);
 }
