@@ -117,6 +117,70 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_tile_kernel(c
     }
 }
 
+// Where tokens and words make few tiles of many k, k is split and the logits'
+// partial sums [splits, tokens, words] are written: 4 x 500 words of 8192 in one
+// tile take 128 stages, one after another.
+struct LogitSumArgs {
+    Operand W, X;
+    unsigned mtiles, tiles;
+    int64_t k_split, words;  // words: a multiple of 4
+    float *sum;
+};
+
+template <class T>
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void logit_sum_kernel(const LogitSumArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    unsigned mt, nt;
+    tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
+    const int64_t split = blockIdx.x / a.tiles;
+    const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
+    const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.X.k ? k0 + a.k_split : a.X.k;
+    Acc<T> acc;
+    acc.clear();
+    tile_product<T, Along, Along>(acc, lds, a.W, m0, a.X, n0, k0, k1);
+    store_sum<T>(acc, a.sum + split * a.X.rows * a.words, m0, a.words, n0, a.X.rows, true, false);
+}
+
+__device__ __forceinline__ float4 logits_of(const float4 *sum, int splits, int64_t fours, int64_t id) {
+    float4 v = sum[id];
+    for (int s = 1; s < splits; ++s) {
+        const float4 o = sum[(int64_t)s * fours + id];
+        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+    }
+    return v;
+}
+
+// The loss of a token per block from them.
+__global__ __launch_bounds__(256) void loss_rows(const float4 *__restrict__ sum, int splits, int64_t words,
+                                                 const int64_t *__restrict__ target, int64_t vocab,
+                                                 float *__restrict__ loss, float *__restrict__ lse) {
+    __shared__ float2 red[4];
+    __shared__ float at;
+    const int64_t t = blockIdx.x, row = words / 4, fours = row * gridDim.x;
+    const int64_t y = target[t];
+    float2 p = make_float2(-INFINITY, 0.0f);
+    for (int64_t k = threadIdx.x; k < row; k += 256) {
+        const float4 q = logits_of(sum, splits, fours, t * row + k);
+        const float v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (4 * k + e >= vocab) continue;
+            p = join(p, make_float2(v[e], v[e] == v[e] ? 1.0f : v[e]));
+            if (4 * k + e == y) at = v[e];
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) p = join(p, make_float2(__shfl_xor(p.x, o, 64), __shfl_xor(p.y, o, 64)));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = p;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) p = join(p, red[w]);
+    const float l = p.x + logf(p.y);
+    lse[t] = l;
+    loss[t] = y >= 0 && y < vocab ? l - at : 0.0f;
+}
+
 // 64 tokens per block, four threads to a token.  8192 tokens' 500 parts each (33
 // MB) in 22 us: 128 blocks, so their loads' latency bounds it, 8 at a time.
 __global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ parts, int64_t tiles, int64_t tokens,
@@ -245,6 +309,30 @@ __device__ __forceinline__ float factor_of(int64_t y, float w, int64_t vocab, fl
 
 // dX and dW of such a piece: 1.59 and 1.64 ms, 1.35 and 1.31 PFLOP/s at MFMA
 // 0.72 busy and 1.77 GHz, where a library product of that size reaches 1.39.
+// h from the logits' partial sums, four words a thread.
+__global__ __launch_bounds__(256) void slope_rows(const float4 *__restrict__ sum, int splits, int64_t tokens,
+                                                  int64_t words, int64_t vocab, const int64_t *__restrict__ target,
+                                                  const float *__restrict__ lse, const float *__restrict__ factor,
+                                                  uint2 *__restrict__ g, bool two) {
+    const int64_t row = words / 4, fours = tokens * row, stride = (int64_t)gridDim.x * 256;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
+        const int64_t t = id / row, v0 = (id - t * row) * 4, y = target[t];
+        const float4 q = logits_of(sum, splits, fours, id);
+        const float w = factor[t], l = lse[t], x[4] = {q.x, q.y, q.z, q.w};
+        float h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p = exp_of(x[e] - l) - (v0 + e == y ? 1.0f : 0.0f);
+            h[e] = w != 0.0f && v0 + e < vocab ? w * p : 0.0f;
+        }
+        const uint2 r = make_uint2(bf16_pair(h[0], h[1]), bf16_pair(h[2], h[3]));
+        g[id] = r;
+        if (two)
+            g[fours + id] = make_uint2(bf16_pair(h[0] - low_half(r.x), h[1] - high_half(r.x)),
+                                       bf16_pair(h[2] - low_half(r.y), h[3] - high_half(r.y)));
+    }
+}
+
 struct DxArgs {
     Operand W, g;    // W [vocab piece, d] across, g [parts of tokens, piece]
     unsigned mtiles, tiles;
@@ -353,18 +441,47 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 #define loss_tile_kernel_of(T) loss_tile_kernel<T>
+#define logit_sum_kernel_of(T) logit_sum_kernel<T>
 #define loss_slope_kernel_of(T) loss_slope_kernel<T>
 #define loss_dx_kernel_of(T) loss_dx_kernel<T>
 #define loss_dw_kernel_of(T) loss_dw_kernel<T>
 
+// k is split where 128 x 128 tiles leave half the chip without one.  Loss of 20
+// tokens of 8192 over 500 words: 18 us so, 66 in one pass; of 300 over 2000: 29
+// and 67; at 250 tiles (64 tokens of 4096 over 32000 words) both take 68.
+Split logit_plan(int64_t words, int64_t tokens, int64_t d, bool one_piece) {
+    return split_plan(words, tokens, d, one_piece && cdiv(words, 128) * cdiv(tokens, 128) <= kCUs / 2);
+}
+
 struct LossPlan {
     Split tile;
-    size_t parts, at, total;
+    size_t parts, at, total;  // parts: partial sums, if split
 };
+
+// The logits' partial sums of `words` (a multiple of 4).
+int logit_sums(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab, int64_t words,
+               const Split &p, float *sum, hipStream_t stream) {
+    LogitSumArgs a{};
+    a.W = Operand{W, d, vocab, d};
+    a.X = Operand{X, ldx, tokens, d};
+    a.mtiles = (unsigned)cdiv(words, p.side_m());
+    a.tiles = (unsigned)p.units(words, tokens);
+    a.k_split = p.k;
+    a.words = words;
+    a.sum = sum;
+    LAUNCH_TILES(logit_sum_kernel_of, Large, p.size, a.tiles * (unsigned)p.splits, stream, a);
+    return launch_status();
+}
 
 LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     LossPlan p;
-    p.tile = split_plan(vocab, tokens, d, false);
+    const int64_t words = cdiv(vocab, 4) * 4;
+    p.tile = logit_plan(words, tokens, d, true);
+    if (p.tile.splits > 1) {
+        p.parts = p.total = round_up((size_t)p.tile.splits * tokens * words * 4, 256);
+        p.at = 0;
+        return p;
+    }
     p.parts = round_up((size_t)cdiv(vocab, p.tile.side_m()) * tokens * sizeof(float2), 256);
     p.at = round_up((size_t)tokens * 4, 256);
     p.total = p.parts + p.at;
@@ -386,7 +503,7 @@ constexpr int64_t kTwoParts = 64;  // tokens up to which h is kept as two parts
 struct LossGradPlan {
     int64_t parts;  // of h
     int64_t piece, pieces;
-    Split dx;
+    Split dx, logits;  // logits: of a single piece, whose k may be split
     size_t g, sum, rows, factor, total;
 };
 
@@ -399,8 +516,11 @@ LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
     p.dx = split_plan(d, rows, p.piece, true);
+    p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
     p.g = round_up((size_t)rows * p.piece * 2, 256);
     p.sum = round_up((size_t)p.dx.splits * rows * d * 4, 256);
+    if (p.logits.splits > 1)  // in turn
+        p.sum = std::max(p.sum, round_up((size_t)p.logits.splits * tokens * p.piece * 4, 256));
     p.rows = dw ? round_up((size_t)rows * d * 2, 256) : 0;
     p.factor = round_up((size_t)tokens * sizeof(float), 256);
     p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
@@ -451,6 +571,14 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
     const Range w[] = {{loss, (size_t)tokens * 4}, {lse, (size_t)tokens * 4}, {workspace, p.total}};
     const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8}};
     if (any_overlap(w, 3, r, 3)) return HSCALE_ERR_OVERLAP;
+    if (p.tile.splits > 1) {
+        const int64_t words = cdiv(vocab, 4) * 4;
+        float *sum = static_cast<float *>(workspace);
+        if (const int st = logit_sums(X, tokens, d, ldx, W, vocab, words, p.tile, sum, stream)) return st;
+        hipLaunchKernelGGL(loss_rows, dim3((unsigned)tokens), dim3(256), 0, stream,
+                           reinterpret_cast<const float4 *>(sum), p.tile.splits, words, target, vocab, loss, lse);
+        return launch_status();
+    }
     LogitArgs a{};
     a.W = Operand{W, d, vocab, d};
     a.X = Operand{X, ldx, tokens, d};
@@ -515,22 +643,30 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t cols = std::min(p.piece, vocab - v0), ldg = cdiv(cols, kPieceStep) * kPieceStep;
         const uint16_t *Wp = static_cast<const uint16_t *>(W) + v0 * d;
-        LogitArgs a{};
-        a.W = Operand{Wp, d, cols, d};
-        a.X = Operand{X, ldx, tokens, d};
-        a.target = target;
-        a.v0 = v0;
-        a.vocab = vocab;
-        a.lse = lse;
-        a.factor = factor;
-        a.two = p.parts == 2;
-        a.g = g;
-        a.ldg = ldg;
-        Split logits = split_plan(ldg, tokens, d, false);
-        if (a.two && logits.size == kLarge) logits.size = kMiddle;
-        a.mtiles = (unsigned)(ldg / logits.side_m());
-        LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
-        if (const int st = launch_status()) return st;
+        if (p.logits.splits > 1) {
+            if (const int st = logit_sums(X, tokens, d, ldx, W, vocab, ldg, p.logits, sum, stream)) return st;
+            hipLaunchKernelGGL(slope_rows, dim3(grid_for(tokens * ldg / 4, 256)), dim3(256), 0, stream,
+                               reinterpret_cast<const float4 *>(sum), p.logits.splits, tokens, ldg, vocab, target, lse,
+                               factor, reinterpret_cast<uint2 *>(g), p.parts == 2);
+            if (const int st = launch_status()) return st;
+        } else {
+            LogitArgs a{};
+            a.W = Operand{Wp, d, cols, d};
+            a.X = Operand{X, ldx, tokens, d};
+            a.target = target;
+            a.v0 = v0;
+            a.vocab = vocab;
+            a.lse = lse;
+            a.factor = factor;
+            a.two = p.parts == 2;
+            a.g = g;
+            a.ldg = ldg;
+            Split logits = split_plan(ldg, tokens, d, false);
+            if (a.two && logits.size == kLarge) logits.size = kMiddle;
+            a.mtiles = (unsigned)(ldg / logits.side_m());
+            LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
+            if (const int st = launch_status()) return st;
+        }
         if (dX) {
             DxArgs x{};
             x.W = Operand{Wp, d, d, cols};

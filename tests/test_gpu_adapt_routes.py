@@ -8,7 +8,7 @@ import torch
 
 from tests import adapt_ref as ref
 from tests.test_gpu_adapt import S_G, _bf, _check_grad, _check_linear, _close, _gen, _low, _problem
-from tests.test_gpu_loss import _problem as _loss_problem
+from tests.test_gpu_loss import _check_grad as _check_loss_grad, _check_loss, _problem as _loss_problem
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
 
@@ -116,3 +116,25 @@ def test_a_weight_that_is_not_finite_reaches_only_its_row_of_dx(hs):
     keep[[0, 3]] = False
     assert torch.equal(got[keep], plain[keep])
     assert not torch.isfinite(got[[0, 3]].float()).all(1).any()
+
+
+@pytest.mark.parametrize("T,d,V", [(1, 4096, 3), (20, 8192, 500), (64, 2064, 1001), (130, 4112, 258), (3, 1024, 9001)])
+def test_loss_of_few_tokens_and_words_of_many_k(hs, T, d, V):
+    X, W, target, weight = _loss_problem(T, d, V, seed=T + V)
+    _, lse = _check_loss(hs, X, W, target)
+    _check_loss_grad(hs, X, W, target, weight, lse)
+
+
+def test_loss_rows_that_are_not_finite_stay_alone(hs):
+    T, d, V = 20, 4096, 300
+    X, W, target, weight = _loss_problem(T, d, V, seed=1)
+    target[7], target[8] = -100, 5
+    loss, lse = hs.token_loss(X, W, target)
+    X = X.clone()
+    X[7], X[8] = float("nan"), float("nan")
+    got, got_lse = hs.token_loss(X, W, target)
+    torch.cuda.synchronize()
+    keep = torch.ones(T, dtype=torch.bool, device=DEV)
+    keep[[7, 8]] = False
+    assert torch.equal(got[keep], loss[keep]) and torch.equal(got_lse[keep], lse[keep])
+    assert got[7] == 0 and got[8].isnan() and got_lse[[7, 8]].isnan().all()
