@@ -535,7 +535,8 @@ size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t voca
 
 /*
  * Softmax cross entropy of each token over a vocabulary, without storing the
- * logits l = X W^T (bf16 products, fp32 sums):
+ * logits l = X W^T (bf16 products, fp32 sums; few tokens over few words keep
+ * partial sums of theirs in the workspace):
  *   lse[t] = log sum_v exp(l[t, v]),  loss[t] = lse[t] - l[t, target[t]]
  * A target outside 0 .. vocab - 1 marks a token that is not scored: loss 0.
  *

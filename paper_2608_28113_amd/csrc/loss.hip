@@ -6,7 +6,8 @@
 //
 // The loss takes one pass of matrix products whose tiles end as a maximum and
 // a sum of exponentials per token; the gradient computes the logits again, a
-// piece of the vocabulary at a time, and only that piece of g is held.
+// piece of the vocabulary at a time, and only that piece of g is held.  Of few
+// tokens and words the logits go through memory, so that k can be split.
 //
 // g meets the products as bf16.  A weight like 1 / n that is rounded with it
 // errs alike in all tokens' terms, which no sum evens out.  So the largest
