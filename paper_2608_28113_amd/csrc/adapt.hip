@@ -128,16 +128,17 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
 }
 
 // Eight checkpointed values restored: bf16(fp32(q s)).  A byte becomes a float
-// in one operation if it is unsigned, and (q + 128) s - 128 s in one fma rounds
-// to the same fp32(q s), as 128 s is exact.
+// in one operation if it is unsigned; (q + 128) - 128 is exact, and the product
+// is rounded once.  (One fma of (q + 128) s and -128 s saves an operation, but
+// 128 s passes fp32's range where a block's largest magnitude is one of bf16's
+// two largest.)
 __device__ __forceinline__ u32x4 restore8(uint32_t lo, uint32_t hi, float s) {
-    const float less = -128.0f * s;
     u32x4 r;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t w = (k < 2 ? lo : hi) ^ 0x80808080u;
-        r[k] = bf16_pair(fmaf((float)(w >> (16 * (k & 1)) & 0xFF), s, less),
-                         fmaf((float)(w >> (16 * (k & 1) + 8) & 0xFF), s, less));
+        r[k] = bf16_pair(((float)(w >> (16 * (k & 1)) & 0xFF) - 128.0f) * s,
+                         ((float)(w >> (16 * (k & 1) + 8) & 0xFF) - 128.0f) * s);
     }
     return r;
 }
