@@ -562,9 +562,8 @@ size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t
  * that hscale_token_loss wrote: with
  *   g[t, v] = weight[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),
  * dX = g W and dW = g^T X.  The logits are computed again, a piece of the
- * vocabulary at a time; g is rounded for the two products, relative to the
- * largest weight, to bf16 (to two bf16 parts for up to 64 tokens), and their
- * sums are fp32.  Tokens that are not scored (target or weight 0) get dX = 0
+ * vocabulary at a time; g, relative to the largest weight, enters the two
+ * products in two bf16 parts (16 bits), and their sums are fp32.  Tokens that are not scored (target or weight 0) get dX = 0
  * and add nothing to dW, whatever their X and lse hold.
  *
  * weight     fp32 [tokens]: d(total) / d(loss[t]); 1 / n for a mean over n

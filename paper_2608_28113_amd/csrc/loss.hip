@@ -9,16 +9,16 @@
 // piece of the vocabulary at a time, and only that piece of g is held.  Of few
 // tokens and words the logits go through memory, so that k can be split.
 //
-// g meets the products as bf16.  A weight like 1 / n that is rounded with it
-// errs alike in all tokens' terms, which no sum evens out.  So the largest
-// weight c stays out, and equal weights are exact:
+// g meets the products as two bf16 parts, the second what the rounding of the
+// first left: within 2^-17 of it.  In one part its rounding errs alike in all of
+// a row's terms wherever the softmax is not spread thin, by up to 0.4 of what
+// the one rounding of dX and dW to bf16 errs.  Both parts multiply the same W
+// and X, one after the other into the same sums, which is twice the matrix work
+// of the two products.  The largest weight c stays out of the parts, whose
+// range then does not depend on it:
 //
-//   h_tv = weight_t / c (exp(l_tv - lse_t) - [v = target]), rounded,
+//   h_tv = weight_t / c (exp(l_tv - lse_t) - [v = target]), in two parts,
 //   dX = c (h W),  dW = c (h^T X).
-//
-// For up to 64 tokens h is kept as two bf16 parts: a gradient of few terms is
-// not averaged over many roundings, and twice 64 rows fill no more than the
-// smallest tile.
 
 #include "matmul.h"
 
@@ -58,9 +58,8 @@ struct LogitArgs {
     int64_t v0, vocab;       // of the whole
     const float *lse;
     const float *factor;     // [tokens]: weight_t / c, 0 if not scored
-    uint16_t *g;             // [tokens, ldg]; the second parts follow
+    uint16_t *g;             // [2, tokens, ldg]: the parts
     int64_t ldg;
-    bool two;
 };
 
 // A tile of words x tokens, reduced over its words where it lies: per token a
@@ -249,8 +248,6 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(
             }
     }
     store_bf16<T>(acc, lds, a.g, a.ldg, m0, a.ldg, n0, a.X.rows, true);
-    if constexpr (T::kBN > 128) return;  // up to 64 tokens: a narrower tile is taken
-    if (!a.two) return;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < T::kNJ; ++j)
@@ -314,7 +311,7 @@ __device__ __forceinline__ float factor_of(int64_t y, float w, int64_t vocab, fl
 __global__ __launch_bounds__(256) void slope_rows(const float4 *__restrict__ sum, int splits, int64_t tokens,
                                                   int64_t words, int64_t vocab, const int64_t *__restrict__ target,
                                                   const float *__restrict__ lse, const float *__restrict__ factor,
-                                                  uint2 *__restrict__ g, bool two) {
+                                                  uint2 *__restrict__ g) {
     const int64_t row = words / 4, fours = tokens * row, stride = (int64_t)gridDim.x * 256;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
         const int64_t t = id / row, v0 = (id - t * row) * 4, y = target[t];
@@ -328,18 +325,49 @@ __global__ __launch_bounds__(256) void slope_rows(const float4 *__restrict__ sum
         }
         const uint2 r = make_uint2(bf16_pair(h[0], h[1]), bf16_pair(h[2], h[3]));
         g[id] = r;
-        if (two)
-            g[fours + id] = make_uint2(bf16_pair(h[0] - low_half(r.x), h[1] - high_half(r.x)),
-                                       bf16_pair(h[2] - low_half(r.y), h[3] - high_half(r.y)));
+        g[fours + id] = make_uint2(bf16_pair(h[0] - low_half(r.x), h[1] - high_half(r.x)),
+                                   bf16_pair(h[2] - low_half(r.y), h[3] - high_half(r.y)));
     }
 }
 
+// The stages of the second part of g, which lies behind the first: the same k
+// of P again.
+template <class T, Layout LP, Layout LQ>
+struct SecondPart {
+    static constexpr bool kAny = true;
+    using SP = Stage<LP, T::kBM, T::kWaves, T::kK>;
+    using SQ = Stage<LQ, T::kBN, T::kWaves, T::kK>;
+    int stages;
+
+    const Operand &P;
+    Operand Q;
+    int64_t m0, n0, k0, k1;
+    bool begun = false;
+
+    __device__ __forceinline__ SecondPart(const Operand &p, int64_t m, const Operand &q, int64_t part, int64_t n,
+                                          int64_t from, int64_t to)
+        : stages((int)((to - from + T::kK - 1) / T::kK)), P(p), Q(q), m0(m), n0(n), k0(from), k1(to) {
+        Q.p = static_cast<const uint16_t *>(q.p) + part;
+    }
+    __device__ __forceinline__ void set(SP &sp, SQ &sq, bool some) {
+        if (!some) {  // stages past the last
+            sp.left = sq.left = 0;
+            return;
+        }
+        if (begun) return;
+        begun = true;
+        const Place<T> at;
+        sp.init(P, m0, k0, k1, at.wm + at.wn * T::kWM, at.lane);
+        sq.init(Q, n0, k0, k1, at.wm + at.wn * T::kWM, at.lane);
+    }
+};
+
 struct DxArgs {
-    Operand W, g;    // W [vocab piece, d] across, g [parts of tokens, piece]
+    Operand W, g;    // W [vocab piece, d] across, g [2, tokens, piece]
     unsigned mtiles, tiles;
     int64_t k_split;
     bool add;
-    float *sum;      // [splits, parts of tokens, d]
+    float *sum;      // [splits, tokens, d]
 };
 
 template <class T>
@@ -352,19 +380,21 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dx_kernel(con
     const int64_t k0 = split * a.k_split, k1 = k0 + a.k_split < a.g.k ? k0 + a.k_split : a.g.k;
     Acc<T> acc;
     acc.clear();
-    if (k0 < k1) tile_product<T, Across, Along>(acc, lds, a.W, m0, a.g, n0, k0, k1);  // a last piece may have fewer splits
+    if (k0 < k1)  // a last piece may have fewer splits
+        tile_product<T, Across, Along>(acc, lds, a.W, m0, a.g, n0, k0, k1,
+                                       SecondPart<T, Across, Along>(a.W, m0, a.g, a.g.rows * a.g.ld, n0, k0, k1));
     store_sum<T>(acc, a.sum + split * a.g.rows * a.W.rows, m0, a.W.rows, n0, a.g.rows, true, a.add);
 }
 
-// Adds the splits, and the parts of a token, and rounds.
-__global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int parts, int64_t fours,
+// Adds the splits and rounds.
+__global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__ sum, int splits, int64_t fours,
                                                       int64_t d, const float *__restrict__ most,
                                                       uint16_t *__restrict__ dX, int64_t lddx) {
     const int64_t stride = (int64_t)gridDim.x * 256;
     const float c = largest(most);
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < fours; id += stride) {
         float4 v = sum[id];
-        for (int s = 1; s < parts; ++s) {
+        for (int s = 1; s < splits; ++s) {
             const float4 o = sum[(int64_t)s * fours + id];
             v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
         }
@@ -375,15 +405,15 @@ __global__ __launch_bounds__(256) void loss_dx_finish(const float4 *__restrict__
 }
 
 // Every token's weight / c, and X with zeros in the rows that are not scored,
-// so that what lies there does not meet the zeros of h in a product; once for
-// each part of h.  Of few tokens each block finds the largest weight itself and
-// the first leaves it in `most`, which saves a launch.
+// so that what lies there does not meet the zeros of h in a product.  Of few
+// tokens each block finds the largest weight itself and the first leaves it in
+// `most`, which saves a launch.
 template <bool few>
 __global__ __launch_bounds__(256) void scored_rows(const uint16_t *__restrict__ X, int64_t ldx, int64_t tokens,
                                                    int64_t d, const int64_t *__restrict__ target,
                                                    const float *__restrict__ weight, int64_t vocab,
                                                    float *__restrict__ most, float *__restrict__ factor,
-                                                   u32x4 *__restrict__ S, int parts) {
+                                                   u32x4 *__restrict__ S) {
     const int64_t stride = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
     float c;
     if constexpr (few) {
@@ -401,7 +431,7 @@ __global__ __launch_bounds__(256) void scored_rows(const uint16_t *__restrict__ 
         const int64_t y = target[t];
         u32x4 v = {0, 0, 0, 0};
         if (y >= 0 && y < vocab && weight[t] != 0.0f) v = *reinterpret_cast<const u32x4 *>(X + t * ldx + k * 8);
-        for (int p = 0; p < parts; ++p) S[p * total + id] = v;
+        S[id] = v;
     }
 }
 
@@ -411,7 +441,7 @@ __global__ __launch_bounds__(256) void clear_kernel(uint2 *__restrict__ p, int64
 }
 
 struct DwArgs {
-    Operand X, g;    // X [parts of tokens, d] across, g [parts of tokens, piece] across
+    Operand X, g;    // X [tokens, d] across, g [2, tokens, piece] across
     const float *most;
     unsigned mtiles;
     int64_t cols;    // rows of dW in this piece
@@ -427,7 +457,8 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
     const int64_t m0 = (int64_t)mt * T::kBM, n0 = (int64_t)nt * T::kBN;
     Acc<T> acc;
     acc.clear();
-    tile_product<T, Across, Across>(acc, lds, a.X, m0, a.g, n0, 0, a.g.k);
+    tile_product<T, Across, Across>(acc, lds, a.X, m0, a.g, n0, 0, a.g.k,
+                                    SecondPart<T, Across, Across>(a.X, m0, a.g, a.g.k * a.g.ld, n0, 0, a.g.k));
     float c = a.most[threadIdx.x & 63];
     for (int i = 64; i < kMost; i += 64) c = fmaxf(c, a.most[i + (threadIdx.x & 63)]);
 #pragma unroll
@@ -489,20 +520,18 @@ LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     return p;
 }
 
-// A piece of g takes up to 512 MB, and at least 2048 of the vocabulary: so that
-// a piece's products fill the chip many times over, and its sums in dX, read and
-// written once a piece, stay below a fiftieth of them.
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+// Both parts of a piece of g take up to 384 MB, and at least 2048 of the
+// vocabulary: so that a piece's products fill the chip many times over, and its
+// sums in dX, read and written once a piece, stay below a twentieth of them.
+constexpr int64_t kPieceBytes = (int64_t)384 << 20;
 constexpr int64_t kLeastPiece = 2048;
 constexpr int64_t kPieceStep = 256;
 // Tokens whose weights each block of scored_rows reads for itself.  384 tokens
 // of 1024 over 8192 words, whole gradient and loss: 76.7 us so, 80.0 with a
 // launch before it; 2048 tokens of 4096: 19 us so, 13 in two launches.
 constexpr int64_t kFewWeights = 512;
-constexpr int64_t kTwoParts = 64;  // tokens up to which h is kept as two parts
 
 struct LossGradPlan {
-    int64_t parts;  // of h
     int64_t piece, pieces;
     Split dx, logits;  // logits: of a single piece, whose k may be split
     size_t g, sum, rows, factor, total;
@@ -510,19 +539,19 @@ struct LossGradPlan {
 
 LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     LossGradPlan p;
-    p.parts = tokens <= kTwoParts ? 2 : 1;
-    const int64_t rows = p.parts * tokens;
-    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (2 * rows) / kPieceStep * kPieceStep);
+    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (4 * tokens) / kPieceStep * kPieceStep);
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    p.dx = split_plan(d, rows, p.piece, true);
+    p.dx = split_plan(d, tokens, 2 * p.piece, true);  // both parts
+    p.dx.k = cdiv(cdiv(p.piece, p.dx.splits), 64) * 64;
+    p.dx.splits = (int)cdiv(p.piece, p.dx.k);
     p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
-    p.g = round_up((size_t)rows * p.piece * 2, 256);
-    p.sum = round_up((size_t)p.dx.splits * rows * d * 4, 256);
+    p.g = round_up((size_t)tokens * p.piece * 4, 256);
+    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
     if (p.logits.splits > 1)  // in turn
         p.sum = std::max(p.sum, round_up((size_t)p.logits.splits * tokens * p.piece * 4, 256));
-    p.rows = dw ? round_up((size_t)rows * d * 2, 256) : 0;
+    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
     p.factor = round_up((size_t)tokens * sizeof(float), 256);
     p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
     return p;
@@ -638,8 +667,7 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         if (const int st = launch_status()) return st;
     }
     hipLaunchKernelGGL(tokens > kFewWeights ? scored_rows<false> : scored_rows<true>, dim3(grid_for(dW ? tokens * d / 8 : tokens, 256)), dim3(256), 0, stream,
-                       static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, most, factor, rows,
-                       (int)p.parts);
+                       static_cast<const uint16_t *>(X), ldx, tokens, d, target, weight, vocab, most, factor, rows);
     if (const int st = launch_status()) return st;
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t cols = std::min(p.piece, vocab - v0), ldg = cdiv(cols, kPieceStep) * kPieceStep;
@@ -648,7 +676,7 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             if (const int st = logit_sums(X, tokens, d, ldx, W, vocab, ldg, p.logits, sum, stream)) return st;
             hipLaunchKernelGGL(slope_rows, dim3(grid_for(tokens * ldg / 4, 256)), dim3(256), 0, stream,
                                reinterpret_cast<const float4 *>(sum), p.logits.splits, tokens, ldg, vocab, target, lse,
-                               factor, reinterpret_cast<uint2 *>(g), p.parts == 2);
+                               factor, reinterpret_cast<uint2 *>(g));
             if (const int st = launch_status()) return st;
         } else {
             LogitArgs a{};
@@ -659,11 +687,9 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             a.vocab = vocab;
             a.lse = lse;
             a.factor = factor;
-            a.two = p.parts == 2;
             a.g = g;
             a.ldg = ldg;
-            Split logits = split_plan(ldg, tokens, d, false);
-            if (a.two && logits.size == kLarge) logits.size = kMiddle;
+            const Split logits = split_plan(ldg, tokens, d, false);
             a.mtiles = (unsigned)(ldg / logits.side_m());
             LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
             if (const int st = launch_status()) return st;
@@ -671,9 +697,9 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         if (dX) {
             DxArgs x{};
             x.W = Operand{Wp, d, d, cols};
-            x.g = Operand{g, ldg, p.parts * tokens, ldg};
+            x.g = Operand{g, ldg, tokens, ldg};
             x.mtiles = (unsigned)cdiv(d, p.dx.side_m());
-            x.tiles = (unsigned)p.dx.units(d, p.parts * tokens);
+            x.tiles = (unsigned)p.dx.units(d, tokens);
             x.k_split = p.dx.k;
             x.add = v0 > 0;
             x.sum = sum;
@@ -682,10 +708,10 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         }
         if (dW) {
             DwArgs b{};
-            b.X = Operand{rows, d, d, p.parts * tokens};
-            b.g = Operand{g, ldg, ldg, p.parts * tokens};
+            b.X = Operand{rows, d, d, tokens};
+            b.g = Operand{g, ldg, ldg, tokens};
             b.most = most;
-            const Split rows_of = split_plan(d, cols, p.parts * tokens, false);
+            const Split rows_of = split_plan(d, cols, 2 * tokens, false);
             b.mtiles = (unsigned)cdiv(d, rows_of.side_m());
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;
@@ -697,7 +723,7 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
     if (dX) {
         const int64_t fours = tokens * d / 4;
         hipLaunchKernelGGL(loss_dx_finish, dim3(grid_for(fours, 256)), dim3(256), 0, stream,
-                           reinterpret_cast<const float4 *>(sum), p.dx.splits * (int)p.parts, fours, d, most,
+                           reinterpret_cast<const float4 *>(sum), p.dx.splits, fours, d, most,
                            static_cast<uint16_t *>(dX), lddx);
         return launch_status();
     }
