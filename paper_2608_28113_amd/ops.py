@@ -34,6 +34,37 @@ def _stream(stream, device) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _elsewhere(stream, device):
+    """`stream` as a torch stream if it is another than `device`'s current one, else None."""
+    if stream is None or device.type != "cuda":
+        return None
+    handle = _stream(stream, device)
+    if handle == torch._C._cuda_getCurrentRawStream(device.index):
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
+def _new(shape, dtype, device, stream, zeros=False, scratch=False) -> torch.Tensor:
+    """A new tensor of a call on `stream`.  The allocator hands memory out again
+    in the order of the stream that it was allocated on, so memory of a call on
+    another stream than the current one is allocated on that one: nothing that
+    pends on the current stream still uses it, and scratch that is dropped when
+    the call returns is not given to the current stream while the call runs.
+    What is returned is recorded on the current stream too, where the caller
+    will use and drop it."""
+    make = torch.zeros if zeros else torch.empty
+    side = _elsewhere(stream, device)
+    if side is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        t = make(shape, dtype=dtype, device=device)
+    if not scratch:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _call(device, fn, *args) -> int:
     """Calls the library with `device` current, so that its launches go to
     the device that holds the operands."""
@@ -61,20 +92,21 @@ def _tensor(t, name: str, dtype, shape, device) -> torch.Tensor:
     return t
 
 
-def _out(t, name: str, dtype, shape, device) -> torch.Tensor:
-    """A caller-provided output (checked) or a new one."""
+def _out(t, name: str, dtype, shape, device, stream) -> torch.Tensor:
+    """A caller-provided output (checked) or a new one of a call on `stream`."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _new(shape, dtype, device, stream)
     return _tensor(t, name, dtype, shape, device)
 
 
-def _workspace(ws, need: int, device) -> tuple[int, int]:
+def _workspace(ws, need: int, device, stream) -> tuple[int, int]:
     """(pointer, bytes) of a caller-provided scratch tensor (any dtype,
-    contiguous, on `device`) or of a new one; the library checks the size."""
+    contiguous, on `device`) or of a new one of a call on `stream`; the library
+    checks the size."""
     if ws is None:
         if need <= 0:
             return 0, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws = _new((need,), torch.uint8, device, stream, scratch=True)
     elif not isinstance(ws, torch.Tensor) or ws.device != device or not ws.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
     return ws.data_ptr(), ws.numel() * ws.element_size()
@@ -123,8 +155,8 @@ def hdiag(X: torch.Tensor, h: torch.Tensor | None = None, workspace: torch.Tenso
     _bf16_matrix(X, "X")
     T, n = X.shape
     dev = X.device
-    h = _out(h, "h", torch.float32, (n,), dev)
-    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev)
+    h = _out(h, "h", torch.float32, (n,), dev, stream)
+    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
     _check(_call(dev, _lib.hscale_hdiag, X.data_ptr(), T, n, h.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_hdiag")
     return h
@@ -160,8 +192,8 @@ def search(W: torch.Tensor, h: torch.Tensor, global_scale: float, window: int | 
     _tensor(h, "h", torch.float32, (n,), dev)
     down, up = _window(window, down, up)
     mode, init_t = _init_mode(init, (m, n // 16), dev)
-    scale_codes = _out(scale_codes, "scale_codes", torch.uint8, (m, n // 16), dev)
-    packed_e2m1 = _out(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), dev)
+    scale_codes = _out(scale_codes, "scale_codes", torch.uint8, (m, n // 16), dev, stream)
+    packed_e2m1 = _out(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), dev, stream)
     s = _stream(stream, dev)
     if mode == _lib.HSCALE_INIT_MAXABS:
         st = _call(dev, _lib.hscale_search_du, W.data_ptr(), m, n, h.data_ptr(), down, up, float(global_scale),
@@ -214,8 +246,8 @@ def search_layers(layers, window: int | None = None, down: int | None = None, up
         m, n = W.shape
         _tensor(h, f"h of layer {k}", torch.float32, (n,), dev)
         codes, packed = (None, None) if outputs is None else outputs[k]
-        codes = _out(codes, f"scale_codes of layer {k}", torch.uint8, (m, n // 16), dev)
-        packed = _out(packed, f"packed_e2m1 of layer {k}", torch.uint8, (m, n // 2), dev)
+        codes = _out(codes, f"scale_codes of layer {k}", torch.uint8, (m, n // 16), dev, stream)
+        packed = _out(packed, f"packed_e2m1 of layer {k}", torch.uint8, (m, n // 2), dev, stream)
         iptr = 0
         if given is not None:
             iptr = _tensor(given[k], f"initial codes of layer {k}", torch.uint8, (m, n // 16), dev).data_ptr()
@@ -261,7 +293,7 @@ def hdiag_accumulate(X: torch.Tensor, h64: torch.Tensor, workspace: torch.Tensor
     T, n = X.shape
     dev = X.device
     _tensor(h64, "h64", torch.float64, (n,), dev)
-    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev)
+    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
     _check(_call(dev, _lib.hscale_hdiag_accumulate, X.data_ptr(), T, n, h64.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_hdiag_accumulate")
     return h64
@@ -274,7 +306,7 @@ def hdiag_finalize(h64: torch.Tensor, h: torch.Tensor | None = None, stream=None
     n = h64.shape[0]
     dev = h64.device
     _tensor(h64, "h64", torch.float64, (n,), dev)
-    h = _out(h, "h", torch.float32, (n,), dev)
+    h = _out(h, "h", torch.float32, (n,), dev, stream)
     _check(_call(dev, _lib.hscale_hdiag_finalize, h64.data_ptr(), n, h.data_ptr(),
                  _stream(stream, dev)), "hscale_hdiag_finalize")
     return h
@@ -287,7 +319,7 @@ def quantize(W: torch.Tensor, global_scale: float, scale_codes: torch.Tensor,
     m, n = W.shape
     dev = W.device
     _tensor(scale_codes, "scale_codes", torch.uint8, (m, n // 16), dev)
-    packed_e2m1 = _out(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), dev)
+    packed_e2m1 = _out(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), dev, stream)
     _check(_call(dev, _lib.hscale_quantize, W.data_ptr(), m, n, float(global_scale), scale_codes.data_ptr(),
                  packed_e2m1.data_ptr(), _stream(stream, dev)), "hscale_quantize")
     return packed_e2m1
@@ -305,11 +337,11 @@ def search_stats(W: torch.Tensor, h: torch.Tensor, global_scale: float, down: in
     _tensor(h, "h", torch.float32, (n,), dev)
     G = (m, n // 16)
     mode, init_t = _init_mode(init, G, dev)
-    out = dict(scale_codes=torch.empty(G, dtype=torch.uint8, device=dev),
-               packed_e2m1=torch.empty((m, n // 2), dtype=torch.uint8, device=dev),
-               shift=torch.empty(G, dtype=torch.int8, device=dev),
-               err_best=torch.empty(G, dtype=torch.float32, device=dev),
-               err_init=torch.empty(G, dtype=torch.float32, device=dev))
+    out = dict(scale_codes=_new(G, torch.uint8, dev, stream),
+               packed_e2m1=_new((m, n // 2), torch.uint8, dev, stream),
+               shift=_new(G, torch.int8, dev, stream),
+               err_best=_new(G, torch.float32, dev, stream),
+               err_init=_new(G, torch.float32, dev, stream))
     st = _call(dev, _lib.hscale_search_stats, W.data_ptr(), m, n, h.data_ptr(), int(down), int(up),
                float(global_scale), mode, init_t.data_ptr() if init_t is not None else 0,
                out["scale_codes"].data_ptr(), out["packed_e2m1"].data_ptr(), out["shift"].data_ptr(),
@@ -334,12 +366,10 @@ def shift_summary(shift: torch.Tensor, err_best: torch.Tensor, err_init: torch.T
             raise ValueError(f"{name} must be a contiguous {dt} tensor on {dev} with one entry per group")
     K = int(down) + int(up) + 1
     # counts are uint64 in the C ABI; int64 holds them (< 2^63) with full torch support
-    out = dict(count=torch.empty(K, dtype=torch.int64, device=dev),
-               sum_init=torch.empty(K, dtype=torch.float64, device=dev),
-               sum_best=torch.empty(K, dtype=torch.float64, device=dev),
-               sum_rel=torch.empty(K, dtype=torch.float64, device=dev))
+    out = dict(count=_new((K,), torch.int64, dev, stream), sum_init=_new((K,), torch.float64, dev, stream),
+               sum_best=_new((K,), torch.float64, dev, stream), sum_rel=_new((K,), torch.float64, dev, stream))
     need = _lib.hscale_shift_summary_workspace_bytes(groups, int(down), int(up))
-    ws = torch.empty(max(need, 8), dtype=torch.uint8, device=dev)
+    ws = _new((max(need, 8),), torch.uint8, dev, stream, scratch=True)
     st = _call(dev, _lib.hscale_shift_summary, shift.data_ptr(), err_best.data_ptr(), err_init.data_ptr(), groups,
                int(down), int(up), out["count"].data_ptr(), out["sum_init"].data_ptr(), out["sum_best"].data_ptr(),
                out["sum_rel"].data_ptr(), ws.data_ptr(), need, _stream(stream, dev))
@@ -370,16 +400,16 @@ def output_error(X: torch.Tensor, W: torch.Tensor, global_scale: float, scale_co
     _tensor(scale_codes, "scale_codes", torch.uint8, (m, n // 16), dev)
     _tensor(packed_e2m1, "packed_e2m1", torch.uint8, (m, n // 2), dev)
     if row_err is None:
-        row_err = torch.zeros(m, dtype=torch.float64, device=dev)
+        row_err = _new((m,), torch.float64, dev, stream, zeros=True)
     _tensor(row_err, "row_err", torch.float64, (m,), dev)
     need = output_error_workspace_bytes(T, n, m)
     try:
-        ws_ptr, ws_bytes = _workspace(workspace, need, dev)
+        ws_ptr, ws_bytes = _workspace(workspace, need, dev, stream)
     except torch.OutOfMemoryError:
         least = _lib.hscale_output_error_least_workspace_bytes(T, n, m)
         if least == need:
             raise
-        ws_ptr, ws_bytes = _workspace(None, least, dev)
+        ws_ptr, ws_bytes = _workspace(None, least, dev, stream)
     _check(_call(dev, _lib.hscale_output_error, X.data_ptr(), T, n, W.data_ptr(), m, float(global_scale),
                  scale_codes.data_ptr(), packed_e2m1.data_ptr(), row_err.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_output_error")
@@ -404,10 +434,10 @@ def _rows_in(t, name: str) -> int:
     return row if rows > 1 else cols
 
 
-def _rows_out(t, name: str, shape, device) -> tuple[torch.Tensor, int]:
+def _rows_out(t, name: str, shape, device, stream) -> tuple[torch.Tensor, int]:
     """A caller-provided bf16 view of rows (checked) or a new tensor, and its row stride."""
     if t is None:
-        return torch.empty(shape, dtype=torch.bfloat16, device=device), shape[1]
+        return _new(shape, torch.bfloat16, device, stream), shape[1]
     return t, _row_view(t, torch.bfloat16, shape, device, name)
 
 
@@ -466,9 +496,9 @@ def adapted_linear(X: torch.Tensor, global_scale: float, scale_codes: torch.Tens
     dev = X.device
     m = _stored(scale_codes, packed_e2m1, n, dev)
     ad = _adapters(A, B, alpha, adapter, T, n, m, dev)
-    Y, ldy = _rows_out(Y, "Y", (T, m), dev)
+    Y, ldy = _rows_out(Y, "Y", (T, m), dev, stream)
     need = adapted_linear_workspace_bytes(T, n, m, *(ad[:2] if ad else (0, 0)))
-    ws_ptr, ws_bytes = _workspace(workspace, need, dev)
+    ws_ptr, ws_bytes = _workspace(workspace, need, dev, stream)
     _check(_call(dev, _lib.hscale_adapted_linear, X.data_ptr(), T, n, ldx, m, float(global_scale),
                  scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad, Y.data_ptr(), ldy, ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_adapted_linear")
@@ -481,8 +511,8 @@ def pack_activations(X: torch.Tensor, q: torch.Tensor | None = None, scale: torc
     ldx = _rows_in(X, "X")
     T, n = X.shape
     dev = X.device
-    q = _out(q, "q", torch.int8, (T, n), dev)
-    scale = _out(scale, "scale", torch.float32, (T, -(-n // CHECKPOINT_BLOCK)), dev)
+    q = _out(q, "q", torch.int8, (T, n), dev, stream)
+    scale = _out(scale, "scale", torch.float32, (T, -(-n // CHECKPOINT_BLOCK)), dev, stream)
     _check(_call(dev, _lib.hscale_pack_activations, X.data_ptr(), T, n, ldx, q.data_ptr(), scale.data_ptr(),
                  _stream(stream, dev)), "hscale_pack_activations")
     return q, scale
@@ -501,7 +531,7 @@ def unpack_activations(q: torch.Tensor, scale: torch.Tensor, X: torch.Tensor | N
     """The bf16 [tokens, in] values that a checkpoint stands for."""
     T, n = _checkpoint(q, scale)
     dev = q.device
-    X, ldx = _rows_out(X, "X", (T, n), dev)
+    X, ldx = _rows_out(X, "X", (T, n), dev, stream)
     _check(_call(dev, _lib.hscale_unpack_activations, q.data_ptr(), scale.data_ptr(), T, n, X.data_ptr(), ldx,
                  _stream(stream, dev)), "hscale_unpack_activations")
     return X
@@ -536,10 +566,10 @@ def adapted_linear_grad(dY: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, 
         raise ValueError("A and B are required")
     if not need_dX and dX is not None:
         raise ValueError("dX given although need_dX is False")
-    dX, lddx = _rows_out(dX, "dX", (T, n), dev) if need_dX else (None, n)
-    dA = _out(dA, "dA", torch.bfloat16, A.shape, dev)
-    dB = _out(dB, "dB", torch.bfloat16, B.shape, dev)
-    ws_ptr, ws_bytes = _workspace(workspace, adapted_linear_grad_workspace_bytes(T, n, m, *ad[:2]), dev)
+    dX, lddx = _rows_out(dX, "dX", (T, n), dev, stream) if need_dX else (None, n)
+    dA = _out(dA, "dA", torch.bfloat16, A.shape, dev, stream)
+    dB = _out(dB, "dB", torch.bfloat16, B.shape, dev, stream)
+    ws_ptr, ws_bytes = _workspace(workspace, adapted_linear_grad_workspace_bytes(T, n, m, *ad[:2]), dev, stream)
     _check(_call(dev, _lib.hscale_adapted_linear_grad, dY.data_ptr(), T, m, lddy, q.data_ptr(), scale.data_ptr(), n,
                  float(global_scale), scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad,
                  0 if dX is None else dX.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr(), ws_ptr, ws_bytes,
@@ -569,9 +599,9 @@ def token_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: tor
     T, d = X.shape
     dev = X.device
     _head(X, W, target)
-    loss = _out(loss, "loss", torch.float32, (T,), dev)
-    lse = _out(lse, "lse", torch.float32, (T,), dev)
-    ws_ptr, ws_bytes = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev)
+    loss = _out(loss, "loss", torch.float32, (T,), dev, stream)
+    lse = _out(lse, "lse", torch.float32, (T,), dev, stream)
+    ws_ptr, ws_bytes = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev, stream)
     _check(_call(dev, _lib.hscale_token_loss, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0], target.data_ptr(),
                  loss.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)), "hscale_token_loss")
     return loss, lse
@@ -596,9 +626,9 @@ def token_loss_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse:
     _tensor(weight, "weight", torch.float32, (T,), dev)
     if (not need_dX and dX is not None) or (not need_dW and dW is not None):
         raise ValueError("an output was given that is not needed")
-    dX, lddx = _rows_out(dX, "dX", (T, d), dev) if need_dX else (None, d)
-    dW = _out(dW, "dW", torch.bfloat16, tuple(W.shape), dev) if need_dW else None
-    ws_ptr, ws_bytes = _workspace(workspace, token_loss_grad_workspace_bytes(T, d, W.shape[0]), dev)
+    dX, lddx = _rows_out(dX, "dX", (T, d), dev, stream) if need_dX else (None, d)
+    dW = _out(dW, "dW", torch.bfloat16, tuple(W.shape), dev, stream) if need_dW else None
+    ws_ptr, ws_bytes = _workspace(workspace, token_loss_grad_workspace_bytes(T, d, W.shape[0]), dev, stream)
     _check(_call(dev, _lib.hscale_token_loss_grad, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0],
                  target.data_ptr(), lse.data_ptr(), weight.data_ptr(), 0 if dX is None else dX.data_ptr(), lddx,
                  0 if dW is None else dW.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)),
