@@ -99,17 +99,18 @@ def _out(t, name: str, dtype, shape, device, stream) -> torch.Tensor:
     return _tensor(t, name, dtype, shape, device)
 
 
-def _workspace(ws, need: int, device, stream) -> tuple[int, int]:
-    """(pointer, bytes) of a caller-provided scratch tensor (any dtype,
+def _workspace(ws, need: int, device, stream) -> tuple[int, int, torch.Tensor | None]:
+    """(pointer, bytes, tensor) of a caller-provided scratch tensor (any dtype,
     contiguous, on `device`) or of a new one of a call on `stream`; the library
-    checks the size."""
+    checks the size.  The caller holds the tensor until its launches are queued,
+    so that no other thread is given the memory before them."""
     if ws is None:
         if need <= 0:
-            return 0, 0
+            return 0, 0, None
         ws = _new((need,), torch.uint8, device, stream, scratch=True)
     elif not isinstance(ws, torch.Tensor) or ws.device != device or not ws.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
 def _row_view(t, dtype, shape, device, name: str) -> int:
@@ -156,7 +157,7 @@ def hdiag(X: torch.Tensor, h: torch.Tensor | None = None, workspace: torch.Tenso
     T, n = X.shape
     dev = X.device
     h = _out(h, "h", torch.float32, (n,), dev, stream)
-    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
     _check(_call(dev, _lib.hscale_hdiag, X.data_ptr(), T, n, h.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_hdiag")
     return h
@@ -293,7 +294,7 @@ def hdiag_accumulate(X: torch.Tensor, h64: torch.Tensor, workspace: torch.Tensor
     T, n = X.shape
     dev = X.device
     _tensor(h64, "h64", torch.float64, (n,), dev)
-    ws_ptr, ws_bytes = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, hdiag_workspace_bytes(T, n), dev, stream)
     _check(_call(dev, _lib.hscale_hdiag_accumulate, X.data_ptr(), T, n, h64.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_hdiag_accumulate")
     return h64
@@ -404,12 +405,12 @@ def output_error(X: torch.Tensor, W: torch.Tensor, global_scale: float, scale_co
     _tensor(row_err, "row_err", torch.float64, (m,), dev)
     need = output_error_workspace_bytes(T, n, m)
     try:
-        ws_ptr, ws_bytes = _workspace(workspace, need, dev, stream)
+        ws_ptr, ws_bytes, held = _workspace(workspace, need, dev, stream)
     except torch.OutOfMemoryError:
         least = _lib.hscale_output_error_least_workspace_bytes(T, n, m)
         if least == need:
             raise
-        ws_ptr, ws_bytes = _workspace(None, least, dev, stream)
+        ws_ptr, ws_bytes, held = _workspace(None, least, dev, stream)
     _check(_call(dev, _lib.hscale_output_error, X.data_ptr(), T, n, W.data_ptr(), m, float(global_scale),
                  scale_codes.data_ptr(), packed_e2m1.data_ptr(), row_err.data_ptr(), ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_output_error")
@@ -498,7 +499,7 @@ def adapted_linear(X: torch.Tensor, global_scale: float, scale_codes: torch.Tens
     ad = _adapters(A, B, alpha, adapter, T, n, m, dev)
     Y, ldy = _rows_out(Y, "Y", (T, m), dev, stream)
     need = adapted_linear_workspace_bytes(T, n, m, *(ad[:2] if ad else (0, 0)))
-    ws_ptr, ws_bytes = _workspace(workspace, need, dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, need, dev, stream)
     _check(_call(dev, _lib.hscale_adapted_linear, X.data_ptr(), T, n, ldx, m, float(global_scale),
                  scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad, Y.data_ptr(), ldy, ws_ptr, ws_bytes,
                  _stream(stream, dev)), "hscale_adapted_linear")
@@ -569,7 +570,7 @@ def adapted_linear_grad(dY: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, 
     dX, lddx = _rows_out(dX, "dX", (T, n), dev, stream) if need_dX else (None, n)
     dA = _out(dA, "dA", torch.bfloat16, A.shape, dev, stream)
     dB = _out(dB, "dB", torch.bfloat16, B.shape, dev, stream)
-    ws_ptr, ws_bytes = _workspace(workspace, adapted_linear_grad_workspace_bytes(T, n, m, *ad[:2]), dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, adapted_linear_grad_workspace_bytes(T, n, m, *ad[:2]), dev, stream)
     _check(_call(dev, _lib.hscale_adapted_linear_grad, dY.data_ptr(), T, m, lddy, q.data_ptr(), scale.data_ptr(), n,
                  float(global_scale), scale_codes.data_ptr(), packed_e2m1.data_ptr(), ad,
                  0 if dX is None else dX.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr(), ws_ptr, ws_bytes,
@@ -601,7 +602,7 @@ def token_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: tor
     _head(X, W, target)
     loss = _out(loss, "loss", torch.float32, (T,), dev, stream)
     lse = _out(lse, "lse", torch.float32, (T,), dev, stream)
-    ws_ptr, ws_bytes = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev, stream)
     _check(_call(dev, _lib.hscale_token_loss, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0], target.data_ptr(),
                  loss.data_ptr(), lse.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)), "hscale_token_loss")
     return loss, lse
@@ -628,7 +629,7 @@ def token_loss_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse:
         raise ValueError("an output was given that is not needed")
     dX, lddx = _rows_out(dX, "dX", (T, d), dev, stream) if need_dX else (None, d)
     dW = _out(dW, "dW", torch.bfloat16, tuple(W.shape), dev, stream) if need_dW else None
-    ws_ptr, ws_bytes = _workspace(workspace, token_loss_grad_workspace_bytes(T, d, W.shape[0]), dev, stream)
+    ws_ptr, ws_bytes, held = _workspace(workspace, token_loss_grad_workspace_bytes(T, d, W.shape[0]), dev, stream)
     _check(_call(dev, _lib.hscale_token_loss_grad, X.data_ptr(), T, d, ldx, W.data_ptr(), W.shape[0],
                  target.data_ptr(), lse.data_ptr(), weight.data_ptr(), 0 if dX is None else dX.data_ptr(), lddx,
                  0 if dW is None else dW.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)),

@@ -5,11 +5,13 @@ the stream it was allocated on: outputs and scratch of a call on a side stream
 that came from the current stream's pool could still be in use there, and
 scratch would go back to it while the call runs."""
 import contextlib
+import gc
+import weakref
 
 import pytest
 import torch
 
-from paper_2608_28113_amd import ops
+from paper_2608_28113_amd import _lib, ops
 from tests.test_adapt_abi import CASES as ADAPT
 from tests.test_front_end import CASES as BASE
 from tests.test_front_end import Reached, fake_gpu  # noqa: F401
@@ -87,6 +89,30 @@ def test_new_memory_belongs_to_the_stream_of_the_call(allocations, fn):
 def test_on_the_current_stream_nothing_is_recorded(allocations, fn):
     _call(fn, allocations, None)
     assert all(under is HERE and recorded is None for _, under, recorded in allocations)
+
+
+@pytest.mark.parametrize("fn", ["hdiag", "output_error", "adapted_linear", "adapted_linear_grad", "token_loss",
+                                "token_loss_grad"])
+def test_scratch_lives_until_the_library_was_called(fake_gpu, monkeypatch, fn):  # noqa: F811
+    """Freed before, it could be given to another thread ahead of the launches."""
+    f, given = _arguments(fn)
+    scratch, empty = [], torch.empty
+
+    def watch(*shape, **kw):
+        t = empty(*shape, **kw)
+        if t.dtype is torch.uint8 and t.dim() == 1:
+            scratch.append(weakref.ref(t))
+        return t
+
+    def reached(*args):
+        gc.collect()
+        assert scratch and all(r() is not None for r in scratch)
+        raise Reached
+
+    monkeypatch.setattr(torch, "empty", watch)
+    monkeypatch.setattr(_lib, f"hscale_{fn}", reached)
+    with pytest.raises(Reached):
+        f(**given, stream=0)
 
 
 def test_a_stream_is_another_one_by_its_handle(monkeypatch):
