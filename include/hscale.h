@@ -539,6 +539,7 @@ size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t voca
  * partial sums of theirs in the workspace):
  *   lse[t] = log sum_v exp(l[t, v]),  loss[t] = lse[t] - l[t, target[t]]
  * A target outside 0 .. vocab - 1 marks a token that is not scored: loss 0.
+ * A word whose logit is -inf adds nothing to the sum; a NaN makes it NaN.
  *
  * X          bf16 [tokens, d], rows ldx <= 2^21 apart, 16-byte aligned rows
  * W          bf16 [vocab, d], 16-byte aligned: the output head
@@ -565,6 +566,8 @@ size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t
  * vocabulary at a time; g, relative to the largest weight, enters the two
  * products in two bf16 parts (16 bits), and their sums are fp32.  Tokens that are not scored (target or weight 0) get dX = 0
  * and add nothing to dW, whatever their X and lse hold.
+ *
+ * W is finite (g of a word is 0 at least once, and 0 times what is not is NaN).
  *
  * weight     fp32 [tokens]: d(total) / d(loss[t]); 1 / n for a mean over n
  * dX         bf16 [tokens, d], rows lddx apart (8-byte aligned rows); NULL:

@@ -96,12 +96,13 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_tile_kernel(c
                 if (k == own) hit = acc.v[i][j][e];
             }
         if (own >= 0 && (own & 4) == 0 && own < 32 * T::kMI) a.at[t] = hit;  // the one lane that holds it
+        const float base = p.x == -INFINITY ? 0.0f : p.x;  // logits of -inf alone add nothing
 #pragma unroll
         for (int i = 0; i < T::kMI; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int k = 32 * i + 8 * (e >> 2) + (e & 3);
-                if (k < words - first) p.y += exp_of(acc.v[i][j][e] - p.x);
+                if (k < words - first) p.y += exp_of(acc.v[i][j][e] - base);
             }
         const float2 o = make_float2(__shfl_xor(p.x, 32, 64), __shfl_xor(p.y, 32, 64));
         p = join(p, o);
