@@ -198,8 +198,6 @@ __global__ __launch_bounds__(256) void unpack_kernel(const uint2 *__restrict__ q
 // Down to the rank: p[t, j] = sum_k z[t, k] A_a[j, k]
 // ---------------------------------------------------------------------------
 
-constexpr int kLowStep = 256;  // k of a split: a multiple of it
-
 // Activations as bf16 rows, or as a checkpoint.
 struct Rows {
     const void *p;       // bf16 [tokens, width] at ld, or int8 [tokens, width]
@@ -542,8 +540,6 @@ __global__ __launch_bounds__(256) void layer_finish(const float *__restrict__ su
 // block, of which each of 8 waves takes an eighth, and one adapter: the nth,
 // in the order of the 32 tokens, that they have.  All of a wave's loads are
 // under way at once.
-constexpr int kFewLowK = 1024;
-
 struct FewLowArgs {
     const uint16_t *X;
     int64_t tokens, ldx, in;
@@ -613,8 +609,6 @@ __device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t 
 // (33 MB of weights, 8 of 24 us by HBM; VALU 0.20 busy, half the time waiting);
 // 515 of 14336 -> 4096 in 104 us, 0.58 PFLOP/s: MFMA 0.31, LDS 0.31, VALU 0.33
 // busy, which two blocks' waves overlap only in part.
-constexpr int kFewK = 512, kFewRows = 128;  // a split is a multiple of kFewK
-
 struct FewArgs {
     const uint8_t *codes;
     const uint8_t *packed;
@@ -907,8 +901,6 @@ struct OuterArgs {
     float by;
 };
 
-constexpr int kOuterCols = 256, kOuterTokens = 64, kOuterThreads = 512;
-
 // 256 columns x 32 kRT ranks of one adapter x one split of the tokens.  Stages
 // of 64 tokens through LDS, laid out as Stage<Across>; the next stage's rows
 // are under way to registers while one multiplies.  Tokens of other adapters
@@ -919,7 +911,7 @@ constexpr int kOuterCols = 256, kOuterTokens = 64, kOuterThreads = 512;
 // blocks that have tokens of their adapter are not many more than run at once,
 // and the longest last.  Sharing out the stages evenly cost more than that (121
 // and 78 us: every block then visits every part of the tokens).
-constexpr int kOuterMasks = 256;
+constexpr int kOuterMasks = 256, kOuterThreads = 512;
 
 // Four bf16 values to where they may not be aligned together.
 __device__ __forceinline__ void store_four(uint16_t *dst, uint32_t lo, uint32_t hi) {
@@ -1140,54 +1132,6 @@ __global__ __launch_bounds__(256) void widen_kernel(const uint16_t *__restrict__
 // Host side
 // ---------------------------------------------------------------------------
 
-
-constexpr int kTargetBlocks = 1024;
-
-// Up to 1024 tokens the stored weights go straight into the product; above,
-// they are converted once and multiplied in tiles.  That way (and the other),
-// us: 512 tokens of 4096 -> 14336 75 (151); 1040 of 4096 -> 14336 153 (161),
-// of 14336 -> 4096 191 (169), of 4096 -> 4096 71 (65), of 4096 -> 1024 27 (29);
-// 2040 of 4096 -> 14336 274 (243).
-constexpr int64_t kFewTokens = 1024;
-// Up to 64 tokens a block takes them all, in sixteens, and the adapters' part
-// is computed beside the product and added at its end (fused); above, a block
-// takes 128, and that is done while tokens x outputs x rank are few.  64 and 80 tokens of
-// 4096 -> 14336 with eight adapters of rank 16: 27 and 38 us, of 4096 -> 1024
-// 11.5 and 13; reading B per token, as the end does, grows with tokens and
-// outputs, where the product's own stages read it once per 128 tokens.
-constexpr int64_t kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
-
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
-inline int low_pad(int rank) { return (rank + 15) / 16 * 16; }
-
-struct Low {
-    int64_t k_split;
-    int splits, slots;
-};
-
-// Ranks that a block of the product down to the rank takes.
-inline int rank_tile(int rank) { return rank <= 32 ? 32 : 64; }
-
-// Splits of k for the product down to the rank: as many as fill the chip, of
-// at least 512 k.
-inline Low low_plan(int64_t tokens, int64_t width, int count, int rank) {
-    Low p;
-    const int64_t blocks = cdiv(tokens, 128) * cdiv(rank, rank_tile(rank));
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kTargetBlocks / blocks, cdiv(width, 2 * kLowStep)));
-    p.k_split = cdiv(cdiv(width, want), kLowStep) * kLowStep;
-    p.splits = (int)cdiv(width, p.k_split);
-    // a slot more costs blocks that find no adapter; few tiles leave room for them
-    p.slots = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(count, 8), 2 * kTargetBlocks / (blocks * p.splits)));
-    return p;
-}
-
-inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
-    return round_up((size_t)p.splits * tokens * rank_pad(rank) * 4, 256);
-}
-
-inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * low_pad(rank) * 2, 256); }
-
 struct Adapters {
     int count, rank;
     const uint16_t *A, *B;
@@ -1223,10 +1167,6 @@ int shrink_to_low(const Rows &z, int64_t tokens, int64_t width, const uint16_t *
     return launch_status();
 }
 
-inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
-    return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
-}
-
 int sum_of_splits(const float *sum, int splits, int64_t tokens, int64_t m, float scale, uint16_t *Y, int64_t ldy,
                   hipStream_t stream) {
     for (int64_t t = 0; t < tokens; t += 65535) {  // as many rows has a grid
@@ -1252,38 +1192,6 @@ int layer(LayerArgs a, const Split &p, float *sum, hipStream_t stream) {
     return p.splits > 1 ? sum_of_splits(sum, p.splits, n, m, a.scale, a.Y, a.ldy, stream) : HSCALE_OK;
 }
 
-struct FewPlan {
-    int64_t k_split;
-    int splits, low_splits, low_slots;
-    bool fused;  // the adapters' part beside the weights' and in the end, not before and with them
-    int tile;    // tokens a block, in sixteens
-};
-
-// The splits of k of the least estimated time in us: rounds of one or two
-// blocks a CU, 256 k of a block in 1.2 to 2.4 us by its tokens (128 tokens
-// 2.3, measured at 512 tokens, 4096 -> 14336), partial sums at 5 TB/s.
-inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
-    FewPlan p;
-    p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
-    p.fused = tokens <= kFewTile ||
-              (count > 0 && tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork);
-    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
-    double least = 0.0;
-    for (int64_t s = 1; s <= 32 && s <= cdiv(in, kFewK); ++s) {
-        const int64_t k = cdiv(cdiv(in, s), kFewK) * kFewK, n = cdiv(in, k);
-        const double each = p.tile > 4 ? 2.3 : 0.9 + 0.35 * p.tile;
-        const double us = cdiv(blocks * n, slots) * (k / 256 * each + 2.0) +
-                          (n > 1 || p.fused ? 3.0 + n * tokens * out * 8 / 5.0e6 : 0.0);
-        if (s > 1 && us >= least) continue;
-        least = us;
-        p.k_split = k;
-        p.splits = (int)n;
-    }
-    p.low_splits = (int)cdiv(in, kFewLowK);
-    p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
-    return p;
-}
-
 bool sizes_ok(int64_t tokens, int64_t in, int64_t out) {
     return tokens >= 0 && tokens <= kMaxTokens && in >= 0 && in % kGroup == 0 && in <= kMaxWidth && out >= 0 &&
            out <= kMaxWidth;
@@ -1291,81 +1199,6 @@ bool sizes_ok(int64_t tokens, int64_t in, int64_t out) {
 
 bool adapters_ok(int32_t count, int32_t rank) {
     return count >= 0 && count <= kMaxAdapters && (count == 0 || (rank >= 8 && rank <= kMaxRank && rank % 8 == 0));
-}
-
-struct LinearPlan {
-    bool few;
-    FewPlan base;
-    Low low;
-    Split tile;
-    size_t weights, partial, low_partial, low_parts, total;
-};
-
-LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
-    LinearPlan p{};
-    p.few = tokens <= kFewTokens;
-    if (p.few) {
-        p.base = few_plan(tokens, in, out, count, rank);
-        if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
-    } else {
-        p.weights = round_up((size_t)out * in * 2, 256);
-        p.tile = split_plan(out, tokens, in, true);
-        p.partial = sum_bytes(p.tile, out, tokens);
-    }
-    if (count > 0 && p.few && p.base.fused) {
-        p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
-    } else if (count > 0) {
-        p.low = low_plan(tokens, in, count, rank);
-        p.low_partial = low_partial_bytes(p.low, tokens, rank);
-        p.low_parts = low_bytes(tokens, rank);
-    }
-    p.total = p.weights + p.partial + p.low_partial + p.low_parts;
-    return p;
-}
-
-struct GradPlan {
-    int64_t width;  // columns of dY as the kernels read it
-    bool widen;
-    Low v, u;
-    int64_t split_a, split_b;
-    int splits_a, splits_b;
-    Split tile;
-    size_t weights, dy, turned, low_partial, low, outer, total;
-};
-
-// Splits of the tokens for the adapters' gradients.
-// Up to 512 tokens are not split, which saves the partial sums and the kernels
-// that add them: 500 tokens of 1024 -> 4096, eight adapters of rank 32, 70 us
-// so and 79 in two splits; 512 of 8192 -> 1024, one of rank 64, 83 and 82.
-constexpr int64_t kOuterWhole = 512;
-
-inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
-    const int64_t blocks = cdiv(width, kOuterCols) * cdiv(rank, rank_tile(rank)) * count;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cdiv(kTargetBlocks, blocks), tokens <= kOuterWhole ? 1 : cdiv(tokens, 256)));
-    split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
-    splits = (int)cdiv(tokens, split);
-}
-
-GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank, bool widen) {
-    GradPlan p{};
-    p.width = cdiv(out, 16) * 16;
-    p.widen = widen;
-    p.weights = round_up((size_t)out * in * 2, 256);
-    p.dy = widen ? round_up((size_t)tokens * p.width * 2, 256) : 0;
-    p.turned = round_up((size_t)count * rank * p.width * 2, 256);
-    p.v = low_plan(tokens, p.width, count, rank);
-    p.u = low_plan(tokens, in, count, rank);
-    p.low_partial = std::max(low_partial_bytes(p.v, tokens, rank), low_partial_bytes(p.u, tokens, rank));
-    p.low = low_bytes(tokens, rank);
-    outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
-    outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
-    const size_t cols_a = p.splits_a > 1 ? (size_t)p.splits_a * in : 0;
-    const size_t cols_b = p.splits_b > 1 ? (size_t)p.splits_b * p.width : 0;
-    p.outer = round_up(std::max(cols_a, cols_b) * count * rank * 4, 256);
-    p.tile = split_plan(in, tokens, p.width, true);
-    p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
-    p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
-    return p;
 }
 
 // dY is read as it lies when its rows are whole 16-byte words of whole groups.
@@ -1390,22 +1223,6 @@ int check_adapters(const hscale_adapters *w, Adapters &ad) {
 inline void split_scale(float s, float &f, int &e) {
     f = 2.0f * std::frexp(s, &e);
     --e;
-}
-
-struct Range {
-    const void *p;
-    size_t n;
-};
-
-// Whether one of the written ranges meets a read one or another written one.
-bool any_overlap(const Range *w, int nw, const Range *r, int nr) {
-    for (int i = 0; i < nw; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (overlaps(w[i].p, w[i].n, w[j].p, w[j].n)) return true;
-        for (int j = 0; j < nr; ++j)
-            if (overlaps(w[i].p, w[i].n, r[j].p, r[j].n)) return true;
-    }
-    return false;
 }
 
 int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, int e, void *W,

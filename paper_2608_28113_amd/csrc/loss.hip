@@ -263,9 +263,6 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(
     store_bf16<T>(acc, lds, a.g + a.X.rows * a.ldg, a.ldg, m0, a.ldg, n0, a.X.rows, true);
 }
 
-// The largest finite |weight| of the scored tokens, a part of it per block.
-constexpr int kMost = 256;
-
 __device__ __forceinline__ float block_max(float v, float *red) {
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o, 64));
@@ -276,6 +273,7 @@ __device__ __forceinline__ float block_max(float v, float *red) {
     return v;
 }
 
+// The largest finite |weight| of the scored tokens, kMost parts of it.
 __device__ __forceinline__ float scored_most(const int64_t *target, const float *weight, int64_t first, int64_t tokens,
                                              int64_t step, int64_t vocab) {
     __shared__ float red[4];
@@ -306,8 +304,6 @@ __device__ __forceinline__ float factor_of(int64_t y, float w, int64_t vocab, fl
     return y < 0 || y >= vocab ? 0.0f : w / c;
 }
 
-// dX and dW of such a piece: 1.59 and 1.64 ms, 1.35 and 1.31 PFLOP/s at MFMA
-// 0.72 busy and 1.77 GHz, where a library product of that size reaches 1.39.
 // h from the logits' partial sums, four words a thread.
 __global__ __launch_bounds__(256) void slope_rows(const float4 *__restrict__ sum, int splits, int64_t tokens,
                                                   int64_t words, int64_t vocab, const int64_t *__restrict__ target,
@@ -471,25 +467,11 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_dw_kernel(con
 // Host side
 // ---------------------------------------------------------------------------
 
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 #define loss_tile_kernel_of(T) loss_tile_kernel<T>
 #define logit_sum_kernel_of(T) logit_sum_kernel<T>
 #define loss_slope_kernel_of(T) loss_slope_kernel<T>
 #define loss_dx_kernel_of(T) loss_dx_kernel<T>
 #define loss_dw_kernel_of(T) loss_dw_kernel<T>
-
-// k is split where 128 x 128 tiles leave half the chip without one.  Loss of 20
-// tokens of 8192 over 500 words: 18 us so, 66 in one pass; of 300 over 2000: 29
-// and 67; at 250 tiles (64 tokens of 4096 over 32000 words) both take 68.
-Split logit_plan(int64_t words, int64_t tokens, int64_t d, bool one_piece) {
-    return split_plan(words, tokens, d, one_piece && cdiv(words, 128) * cdiv(tokens, 128) <= kCUs / 2);
-}
-
-struct LossPlan {
-    Split tile;
-    size_t parts, at, total;  // parts: partial sums, if split
-};
 
 // The logits' partial sums of `words` (a multiple of 4).
 int logit_sums(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab, int64_t words,
@@ -506,76 +488,14 @@ int logit_sums(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void
     return launch_status();
 }
 
-LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
-    LossPlan p;
-    const int64_t words = cdiv(vocab, 4) * 4;
-    p.tile = logit_plan(words, tokens, d, true);
-    if (p.tile.splits > 1) {
-        p.parts = p.total = round_up((size_t)p.tile.splits * tokens * words * 4, 256);
-        p.at = 0;
-        return p;
-    }
-    p.parts = round_up((size_t)cdiv(vocab, p.tile.side_m()) * tokens * sizeof(float2), 256);
-    p.at = round_up((size_t)tokens * 4, 256);
-    p.total = p.parts + p.at;
-    return p;
-}
-
-// Both parts of a piece of g take up to 384 MB, and at least 2048 of the
-// vocabulary: so that a piece's products fill the chip many times over, and its
-// sums in dX, read and written once a piece, stay below a twentieth of them.
-constexpr int64_t kPieceBytes = (int64_t)384 << 20;
-constexpr int64_t kLeastPiece = 2048;
-constexpr int64_t kPieceStep = 256;
 // Tokens whose weights each block of scored_rows reads for itself.  384 tokens
 // of 1024 over 8192 words, whole gradient and loss: 76.7 us so, 80.0 with a
 // launch before it; 2048 tokens of 4096: 19 us so, 13 in two launches.
 constexpr int64_t kFewWeights = 512;
 
-struct LossGradPlan {
-    int64_t piece, pieces;
-    Split dx, logits;  // logits: of a single piece, whose k may be split
-    size_t g, sum, rows, factor, total;
-};
-
-LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
-    LossGradPlan p;
-    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (4 * tokens) / kPieceStep * kPieceStep);
-    p.pieces = cdiv(vocab, fit);
-    p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
-    p.pieces = cdiv(vocab, p.piece);
-    p.dx = split_plan(d, tokens, 2 * p.piece, true);  // both parts
-    p.dx.k = cdiv(cdiv(p.piece, p.dx.splits), 64) * 64;
-    p.dx.splits = (int)cdiv(p.piece, p.dx.k);
-    p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
-    p.g = round_up((size_t)tokens * p.piece * 4, 256);
-    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
-    if (p.logits.splits > 1)  // in turn
-        p.sum = std::max(p.sum, round_up((size_t)p.logits.splits * tokens * p.piece * 4, 256));
-    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
-    p.factor = round_up((size_t)tokens * sizeof(float), 256);
-    p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
-    return p;
-}
-
 bool loss_sizes_ok(int64_t tokens, int64_t d, int64_t vocab) {
     return tokens >= 0 && tokens <= kMaxTokens && d >= 0 && d % 16 == 0 && d <= kMaxWidth && vocab >= 0 &&
            vocab <= kMaxVocab && tokens * vocab <= kMaxLogits;
-}
-
-struct Range {
-    const void *p;
-    size_t n;
-};
-
-bool any_overlap(const Range *w, int nw, const Range *r, int nr) {
-    for (int i = 0; i < nw; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (overlaps(w[i].p, w[i].n, w[j].p, w[j].n)) return true;
-        for (int j = 0; j < nr; ++j)
-            if (overlaps(w[i].p, w[i].n, r[j].p, r[j].n)) return true;
-    }
-    return false;
 }
 
 }  // namespace

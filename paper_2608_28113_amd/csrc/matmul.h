@@ -11,6 +11,7 @@
 #pragma once
 
 #include "common.h"
+#include "plan.h"
 
 namespace {
 
@@ -207,55 +208,6 @@ typedef Tile<2, 2, 4, 4, 64, 2, 2> Large;        // 256 x 256
 typedef Tile<2, 2, 4, 2, 64, 3, 2> Middle;       // 256 x 128
 typedef Tile<2, 2, 2, 2, 64, 4, 2> Small;        // 128 x 128: its ring hides latency where blocks are few
 typedef Tile<2, 4, 4, 2, 32, 4, 2> LargeAcross;  // 256 x 256 for two operands across, in eight waves: four run out of registers
-constexpr int kCUs = 256;
-
-// A product in tiles of one size and splits of k, whose partial sums are
-// written and read again.
-enum Size { kLarge, kMiddle, kSmall };
-struct Split {
-    Size size;
-    int64_t k;   // of a split, a multiple of 64
-    int splits;
-    int64_t side_m() const { return size == kSmall ? 128 : 256; }
-    int64_t side_n() const { return size == kLarge ? 256 : 128; }
-    int64_t units(int64_t m, int64_t n) const {
-        return (m + side_m() - 1) / side_m() * ((n + side_n() - 1) / side_n());
-    }
-};
-
-// Estimated time of it in us: rounds of up to 256 blocks, each with its start
-// and end and its stages of 64 k.  A stage takes 1.2 to 1.6 us in the large
-// tile, 0.75 to 1.0 in the middle one and 0.5 to 0.6 in the small one, by how
-// many of the CUs share the L2s (measured at 1024 x 1024 to 8192 x 8192, 4096
-// deep); sums go at 5 TB/s.
-inline double split_us(int64_t m, int64_t n, int64_t k, const Split &p) {
-    const int64_t units = p.units(m, n) * p.splits;
-    const double full = units < kCUs ? (double)units / kCUs : 1.0;
-    const double stage = p.size == kLarge ? 1.2 + 0.4 * full : p.size == kMiddle ? 0.75 + 0.25 * full
-                                                                                 : 0.5 + 0.1 * full;
-    const double stages = (double)(((k + 63) / 64 + p.splits - 1) / p.splits);
-    return (units + kCUs - 1) / kCUs * (stages * stage + 3.0) + 3.0 +
-           (p.splits > 1 ? 3.0 + p.splits * m * n * 8 / 5.0e6 : 0.0);
-}
-
-// The tile and, if it may, the splits of at least 256 k of the least estimated time.
-inline Split split_plan(int64_t m, int64_t n, int64_t k, bool may_split) {
-    Split least{kLarge, k, 1};
-    double best = split_us(m, n, k, least);
-    for (int size = kLarge; size <= kSmall; ++size)
-        for (int64_t s = 1; s == 1 || (may_split && s <= 32 && (k + s - 1) / s >= 256); ++s) {
-            const Split p{(Size)size, (k + s - 1) / s, (int)s};
-            const double us = split_us(m, n, k, p);
-            if (us < best) {
-                best = us;
-                least = p;
-            }
-        }
-    least.k = (least.k + 63) / 64 * 64;
-    least.splits = (int)((k + least.k - 1) / least.k);
-    return least;
-}
-
 // Launches KERNEL(tile) in the plan's tile.
 #define LAUNCH_TILES(KERNEL, LARGE, size, blocks, stream, ...)                                                    \
     do {                                                                                                          \

@@ -1,0 +1,294 @@
+// How the operators of a stored layer in use (adapt.hip, loss.hip) are split
+// into tiles, splits and launches, and the workspaces that takes: host code
+// that goes by sizes alone.
+//
+// Times beside the rules are of one MI355X.
+#pragma once
+
+#include "host.h"
+
+namespace {
+
+constexpr int kCUs = 256;
+
+// A product in tiles of one size and splits of k, whose partial sums are
+// written and read again.
+enum Size { kLarge, kMiddle, kSmall };
+struct Split {
+    Size size;
+    int64_t k;   // of a split, a multiple of 64
+    int splits;
+    int64_t side_m() const { return size == kSmall ? 128 : 256; }
+    int64_t side_n() const { return size == kLarge ? 256 : 128; }
+    int64_t units(int64_t m, int64_t n) const {
+        return (m + side_m() - 1) / side_m() * ((n + side_n() - 1) / side_n());
+    }
+};
+
+// Estimated time of it in us: rounds of up to 256 blocks, each with its start
+// and end and its stages of 64 k.  A stage takes 1.2 to 1.6 us in the large
+// tile, 0.75 to 1.0 in the middle one and 0.5 to 0.6 in the small one, by how
+// many of the CUs share the L2s (measured at 1024 x 1024 to 8192 x 8192, 4096
+// deep); sums go at 5 TB/s.
+inline double split_us(int64_t m, int64_t n, int64_t k, const Split &p) {
+    const int64_t units = p.units(m, n) * p.splits;
+    const double full = units < kCUs ? (double)units / kCUs : 1.0;
+    const double stage = p.size == kLarge ? 1.2 + 0.4 * full : p.size == kMiddle ? 0.75 + 0.25 * full
+                                                                                 : 0.5 + 0.1 * full;
+    const double stages = (double)(((k + 63) / 64 + p.splits - 1) / p.splits);
+    return (units + kCUs - 1) / kCUs * (stages * stage + 3.0) + 3.0 +
+           (p.splits > 1 ? 3.0 + p.splits * m * n * 8 / 5.0e6 : 0.0);
+}
+
+// The tile and, if it may, the splits of at least 256 k of the least estimated time.
+inline Split split_plan(int64_t m, int64_t n, int64_t k, bool may_split) {
+    Split least{kLarge, k, 1};
+    double best = split_us(m, n, k, least);
+    for (int size = kLarge; size <= kSmall; ++size)
+        for (int64_t s = 1; s == 1 || (may_split && s <= 32 && (k + s - 1) / s >= 256); ++s) {
+            const Split p{(Size)size, (k + s - 1) / s, (int)s};
+            const double us = split_us(m, n, k, p);
+            if (us < best) {
+                best = us;
+                least = p;
+            }
+        }
+    least.k = (least.k + 63) / 64 * 64;
+    least.splits = (int)((k + least.k - 1) / least.k);
+    return least;
+}
+
+inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
+    return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
+}
+
+// ---------------------------------------------------------------------------
+// The layer and its adapters
+// ---------------------------------------------------------------------------
+
+constexpr int kLowStep = 256;                   // down to the rank: k of a split is a multiple of it
+constexpr int kFewLowK = 1024;                  // k of a block of it for few tokens
+constexpr int kFewK = 512, kFewRows = 128;      // few tokens: a split is a multiple of kFewK, output rows of a block
+constexpr int kOuterCols = 256, kOuterTokens = 64;  // gradients of the adapters: columns of a block, tokens of a stage
+constexpr int kTargetBlocks = 1024;
+
+// Up to 1024 tokens the stored weights go straight into the product; above,
+// they are converted once and multiplied in tiles.  That way (and the other),
+// us: 512 tokens of 4096 -> 14336 75 (151); 1040 of 4096 -> 14336 153 (161),
+// of 14336 -> 4096 191 (169), of 4096 -> 4096 71 (65), of 4096 -> 1024 27 (29);
+// 2040 of 4096 -> 14336 274 (243).
+constexpr int64_t kFewTokens = 1024;
+// Up to 64 tokens a block takes them all, in sixteens, and the adapters' part
+// is computed beside the product and added at its end (fused); above, a block
+// takes 128, and that is done while tokens x outputs x rank are few.  64 and 80
+// tokens of 4096 -> 14336 with eight adapters of rank 16: 27 and 38 us, of
+// 4096 -> 1024 11.5 and 13; reading B per token, as the end does, grows with
+// tokens and outputs, where the product's own stages read it once per 128
+// tokens.
+constexpr int64_t kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
+
+inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
+inline int low_pad(int rank) { return (rank + 15) / 16 * 16; }
+
+struct Low {
+    int64_t k_split;
+    int splits, slots;
+};
+
+// Ranks that a block of the product down to the rank takes.
+inline int rank_tile(int rank) { return rank <= 32 ? 32 : 64; }
+
+// Splits of k for the product down to the rank: as many as fill the chip, of
+// at least 512 k.
+inline Low low_plan(int64_t tokens, int64_t width, int count, int rank) {
+    Low p;
+    const int64_t blocks = cdiv(tokens, 128) * cdiv(rank, rank_tile(rank));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kTargetBlocks / blocks, cdiv(width, 2 * kLowStep)));
+    p.k_split = cdiv(cdiv(width, want), kLowStep) * kLowStep;
+    p.splits = (int)cdiv(width, p.k_split);
+    // a slot more costs blocks that find no adapter; few tiles leave room for them
+    p.slots = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(count, 8), 2 * kTargetBlocks / (blocks * p.splits)));
+    return p;
+}
+
+inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
+    return round_up((size_t)p.splits * tokens * rank_pad(rank) * 4, 256);
+}
+
+inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * low_pad(rank) * 2, 256); }
+
+struct FewPlan {
+    int64_t k_split;
+    int splits, low_splits, low_slots;
+    bool fused;  // the adapters' part beside the weights' and in the end, not before and with them
+    int tile;    // tokens a block, in sixteens
+};
+
+// The splits of k of the least estimated time in us: rounds of one or two
+// blocks a CU, 256 k of a block in 1.2 to 2.4 us by its tokens (128 tokens
+// 2.3, measured at 512 tokens, 4096 -> 14336), partial sums at 5 TB/s.
+inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
+    FewPlan p;
+    p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
+    p.fused = tokens <= kFewTile ||
+              (count > 0 && tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork);
+    const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
+    double least = 0.0;
+    for (int64_t s = 1; s <= 32 && s <= cdiv(in, kFewK); ++s) {
+        const int64_t k = cdiv(cdiv(in, s), kFewK) * kFewK, n = cdiv(in, k);
+        const double each = p.tile > 4 ? 2.3 : 0.9 + 0.35 * p.tile;
+        const double us = cdiv(blocks * n, slots) * (k / 256 * each + 2.0) +
+                          (n > 1 || p.fused ? 3.0 + n * tokens * out * 8 / 5.0e6 : 0.0);
+        if (s > 1 && us >= least) continue;
+        least = us;
+        p.k_split = k;
+        p.splits = (int)n;
+    }
+    p.low_splits = (int)cdiv(in, kFewLowK);
+    p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
+    return p;
+}
+
+struct LinearPlan {
+    bool few;
+    FewPlan base;
+    Low low;
+    Split tile;
+    size_t weights, partial, low_partial, low_parts, total;
+};
+
+inline LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
+    LinearPlan p{};
+    p.few = tokens <= kFewTokens;
+    if (p.few) {
+        p.base = few_plan(tokens, in, out, count, rank);
+        if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
+    } else {
+        p.weights = round_up((size_t)out * in * 2, 256);
+        p.tile = split_plan(out, tokens, in, true);
+        p.partial = sum_bytes(p.tile, out, tokens);
+    }
+    if (count > 0 && p.few && p.base.fused) {
+        p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
+    } else if (count > 0) {
+        p.low = low_plan(tokens, in, count, rank);
+        p.low_partial = low_partial_bytes(p.low, tokens, rank);
+        p.low_parts = low_bytes(tokens, rank);
+    }
+    p.total = p.weights + p.partial + p.low_partial + p.low_parts;
+    return p;
+}
+
+struct GradPlan {
+    int64_t width;  // columns of dY as the kernels read it
+    bool widen;
+    Low v, u;
+    int64_t split_a, split_b;
+    int splits_a, splits_b;
+    Split tile;
+    size_t weights, dy, turned, low_partial, low, outer, total;
+};
+
+// Up to 512 tokens are not split for the adapters' gradients, which saves the
+// partial sums and the kernels that add them: 500 tokens of 1024 -> 4096, eight
+// adapters of rank 32, 70 us so and 79 in two splits; 512 of 8192 -> 1024, one
+// of rank 64, 83 and 82.
+constexpr int64_t kOuterWhole = 512;
+
+// Splits of the tokens for the adapters' gradients.
+inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
+    const int64_t blocks = cdiv(width, kOuterCols) * cdiv(rank, rank_tile(rank)) * count;
+    const int64_t want = tokens <= kOuterWhole ? 1 : std::min(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256));
+    split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
+    splits = (int)cdiv(tokens, split);
+}
+
+inline GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank, bool widen) {
+    GradPlan p{};
+    p.width = cdiv(out, 16) * 16;
+    p.widen = widen;
+    p.weights = round_up((size_t)out * in * 2, 256);
+    p.dy = widen ? round_up((size_t)tokens * p.width * 2, 256) : 0;
+    p.turned = round_up((size_t)count * rank * p.width * 2, 256);
+    p.v = low_plan(tokens, p.width, count, rank);
+    p.u = low_plan(tokens, in, count, rank);
+    p.low_partial = std::max(low_partial_bytes(p.v, tokens, rank), low_partial_bytes(p.u, tokens, rank));
+    p.low = low_bytes(tokens, rank);
+    outer_plan(tokens, in, count, rank, p.split_a, p.splits_a);
+    outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
+    const size_t cols_a = p.splits_a > 1 ? (size_t)p.splits_a * in : 0;
+    const size_t cols_b = p.splits_b > 1 ? (size_t)p.splits_b * p.width : 0;
+    p.outer = round_up(std::max(cols_a, cols_b) * count * rank * 4, 256);
+    p.tile = split_plan(in, tokens, p.width, true);
+    p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
+    p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
+    return p;
+}
+
+// ---------------------------------------------------------------------------
+// The token loss and its gradient
+// ---------------------------------------------------------------------------
+
+constexpr int kMost = 256;  // parts of the largest weight
+
+// k is split where 128 x 128 tiles leave half the chip without one.  Loss of 20
+// tokens of 8192 over 500 words: 18 us so, 66 in one pass; of 300 over 2000: 29
+// and 67; at 250 tiles (64 tokens of 4096 over 32000 words) both take 68.
+inline Split logit_plan(int64_t words, int64_t tokens, int64_t d, bool one_piece) {
+    return split_plan(words, tokens, d, one_piece && cdiv(words, 128) * cdiv(tokens, 128) <= kCUs / 2);
+}
+
+struct LossPlan {
+    Split tile;
+    size_t parts, at, total;  // parts: partial sums, if split
+};
+
+inline LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
+    LossPlan p;
+    const int64_t words = cdiv(vocab, 4) * 4;
+    p.tile = logit_plan(words, tokens, d, true);
+    if (p.tile.splits > 1) {
+        p.parts = p.total = round_up((size_t)p.tile.splits * tokens * words * 4, 256);
+        p.at = 0;
+        return p;
+    }
+    p.parts = round_up((size_t)cdiv(vocab, p.tile.side_m()) * tokens * 2 * sizeof(float), 256);
+    p.at = round_up((size_t)tokens * 4, 256);
+    p.total = p.parts + p.at;
+    return p;
+}
+
+// Both parts of a piece of g take up to 384 MB, and at least 2048 of the
+// vocabulary: so that a piece's products fill the chip many times over, and its
+// sums in dX, read and written once a piece, stay below a twentieth of them.
+constexpr int64_t kPieceBytes = (int64_t)384 << 20;
+constexpr int64_t kLeastPiece = 2048;
+constexpr int64_t kPieceStep = 256;
+
+struct LossGradPlan {
+    int64_t piece, pieces;
+    Split dx, logits;  // logits: of a single piece, whose k may be split
+    size_t g, sum, rows, factor, total;
+};
+
+inline LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
+    LossGradPlan p;
+    const int64_t fit = std::max(kLeastPiece, kPieceBytes / (4 * tokens) / kPieceStep * kPieceStep);
+    p.pieces = cdiv(vocab, fit);
+    p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
+    p.pieces = cdiv(vocab, p.piece);
+    p.dx = split_plan(d, tokens, 2 * p.piece, true);  // both parts
+    p.dx.k = cdiv(cdiv(p.piece, p.dx.splits), 64) * 64;
+    p.dx.splits = (int)cdiv(p.piece, p.dx.k);
+    p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
+    p.g = round_up((size_t)tokens * p.piece * 4, 256);
+    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
+    if (p.logits.splits > 1)  // in turn
+        p.sum = std::max(p.sum, round_up((size_t)p.logits.splits * tokens * p.piece * 4, 256));
+    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
+    p.factor = round_up((size_t)tokens * sizeof(float), 256);
+    p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
+    return p;
+}
+
+}  // namespace
