@@ -848,7 +848,7 @@ struct FewFinishArgs {
     int splits;
     int64_t tokens, out;
     float f;
-    const float *low;      // [low_splits, tokens, rank_pad], NULL: no adapters
+    const float *low;      // [low_splits, tokens, rank_pad]
     int low_splits, rank, rank_pad, count;
     const uint16_t *B;     // [count, out, rank]
     const float *alpha;
@@ -861,7 +861,7 @@ struct FewFinishArgs {
 __global__ __launch_bounds__(256) void few_finish(const FewFinishArgs a) {
     __shared__ float u[kMaxRank];
     const int64_t t = blockIdx.y, m = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int id = a.low ? adapter_of(a.ids, a.count, t) : kNoAdapter;
+    const int id = adapter_of(a.ids, a.count, t);
     const int64_t plane = a.tokens * a.out, low_plane = a.tokens * a.rank_pad;
     float y = m < a.out ? sum_splits(a.partial + t * a.out + m, a.splits, plane) * a.f : 0.0f;
     if (id != kNoAdapter) {
@@ -1326,7 +1326,7 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
         a.partial = p.partial ? sum : nullptr;
         a.Y = y, a.ldy = ldy, a.wide = aligned(Y, 8) && (tokens == 1 || ldy % 4 == 0);
         a.rank = rank;
-        if (ad.count && p.base.fused) {
+        if (p.base.fused) {
             a.low = FewLowArgs{a.X, tokens, ldx, in, ad.A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, low_sum,
                                p.base.low_splits, p.base.low_slots};
             a.low_blocks = (int)cdiv(tokens, 32) * (rank_pad(ad.rank) / 32) * p.base.low_splits * p.base.low_slots;
@@ -1353,8 +1353,8 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
 #undef FEW
         if (const int st = launch_status()) return st;
         if (!p.base.fused) return p.partial ? sum_of_splits(sum, p.base.splits, tokens, out, f, y, ldy, stream) : HSCALE_OK;
-        const FewFinishArgs last{sum, p.base.splits, tokens, out, f, ad.count ? low_sum : nullptr, p.base.low_splits,
-                              ad.rank, rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
+        const FewFinishArgs last{sum, p.base.splits, tokens, out, f, low_sum, p.base.low_splits, ad.rank,
+                              rank_pad(ad.rank), ad.count, ad.B, ad.alpha, ad.ids, y, ldy};
         hipLaunchKernelGGL(few_finish, dim3((unsigned)cdiv(out, 256), (unsigned)tokens), dim3(256), 0, stream, last);
         return launch_status();
     }

@@ -130,8 +130,8 @@ struct FewPlan {
 inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
     FewPlan p;
     p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
-    p.fused = tokens <= kFewTile ||
-              (count > 0 && tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork);
+    p.fused = count > 0 &&
+              (tokens <= kFewTile || (tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork));
     const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
     double least = 0.0;
     for (int64_t s = 1; s <= 32 && s <= cdiv(in, kFewK); ++s) {
@@ -168,7 +168,7 @@ inline LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count
         p.tile = split_plan(out, tokens, in, true);
         p.partial = sum_bytes(p.tile, out, tokens);
     }
-    if (count > 0 && p.few && p.base.fused) {
+    if (p.few && p.base.fused) {
         p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
     } else if (count > 0) {
         p.low = low_plan(tokens, in, count, rank);
