@@ -443,6 +443,10 @@ int hscale_quantize(const void *W, int64_t out, int64_t in, float global_scale,
  * token: what is not finite in a row of X or dY, or in the rows of tokens
  * that are not scored, reaches no other token's result.  Adapters' weights
  * must be finite where a token of the call uses them.
+ *
+ * What a _workspace_bytes function of this part returns does not fall with the
+ * number of tokens: a workspace for the most tokens of a program serves its
+ * every call of the same widths and adapters.
  * ---------------------------------------------------------------------------
  */
 
@@ -564,8 +568,9 @@ size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t
  *   g[t, v] = weight[t] (exp(l[t, v] - lse[t]) - [v = target[t]]),
  * dX = g W and dW = g^T X.  The logits are computed again, a piece of the
  * vocabulary at a time; g, relative to the largest weight, enters the two
- * products in two bf16 parts (16 bits), and their sums are fp32.  Tokens that are not scored (target or weight 0) get dX = 0
- * and add nothing to dW, whatever their X and lse hold.
+ * products in two bf16 parts (16 bits), and their sums are fp32.  Tokens that
+ * are not scored (target or weight 0) get dX = 0 and add nothing to dW,
+ * whatever their X and lse hold.
  *
  * W is finite (g of a word is 0 at least once, and 0 times what is not is NaN).
  *

@@ -1271,7 +1271,7 @@ int hscale_unpack_activations(const int8_t *q, const float *scale, int64_t token
 
 size_t hscale_adapted_linear_workspace_bytes(int64_t tokens, int64_t in, int64_t out, int32_t count, int32_t rank) {
     if (!sizes_ok(tokens, in, out) || !adapters_ok(count, rank) || tokens == 0 || in == 0 || out == 0) return 0;
-    return linear_plan(tokens, in, out, count, rank).total;
+    return most_linear(tokens, in, out, count, rank);
 }
 
 int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx, int64_t out, float global_scale,
@@ -1285,11 +1285,12 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
     Adapters ad;
     if (const int st = check_adapters(adapters, ad)) return st;
     const LinearPlan p = linear_plan(tokens, in, out, ad.count, ad.rank);
-    if (!X || !scale_codes || !packed_e2m1 || !Y || (!workspace && p.total)) return HSCALE_ERR_NULL;
+    const size_t need = most_linear(tokens, in, out, ad.count, ad.rank);
+    if (!X || !scale_codes || !packed_e2m1 || !Y || (!workspace && need)) return HSCALE_ERR_NULL;
     if (!aligned(X, 16) || (tokens > 1 && ldx % 8 != 0) || !aligned(packed_e2m1, 8) || !aligned(Y, 2) ||
         !aligned(workspace, 256))
         return HSCALE_ERR_ALIGN;
-    if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+    if (workspace_bytes < need) return HSCALE_ERR_WORKSPACE;
     const size_t low_size = (size_t)ad.count * ad.rank * 2;
     const Range w[] = {{Y, span(tokens, ldy, out, 2)}, {workspace, p.total}};
     const Range r[] = {{X, span(tokens, ldx, in, 2)}, {scale_codes, (size_t)out * (in / kGroup)},
@@ -1374,7 +1375,7 @@ size_t hscale_adapted_linear_grad_workspace_bytes(int64_t tokens, int64_t in, in
                                                   int32_t rank) {
     if (!sizes_ok(tokens, in, out) || !adapters_ok(count, rank) || count == 0 || tokens == 0 || in == 0 || out == 0)
         return 0;
-    return grad_plan(tokens, in, out, count, rank, true).total;
+    return most_grad(tokens, in, out, count, rank, true);
 }
 
 int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int64_t lddy, const int8_t *q,
@@ -1392,13 +1393,15 @@ int hscale_adapted_linear_grad(const void *dY, int64_t tokens, int64_t out, int6
     if (!dA || !dB) return HSCALE_ERR_NULL;
     if (!aligned(dA, 2) || !aligned(dB, 2)) return HSCALE_ERR_ALIGN;
     GradPlan p{};
+    size_t need = 0;
     if (tokens > 0) {
         if (!dY || !q || !scale || !scale_codes || !packed_e2m1 || !workspace) return HSCALE_ERR_NULL;
         if (!aligned(dY, 2) || !aligned(q, 16) || !aligned(scale, 4) || !aligned(packed_e2m1, 8) || !aligned(dX, 2) ||
             !aligned(workspace, 256))
             return HSCALE_ERR_ALIGN;
         p = grad_plan(tokens, in, out, ad.count, ad.rank, needs_widening(dY, out, tokens > 1 ? lddy : 0));
-        if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+        need = most_grad(tokens, in, out, ad.count, ad.rank, p.widen);
+        if (workspace_bytes < need) return HSCALE_ERR_WORKSPACE;
     }
     const size_t low_size = (size_t)ad.count * ad.rank * 2;
     const Range w[] = {{dX, dX ? span(tokens, lddx, in, 2) : 0}, {dA, low_size * in}, {dB, low_size * out},

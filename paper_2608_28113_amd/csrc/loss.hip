@@ -504,7 +504,7 @@ extern "C" {
 
 size_t hscale_token_loss_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) {
     if (!loss_sizes_ok(tokens, d, vocab) || tokens == 0 || d == 0 || vocab == 0) return 0;
-    return loss_plan(tokens, d, vocab).total;
+    return most_loss(tokens, d, vocab);
 }
 
 int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
@@ -518,7 +518,8 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
         !aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 256))
         return HSCALE_ERR_ALIGN;
     const LossPlan p = loss_plan(tokens, d, vocab);
-    if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+    const size_t need = most_loss(tokens, d, vocab);
+    if (workspace_bytes < need) return HSCALE_ERR_WORKSPACE;
     const Range w[] = {{loss, (size_t)tokens * 4}, {lse, (size_t)tokens * 4}, {workspace, p.total}};
     const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8}};
     if (any_overlap(w, 3, r, 3)) return HSCALE_ERR_OVERLAP;
@@ -547,7 +548,7 @@ int hscale_token_loss(const void *X, int64_t tokens, int64_t d, int64_t ldx, con
 
 size_t hscale_token_loss_grad_workspace_bytes(int64_t tokens, int64_t d, int64_t vocab) {
     if (!loss_sizes_ok(tokens, d, vocab) || tokens == 0 || d == 0 || vocab == 0) return 0;
-    return loss_grad_plan(tokens, d, vocab, true).total;
+    return most_loss_grad(tokens, d, vocab, true);
 }
 
 int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void *W, int64_t vocab,
@@ -570,7 +571,8 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
         !aligned(dW, 8) || !aligned(workspace, 256))
         return HSCALE_ERR_ALIGN;
     const LossGradPlan p = loss_grad_plan(tokens, d, vocab, dW != nullptr);
-    if (workspace_bytes < p.total) return HSCALE_ERR_WORKSPACE;
+    const size_t need = most_loss_grad(tokens, d, vocab, dW != nullptr);
+    if (workspace_bytes < need) return HSCALE_ERR_WORKSPACE;
     const Range w[] = {{dX, dX ? span(tokens, lddx, d, 2) : 0}, {dW, dW ? (size_t)vocab * d * 2 : 0},
                        {workspace, p.total}};
     const Range r[] = {{X, span(tokens, ldx, d, 2)}, {W, (size_t)vocab * d * 2}, {target, (size_t)tokens * 8},
@@ -610,7 +612,7 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             a.factor = factor;
             a.g = g;
             a.ldg = ldg;
-            const Split logits = split_plan(ldg, tokens, d, false);
+            const Split logits = slope_plan(ldg, tokens, d);
             a.mtiles = (unsigned)(ldg / logits.side_m());
             LAUNCH_TILES(loss_slope_kernel_of, Large, logits.size, logits.units(ldg, tokens), stream, a);
             if (const int st = launch_status()) return st;
@@ -632,7 +634,7 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
             b.X = Operand{rows, d, d, tokens};
             b.g = Operand{g, ldg, ldg, tokens};
             b.most = most;
-            const Split rows_of = split_plan(d, cols, 2 * tokens, false);
+            const Split rows_of = dw_plan(d, cols, tokens);
             b.mtiles = (unsigned)cdiv(d, rows_of.side_m());
             b.cols = cols;
             b.dW = static_cast<uint16_t *>(dW) + v0 * d;

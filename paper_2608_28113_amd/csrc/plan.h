@@ -2,6 +2,12 @@
 // into tiles, splits and launches, and the workspaces that takes: host code
 // that goes by sizes alone.
 //
+// A plan of fewer tokens may split more and need more for its partial sums than
+// one of many.  These sums have a limit each, and what a call asks for (the
+// functions most_...) is a bound that grows with its tokens: a workspace for a
+// program's most tokens serves its every call, and each call takes the same way
+// whatever it is given.
+//
 // Times beside the rules are of one MI355X.
 #pragma once
 
@@ -40,12 +46,21 @@ inline double split_us(int64_t m, int64_t n, int64_t k, const Split &p) {
            (p.splits > 1 ? 3.0 + p.splits * m * n * 8 / 5.0e6 : 0.0);
 }
 
-// The tile and, if it may, the splits of at least 256 k of the least estimated time.
-inline Split split_plan(int64_t m, int64_t n, int64_t k, bool may_split) {
+constexpr int kMostSplits = 32;
+constexpr int64_t kLeastSplit = 256;  // k of one
+
+// Limits of partial sums: of a product in tiles, of the layer for few tokens and
+// of logits.  At 5 TB/s 256 MB take 107 us to write and read again, as long as
+// 25 stages of every block; in such tiles 256 blocks' sums are 64 MB or less.
+constexpr int64_t kTileSums = (int64_t)256 << 20, kFewSums = (int64_t)64 << 20, kLogitSums = (int64_t)32 << 20;
+
+// The tile and the splits of the least estimated time, whose sums are at most
+// `most` bytes (0: not split).
+inline Split split_plan(int64_t m, int64_t n, int64_t k, int64_t most) {
     Split least{kLarge, k, 1};
     double best = split_us(m, n, k, least);
     for (int size = kLarge; size <= kSmall; ++size)
-        for (int64_t s = 1; s == 1 || (may_split && s <= 32 && (k + s - 1) / s >= 256); ++s) {
+        for (int64_t s = 1; s == 1 || (s <= kMostSplits && cdiv(k, s) >= kLeastSplit && s * m * n * 4 <= most); ++s) {
             const Split p{(Size)size, (k + s - 1) / s, (int)s};
             const double us = split_us(m, n, k, p);
             if (us < best) {
@@ -60,6 +75,12 @@ inline Split split_plan(int64_t m, int64_t n, int64_t k, bool may_split) {
 
 inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
     return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
+}
+
+// Of split_plan(m, up to n, up to k, most).
+inline size_t most_sums(int64_t m, int64_t n, int64_t k, int64_t most) {
+    const int64_t splits = std::min<int64_t>(kMostSplits, (k - 1) / (kLeastSplit - 1));
+    return splits > 1 ? round_up((size_t)std::min(splits * m * n * 4, most), 256) : 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -115,6 +136,14 @@ inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
     return round_up((size_t)p.splits * tokens * rank_pad(rank) * 4, 256);
 }
 
+// Of low_plan for up to `tokens`: splits x tokens are at most kTargetBlocks x 128
+// over the rank's tiles, or the tokens.
+inline size_t most_low_partial(int64_t tokens, int64_t width, int rank) {
+    const int64_t rows = std::min(cdiv(width, 2 * kLowStep) * tokens,
+                                  (int64_t)kTargetBlocks * 128 / cdiv(rank, rank_tile(rank)));
+    return round_up((size_t)std::max(tokens, rows) * rank_pad(rank) * 4, 256);
+}
+
 inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * low_pad(rank) * 2, 256); }
 
 struct FewPlan {
@@ -134,8 +163,9 @@ inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int 
               (tokens <= kFewTile || (tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork));
     const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
     double least = 0.0;
-    for (int64_t s = 1; s <= 32 && s <= cdiv(in, kFewK); ++s) {
+    for (int64_t s = 1; s <= kMostSplits && s <= cdiv(in, kFewK); ++s) {
         const int64_t k = cdiv(cdiv(in, s), kFewK) * kFewK, n = cdiv(in, k);
+        if (n > 1 && n * tokens * out * 4 > kFewSums) continue;
         const double each = p.tile > 4 ? 2.3 : 0.9 + 0.35 * p.tile;
         const double us = cdiv(blocks * n, slots) * (k / 256 * each + 2.0) +
                           (n > 1 || p.fused ? 3.0 + n * tokens * out * 8 / 5.0e6 : 0.0);
@@ -165,7 +195,7 @@ inline LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count
         if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
     } else {
         p.weights = round_up((size_t)out * in * 2, 256);
-        p.tile = split_plan(out, tokens, in, true);
+        p.tile = split_plan(out, tokens, in, kTileSums);
         p.partial = sum_bytes(p.tile, out, tokens);
     }
     if (p.few && p.base.fused) {
@@ -177,6 +207,23 @@ inline LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count
     }
     p.total = p.weights + p.partial + p.low_partial + p.low_parts;
     return p;
+}
+
+// Of linear_plan for up to `tokens`.
+inline size_t most_linear(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
+    const int64_t t = std::min(tokens, kFewTokens), splits = std::min<int64_t>(kMostSplits, cdiv(in, kFewK));
+    int64_t sums = splits > 1 ? std::min(splits * t * out * 4, kFewSums) : 0;
+    size_t low = 0;
+    if (count > 0) {  // fused, k may be whole
+        sums = std::max(sums, std::max(std::min(t, kFewTile) * out, std::min(t * out, kFewFusedWork / (rank + 8))) * 4);
+        const size_t fused = (size_t)cdiv(in, kFewLowK) * std::min(t, kFewFused) * rank_pad(rank) * 4;
+        low = std::max(round_up(fused, 256), most_low_partial(t, in, rank)) + low_bytes(t, rank);
+    }
+    const size_t few = round_up((size_t)sums, 256) + low;
+    if (tokens <= kFewTokens) return few;
+    const size_t many = round_up((size_t)out * in * 2, 256) + most_sums(out, tokens, in, kTileSums) +
+                        (count > 0 ? most_low_partial(tokens, in, rank) + low_bytes(tokens, rank) : 0);
+    return std::max(few, many);
 }
 
 struct GradPlan {
@@ -195,10 +242,14 @@ struct GradPlan {
 // of rank 64, 83 and 82.
 constexpr int64_t kOuterWhole = 512;
 
-// Splits of the tokens for the adapters' gradients.
-inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
+// Splits of the tokens for the adapters' gradients, and the most of them.
+inline int64_t most_outer_splits(int64_t tokens, int64_t width, int count, int rank) {
     const int64_t blocks = cdiv(width, kOuterCols) * cdiv(rank, rank_tile(rank)) * count;
-    const int64_t want = tokens <= kOuterWhole ? 1 : std::min(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256));
+    return tokens <= kOuterWhole ? 1 : std::min(cdiv(kTargetBlocks, blocks), cdiv(tokens, 256));
+}
+
+inline void outer_plan(int64_t tokens, int64_t width, int count, int rank, int64_t &split, int &splits) {
+    const int64_t want = most_outer_splits(tokens, width, count, rank);
     split = cdiv(cdiv(tokens, want), kOuterTokens) * kOuterTokens;
     splits = (int)cdiv(tokens, split);
 }
@@ -219,10 +270,22 @@ inline GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, in
     const size_t cols_a = p.splits_a > 1 ? (size_t)p.splits_a * in : 0;
     const size_t cols_b = p.splits_b > 1 ? (size_t)p.splits_b * p.width : 0;
     p.outer = round_up(std::max(cols_a, cols_b) * count * rank * 4, 256);
-    p.tile = split_plan(in, tokens, p.width, true);
+    p.tile = split_plan(in, tokens, p.width, kTileSums);
     p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
     p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
     return p;
+}
+
+// Of grad_plan for up to `tokens`.
+inline size_t most_grad(int64_t tokens, int64_t in, int64_t out, int count, int rank, bool widen) {
+    const int64_t width = cdiv(out, 16) * 16;
+    const int64_t a = most_outer_splits(tokens, in, count, rank), b = most_outer_splits(tokens, width, count, rank);
+    const int64_t cols = std::max(a > 1 ? a * in : 0, b > 1 ? b * width : 0);
+    const size_t outer = round_up((size_t)cols * count * rank * 4, 256);
+    return round_up((size_t)out * in * 2, 256) + (widen ? round_up((size_t)tokens * width * 2, 256) : 0) +
+           round_up((size_t)count * rank * width * 2, 256) +
+           std::max(most_low_partial(tokens, width, rank), most_low_partial(tokens, in, rank)) +
+           2 * low_bytes(tokens, rank) + std::max(outer, most_sums(in, tokens, width, kTileSums));
 }
 
 // ---------------------------------------------------------------------------
@@ -235,7 +298,12 @@ constexpr int kMost = 256;  // parts of the largest weight
 // tokens of 8192 over 500 words: 18 us so, 66 in one pass; of 300 over 2000: 29
 // and 67; at 250 tiles (64 tokens of 4096 over 32000 words) both take 68.
 inline Split logit_plan(int64_t words, int64_t tokens, int64_t d, bool one_piece) {
-    return split_plan(words, tokens, d, one_piece && cdiv(words, 128) * cdiv(tokens, 128) <= kCUs / 2);
+    return split_plan(words, tokens, d, one_piece && cdiv(words, 128) * cdiv(tokens, 128) <= kCUs / 2 ? kLogitSums : 0);
+}
+
+// Of logit_plan for up to `tokens`.
+inline size_t most_logit_sums(int64_t words, int64_t tokens, int64_t d) {
+    return cdiv(words, 128) <= kCUs / 2 ? most_sums(words, tokens, d, kLogitSums) : 0;
 }
 
 struct LossPlan {
@@ -258,10 +326,16 @@ inline LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     return p;
 }
 
-// Both parts of a piece of g take up to 384 MB, and at least 2048 of the
+// Of loss_plan for up to `tokens`.
+inline size_t most_loss(int64_t tokens, int64_t d, int64_t vocab) {
+    const size_t parts = round_up((size_t)cdiv(vocab, 128) * tokens * 2 * sizeof(float), 256);
+    return std::max(parts + round_up((size_t)tokens * 4, 256), most_logit_sums(cdiv(vocab, 4) * 4, tokens, d));
+}
+
+// Both parts of a piece of g take up to 380 MB, and at least 2048 of the
 // vocabulary: so that a piece's products fill the chip many times over, and its
 // sums in dX, read and written once a piece, stay below a twentieth of them.
-constexpr int64_t kPieceBytes = (int64_t)384 << 20;
+constexpr int64_t kPieceBytes = (int64_t)380 << 20;
 constexpr int64_t kLeastPiece = 2048;
 constexpr int64_t kPieceStep = 256;
 
@@ -277,7 +351,7 @@ inline LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, boo
     p.pieces = cdiv(vocab, fit);
     p.piece = cdiv(cdiv(vocab, p.pieces), kPieceStep) * kPieceStep;
     p.pieces = cdiv(vocab, p.piece);
-    p.dx = split_plan(d, tokens, 2 * p.piece, true);  // both parts
+    p.dx = split_plan(d, tokens, 2 * p.piece, kTileSums);  // both parts
     p.dx.k = cdiv(cdiv(p.piece, p.dx.splits), 64) * 64;
     p.dx.splits = (int)cdiv(p.piece, p.dx.k);
     p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
@@ -290,5 +364,19 @@ inline LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, boo
     p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
     return p;
 }
+
+// Of loss_grad_plan for up to `tokens`.
+inline size_t most_loss_grad(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
+    const int64_t words = cdiv(vocab, kPieceStep) * kPieceStep;
+    const int64_t g = std::min(std::max(kPieceBytes, 4 * tokens * kLeastPiece), 4 * tokens * words);
+    const size_t sum = std::max(round_up((size_t)tokens * d * 4, 256), most_sums(d, tokens, 2 * words, kTileSums));
+    return round_up((size_t)g, 256) + std::max(sum, most_logit_sums(words, tokens, d)) +
+           (dw ? round_up((size_t)tokens * d * 2, 256) : 0) + round_up((size_t)tokens * sizeof(float), 256) +
+           kMost * sizeof(float);
+}
+
+// The tiles of a piece's slopes (`ldg` words) and of its rows of dW (`cols`).
+inline Split slope_plan(int64_t ldg, int64_t tokens, int64_t d) { return split_plan(ldg, tokens, d, 0); }
+inline Split dw_plan(int64_t d, int64_t cols, int64_t tokens) { return split_plan(d, cols, 2 * tokens, 0); }
 
 }  // namespace
