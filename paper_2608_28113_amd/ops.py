@@ -55,7 +55,7 @@ def _new(shape, dtype, device, stream, zeros=False, scratch=False) -> torch.Tens
     What is returned is recorded on the current stream too, where the caller
     will use and drop it."""
     make = torch.zeros if zeros else torch.empty
-    side = _elsewhere(stream, device)
+    side = None if stream is None else _elsewhere(stream, device)
     if side is None:
         return make(shape, dtype=dtype, device=device)
     with torch.cuda.stream(side):
@@ -424,6 +424,13 @@ def output_error(X: torch.Tensor, W: torch.Tensor, global_scale: float, scale_co
 CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
 
 
+def _no_graph(where: str, *tensors) -> None:
+    """Refuses tensors whose gradient would be expected and lost: the calls record no graph."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{where} records no graph: call it under torch.no_grad(), in an autograd function or with "
+                         f"detached tensors, and take the gradients from {where}_grad")
+
+
 def _rows_in(t, name: str) -> int:
     """t is a 2-D bf16 CUDA view with unit column stride; its row stride."""
     if not _on_device(t) or t.dtype is not torch.bfloat16 or t.dim() != 2:
@@ -491,12 +498,16 @@ def adapted_linear(X: torch.Tensor, global_scale: float, scale_codes: torch.Tens
     bf16 [adapters, out, rank] (rank a multiple of 8 up to 256), alpha fp32
     [adapters] (1 when None), adapter int32 [tokens], where a number outside
     0 .. adapters - 1 means none; with one adapter it may be None: all use it.
+
+    No graph is recorded: tensors that require a gradient are refused where
+    torch would record one (adapted_linear_grad returns the gradients).
     """
     ldx = _rows_in(X, "X")
     T, n = X.shape
     dev = X.device
     m = _stored(scale_codes, packed_e2m1, n, dev)
     ad = _adapters(A, B, alpha, adapter, T, n, m, dev)
+    _no_graph("adapted_linear", X, A, B, alpha)
     Y, ldy = _rows_out(Y, "Y", (T, m), dev, stream)
     need = adapted_linear_workspace_bytes(T, n, m, *(ad[:2] if ad else (0, 0)))
     ws_ptr, ws_bytes, held = _workspace(workspace, need, dev, stream)
@@ -595,11 +606,14 @@ def token_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: tor
     """Softmax cross entropy of each token over the vocabulary, without the
     logits X W^T in memory: (loss, lse), fp32 [tokens].  X is bf16 [tokens, d]
     (rows may be strided), W bf16 [vocab, d], target int64 [tokens]; a target
-    outside 0 .. vocab - 1 is not scored (loss 0)."""
+    outside 0 .. vocab - 1 is not scored (loss 0).  Tensors that require a
+    gradient are refused where torch would record a graph (token_loss_grad
+    returns the gradients)."""
     ldx = _rows_in(X, "X")
     T, d = X.shape
     dev = X.device
     _head(X, W, target)
+    _no_graph("token_loss", X, W)
     loss = _out(loss, "loss", torch.float32, (T,), dev, stream)
     lse = _out(lse, "lse", torch.float32, (T,), dev, stream)
     ws_ptr, ws_bytes, held = _workspace(workspace, token_loss_workspace_bytes(T, d, W.shape[0]), dev, stream)
