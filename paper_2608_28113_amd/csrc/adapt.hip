@@ -9,7 +9,7 @@
 //   dA_a = sum_t v_t x_t^T,      dB_a = sum_t dy_t u_t^T     over its tokens
 //
 // An E2M1 value has 2 significant bits and an E4M3 scale 4, so with the power
-// of two of s_g = f 2^e (1 <= f < 2) W^ is exact in bf16: the products with W^
+// of two of s_g = f 2^e W^ is exact in bf16: the products with W^
 // are bf16 products accumulated in fp32, and f multiplies the sum.  u and v are
 // kept as two bf16 parts (within 2^-16), so that nothing of the adapters' part
 // is rounded to 8 bits before the result is.
@@ -1219,10 +1219,16 @@ int check_adapters(const hscale_adapters *w, Adapters &ad) {
     return HSCALE_OK;
 }
 
-// s = f 2^e with 1 <= f < 2.
+// s = f 2^e with 1 <= f < 2, or more where 2^e would take the largest weight,
+// 448 x 6, out of bf16's range.
 inline void split_scale(float s, float &f, int &e) {
+    constexpr int kMostE = 100;
     f = 2.0f * std::frexp(s, &e);
     --e;
+    if (e > kMostE) {
+        f = std::ldexp(f, e - kMostE);
+        e = kMostE;
+    }
 }
 
 int stored_weights(const uint8_t *codes, const uint8_t *packed, int64_t out, int64_t in, int e, void *W,
