@@ -99,14 +99,18 @@ constexpr int kTargetBlocks = 1024;
 // of 14336 -> 4096 191 (169), of 4096 -> 4096 71 (65), of 4096 -> 1024 27 (29);
 // 2040 of 4096 -> 14336 274 (243).
 constexpr int64_t kFewTokens = 1024;
-// Up to 64 tokens a block takes them all, in sixteens, and the adapters' part
-// is computed beside the product and added at its end (fused); above, a block
-// takes 128, and that is done while tokens x outputs x rank are few.  64 and 80
-// tokens of 4096 -> 14336 with eight adapters of rank 16: 27 and 38 us, of
-// 4096 -> 1024 11.5 and 13; reading B per token, as the end does, grows with
-// tokens and outputs, where the product's own stages read it once per 128
-// tokens.
-constexpr int64_t kFewTile = 64, kFewFused = 512, kFewFusedWork = (int64_t)64 << 20;
+// Up to 64 tokens a block takes them all, in sixteens, above it takes 128.  The
+// adapters' part is computed beside the product and added at its end (fused)
+// while tokens x outputs x rank are few: the end reads B once per token, where
+// the product's own stages, after two kernels before it, read it once per block
+// of tokens and adapter among them.  Fused (and not), us, 64 tokens with 1, 8
+// and 32 adapters: 4096 -> 4096, rank 128 26 (29), 32 (45), 48 (103), rank 256
+// 36 (34), 52 (66), 84 (161); 4096 -> 14336, rank 64 50 (35), 55 (43), 65 (77),
+// rank 128 75 (37), 83 (53), 165 (114), rank 256 128 (42), 151 (74), 369 (214).
+// The limit up to 64 tokens, 80 Mi, lies where no number of adapters loses much.
+// 80 tokens of 4096 -> 14336 with eight of rank 16 take 38 us fused.
+constexpr int64_t kFewTile = 64, kFewFused = 512;
+constexpr int64_t kFewTileWork = (int64_t)80 << 20, kFewFusedWork = (int64_t)64 << 20;  // up to 64 tokens, and above
 
 inline int rank_pad(int rank) { return (rank + 31) / 32 * 32; }
 inline int low_pad(int rank) { return (rank + 15) / 16 * 16; }
@@ -159,8 +163,8 @@ struct FewPlan {
 inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
     FewPlan p;
     p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
-    p.fused = count > 0 &&
-              (tokens <= kFewTile || (tokens <= kFewFused && tokens * out * (rank + 8) <= kFewFusedWork));
+    p.fused = count > 0 && tokens <= kFewFused &&
+              tokens * out * (rank + 8) <= (tokens <= kFewTile ? kFewTileWork : kFewFusedWork);
     const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
     double least = 0.0;
     for (int64_t s = 1; s <= kMostSplits && s <= cdiv(in, kFewK); ++s) {
@@ -215,7 +219,8 @@ inline size_t most_linear(int64_t tokens, int64_t in, int64_t out, int count, in
     int64_t sums = splits > 1 ? std::min(splits * t * out * 4, kFewSums) : 0;
     size_t low = 0;
     if (count > 0) {  // fused, k may be whole
-        sums = std::max(sums, std::max(std::min(t, kFewTile) * out, std::min(t * out, kFewFusedWork / (rank + 8))) * 4);
+        sums = std::max(sums, std::min(std::min(t, kFewTile) * out, kFewTileWork / (rank + 8)) * 4);
+        sums = std::max(sums, std::min(t * out, kFewFusedWork / (rank + 8)) * 4);
         const size_t fused = (size_t)cdiv(in, kFewLowK) * std::min(t, kFewFused) * rank_pad(rank) * 4;
         low = std::max(round_up(fused, 256), most_low_partial(t, in, rank)) + low_bytes(t, rank);
     }

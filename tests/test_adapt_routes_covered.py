@@ -8,7 +8,7 @@ import subprocess
 import pytest
 
 from tests import test_gpu_adapt, test_gpu_adapt_plain, test_gpu_adapt_routes, test_gpu_adapt_tiles, test_gpu_loss
-from tests import test_gpu_loss_precision
+from tests import test_gpu_adapt_wide, test_gpu_loss_precision
 from tests.test_adapt_plans import driver  # noqa: F401
 
 
@@ -22,7 +22,7 @@ def _tested():
     names = "T,n,m,count,rank,how"
     for case in (_sizes(test_gpu_adapt.test_linear_matches_64_bits, names)
                  + _sizes(test_gpu_adapt_routes.test_linear_on_both_sides_of_every_change, names)
-                 + test_gpu_adapt_tiles.LINEAR):
+                 + test_gpu_adapt_tiles.LINEAR + test_gpu_adapt_wide.LINEAR):
         lines.append("linear %d %d %d %d %d" % tuple(case[:5]))
     plain = test_gpu_adapt_plain.test_matches_64_bits_in_rows_of_any_stride
     lines += [f"linear {T} {n} {m} 0 0" for T in _sizes(plain, "T") for n, m in _sizes(plain, "n,m")]
