@@ -55,8 +55,7 @@ def _new(shape, dtype, device, stream, zeros=False, scratch=False) -> torch.Tens
     What is returned is recorded on the current stream too, where the caller
     will use and drop it."""
     make = torch.zeros if zeros else torch.empty
-    side = None if stream is None else _elsewhere(stream, device)
-    if side is None:
+    if stream is None or (side := _elsewhere(stream, device)) is None:
         return make(shape, dtype=dtype, device=device)
     with torch.cuda.stream(side):
         t = make(shape, dtype=dtype, device=device)
@@ -426,9 +425,11 @@ CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
 
 def _no_graph(where: str, *tensors) -> None:
     """Refuses tensors whose gradient would be expected and lost: the calls record no graph."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError(f"{where} records no graph: call it under torch.no_grad(), in an autograd function or with "
-                         f"detached tensors, and take the gradients from {where}_grad")
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{where} records no graph: call it under torch.no_grad(), in an autograd function "
+                                 f"or with detached tensors, and take the gradients from {where}_grad")
 
 
 def _rows_in(t, name: str) -> int:
