@@ -146,7 +146,7 @@ __device__ __forceinline__ u32x4 restore8(uint32_t lo, uint32_t hi, float s) {
 // A thread per 8 values, 16 threads per block of 128 (the last of a row may
 // be shorter): s = fp32(m fp32(1/127)) with m = max(|x|, 2^-100), and
 // q = rint(fp32(x fp32(127 / m))).  HBM bounds this and the way back: 16384 x
-// 14336 in 136 and 109 us, 5.2 and 6.5 TB/s.
+// 14336 in 136 and 111 us, 5.2 and 6.4 TB/s.
 __global__ __launch_bounds__(256) void pack_kernel(const uint16_t *__restrict__ X, int64_t tokens, int64_t in,
                                                    int64_t ldx, uint2 *__restrict__ q, float *__restrict__ scale) {
     const int64_t blocks = (in + kCkBlock - 1) / kCkBlock, total = tokens * blocks * 16;
@@ -225,9 +225,10 @@ struct ShrinkArgs {
 // bytes at a time (two lanes 32 consecutive ones); the adapter's rows, the
 // same for all waves, come through LDS, 16-byte chunk c of row j at c ^ (j % 16).
 // Checkpoints are taken 256 k at a time, so that as many bytes are under way.
-// 8192 x 4096 at rank 16 in 17 us (3.9 TB/s); a checkpoint of 8192 x 14336 at
-// rank 64 in 85 us (1.4 TB/s of 121 MB; MFMA 0.07 and VALU 0.18 busy): few and
-// short stages, each of which waits for its loads and for the block's barrier.
+// 8192 x 4096 at rank 16 in 17 to 20 us (3.9 to 3.4 TB/s); a checkpoint of 8192 x
+// 14336 at rank 64 in 95 us (1.3 TB/s of 121 MB; MFMA 0.06 and VALU 0.20 busy, 0.44
+// of the waves' time waiting): few and short stages, each of which waits for its
+// loads and for the block's barrier.
 template <bool kCheckpoint, int kMI>
 __global__ __launch_bounds__(256, 2) void shrink_kernel(const ShrinkArgs a) {
     constexpr int kK = kCheckpoint ? 256 : 128, kARow = kK * 2, kABytes = 32 * kMI * kARow;
@@ -479,9 +480,9 @@ struct LayerArgs {
 
 template <class T, Layout LW>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void layer_kernel(const LayerArgs a) {
-    // 8192 tokens of 4096 -> 14336 with adapters of rank 16: 790 us, 1.22 PFLOP/s
-    // at MFMA 0.63 busy and 1.87 GHz; the plain product in the same tiles reaches
-    // 1.25 to 1.35 as the chip's power lets its clock.
+    // 8192 tokens of 4096 -> 14336 with adapters of rank 16: 790 to 826 us, 1.22 to
+    // 1.17 PFLOP/s at MFMA 0.62 busy and 1.87 GHz; the plain product in the same
+    // tiles reaches 1.25 to 1.35 as the chip's power lets its clock.
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
     unsigned mt, nt;
     tile_of_block(blockIdx.x % a.tiles, a.tiles, a.mtiles, mt, nt);
@@ -600,15 +601,19 @@ __device__ __forceinline__ void few_low(const FewLowArgs &a, int block, uint8_t 
 
 // W^ against few tokens: 128 output rows x 16 kNT tokens x one split of k per
 // block.  8 waves: 32 rows each, and each half of a chunk of k its own four.
-// HBM bounds it for few tokens, the conversion of the weights (about 11 cycles
-// for two per lane) and LDS reads of X for 64.  A wave's MFMA operand of
+// Latency bounds it: the conversion of the weights (about 11 cycles for two per
+// lane) keeps the VALU a fifth to a third busy, and the waves wait for loads
+// and for each other.  A wave's MFMA operand of
 // weights comes straight from memory, 32 consecutive weights a lane: which k
 // meets which place in a step does not matter, as both operands agree.  X goes
 // through LDS, 16 bytes a lane, row t's 16-byte chunk c at c ^ (t % 16).
-// 1 token of 4096 -> 1024 in 6.7 us, latency alone; 48 of 4096 -> 14336 in 24 us
-// (33 MB of weights, 8 of 24 us by HBM; VALU 0.20 busy, half the time waiting);
-// 515 of 14336 -> 4096 in 104 us, 0.58 PFLOP/s: MFMA 0.31, LDS 0.31, VALU 0.33
-// busy, which two blocks' waves overlap only in part.
+// 1 token of 4096 -> 1024 in 6.6 us; 48 of 4096 -> 14336 with 32 adapters in 24 us
+// (33 MB of weights, 5 us of HBM's time; VALU 0.20 busy, 0.54 of the waves' time
+// waiting: the 256 blocks that go down to the rank come before the 448 of the
+// product, which 512 places do not hold together); 515 of 14336 -> 4096 in 104 us,
+// 0.58 PFLOP/s, a fifth of it on the empty columns of the fifth block of 128:
+// MFMA 0.31, LDS 0.31, VALU 0.33 busy, which two blocks' waves overlap only in
+// part.
 struct FewArgs {
     const uint8_t *codes;
     const uint8_t *packed;
@@ -907,10 +912,11 @@ struct OuterArgs {
 // are not read and enter as zeros, stages without any are passed over: which
 // ones have some is found for many stages at a time, so that a stage's rows
 // do not wait for its adapters' numbers.  A checkpoint of 8192 x 14336 (two
-// parts of rank 64, four adapters) takes 85 us, dY of 8192 x 4096 46: the
-// blocks that have tokens of their adapter are not many more than run at once,
-// and the longest last.  Sharing out the stages evenly cost more than that (121
-// and 78 us: every block then visits every part of the tokens).
+// parts of rank 64, four adapters, nearly all tokens of one of them) takes 90 us,
+// dY of 8192 x 4096 46: the blocks that have tokens of their adapter are a
+// quarter of all, not many more than run at once, and the longest last.  Sharing
+// out the stages evenly cost more than that on these tokens (121 and 78 us: every
+// block then visits every part of them).
 constexpr int kOuterMasks = 256, kOuterThreads = 512;
 
 // Four bf16 values to where they may not be aligned together.

@@ -65,8 +65,9 @@ struct LogitArgs {
 // A tile of words x tokens, reduced over its words where it lies: per token a
 // maximum and a sum in registers, then over lanes and waves.  Words are the
 // tile's rows, so that a lane holds 64 of one token's.  2040 tokens of 4096 over
-// 32003 words: 453 us, 1.18 PFLOP/s (MFMA 0.61 busy); 8192 over 128000: 6.8 ms,
-// 1.26 PFLOP/s: the product, at the clock the chip's power leaves it.
+// 32003 words: 453 to 477 us, 1.18 to 1.12 PFLOP/s (MFMA 0.6 busy); 8192 over
+// 128000: 6.8 to 7.0 ms, 1.25 PFLOP/s: the product, at the clock the chip's power
+// leaves it.
 template <class T>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_tile_kernel(const LogitArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
@@ -212,10 +213,10 @@ __global__ __launch_bounds__(256) void loss_finish(const float2 *__restrict__ pa
     loss[t] = y >= 0 && y < vocab ? l - at[t] : 0.0f;
 }
 
-// h of a piece of the vocabulary, bf16; zeros where a token is not scored and
-// beyond the vocabulary.  8192 tokens of 4096 over 32000 words: 1.85 to 1.9 ms,
-// 1.15 PFLOP/s; the exponentials and 524 MB of h come after the products, which
-// the one block that a CU holds cannot overlap.
+// Both parts of h of a piece of the vocabulary; zeros where a token is not scored
+// and beyond the vocabulary.  8192 tokens of 4096 over 11776 words: 0.77 ms, 1.03
+// PFLOP/s (MFMA 0.51 busy); the exponentials and 386 MB of h come after the
+// products, which the one block that a CU holds cannot overlap.
 template <class T>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void loss_slope_kernel(const LogitArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
@@ -359,6 +360,9 @@ struct SecondPart {
     }
 };
 
+// dX and dW of such a piece, both parts: 1.27 and 1.31 ms, 1.24 and 1.21 PFLOP/s
+// at MFMA 0.65 busy and 1.8 GHz, where a library product as large as one of the
+// parts of 32000 words reaches 1.39.
 struct DxArgs {
     Operand W, g;    // W [vocab piece, d] across, g [2, tokens, piece]
     unsigned mtiles, tiles;
@@ -488,9 +492,9 @@ int logit_sums(const void *X, int64_t tokens, int64_t d, int64_t ldx, const void
     return launch_status();
 }
 
-// Tokens whose weights each block of scored_rows reads for itself.  384 tokens
-// of 1024 over 8192 words, whole gradient and loss: 76.7 us so, 80.0 with a
-// launch before it; 2048 tokens of 4096: 19 us so, 13 in two launches.
+// Tokens whose weights each block of scored_rows reads for itself.  A launch
+// before it costs 3.3 us of a call over 384 tokens of 1024; for 2048 tokens of
+// 4096 it takes 19 us so, 13 in two launches.
 constexpr int64_t kFewWeights = 512;
 
 bool loss_sizes_ok(int64_t tokens, int64_t d, int64_t vocab) {

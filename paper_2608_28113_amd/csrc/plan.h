@@ -51,7 +51,7 @@ constexpr int64_t kLeastSplit = 256;  // k of one
 
 // Limits of partial sums: of a product in tiles, of the layer for few tokens and
 // of logits.  At 5 TB/s 256 MB take 107 us to write and read again, as long as
-// 25 stages of every block; in such tiles 256 blocks' sums are 64 MB or less.
+// 67 stages of the large tile; one round of 256 blocks has sums of 16 to 64 MB.
 constexpr int64_t kTileSums = (int64_t)256 << 20, kFewSums = (int64_t)64 << 20, kLogitSums = (int64_t)32 << 20;
 
 // The tile and the splits of the least estimated time, whose sums are at most
