@@ -17,6 +17,7 @@
 // Times below are of one MI355X, whose large copies reach 4.9 TB/s, streaming
 // reads 6.9 TB/s and large bf16 products 1.4 to 1.5 PFLOP/s.
 
+#include "checks.h"
 #include "matmul.h"
 
 #include <algorithm>

@@ -17,7 +17,6 @@
 #include <cstring>
 #include <type_traits>
 
-#include "host.h"
 #include "hscale.h"
 
 namespace {
@@ -152,8 +151,16 @@ __device__ __forceinline__ void load_group(const u32x4 *__restrict__ W, int64_t 
 }
 
 // ---------------------------------------------------------------------------
-// Host side: checks and launches shared by the entry points
+// Host side: argument checks shared by the entry points
 // ---------------------------------------------------------------------------
+
+inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
+    if (na == 0 || nb == 0) return false;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    return a0 < b0 + nb && b0 < a0 + na;
+}
 
 // True when s_g keeps every S[c] a finite normal fp32 with a finite
 // reciprocal: s_g * 2^-9 >= 2^-126 and s_g * 448 < 2^128.
@@ -178,5 +185,14 @@ inline int grid_for(int64_t groups, int threads) {
 }
 
 inline int launch_status() { return hipGetLastError() == hipSuccess ? HSCALE_OK : HSCALE_ERR_HIP; }
+
+// Bytes spanned by `rows` rows of `width` elements at a row stride of `ld`
+// elements of `elem` bytes each.
+inline size_t span(int64_t rows, int64_t ld, int64_t width, size_t elem) {
+    if (rows <= 0 || width <= 0) return 0;
+    return ((size_t)(rows - 1) * (size_t)ld + (size_t)width) * elem;
+}
+
+inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 }  // namespace

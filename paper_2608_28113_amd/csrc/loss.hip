@@ -20,6 +20,7 @@
 //   h_tv = weight_t / c (exp(l_tv - lse_t) - [v = target]), in two parts,
 //   dX = c (h W),  dW = c (h^T X).
 
+#include "checks.h"
 #include "matmul.h"
 
 #include <algorithm>

@@ -11,9 +11,14 @@
 // Times beside the rules are of one MI355X.
 #pragma once
 
-#include "host.h"
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
 
 namespace {
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t round_256(size_t bytes) { return (bytes + 255) / 256 * 256; }  // parts of a workspace
 
 constexpr int kCUs = 256;
 
@@ -74,13 +79,13 @@ inline Split split_plan(int64_t m, int64_t n, int64_t k, int64_t most) {
 }
 
 inline size_t sum_bytes(const Split &p, int64_t m, int64_t n) {
-    return p.splits > 1 ? round_up((size_t)p.splits * m * n * 4, 256) : 0;
+    return p.splits > 1 ? round_256((size_t)p.splits * m * n * 4) : 0;
 }
 
 // Of split_plan(m, up to n, up to k, most).
 inline size_t most_sums(int64_t m, int64_t n, int64_t k, int64_t most) {
     const int64_t splits = std::min<int64_t>(kMostSplits, (k - 1) / (kLeastSplit - 1));
-    return splits > 1 ? round_up((size_t)std::min(splits * m * n * 4, most), 256) : 0;
+    return splits > 1 ? round_256((size_t)std::min(splits * m * n * 4, most)) : 0;
 }
 
 // ---------------------------------------------------------------------------
@@ -137,7 +142,7 @@ inline Low low_plan(int64_t tokens, int64_t width, int count, int rank) {
 }
 
 inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
-    return round_up((size_t)p.splits * tokens * rank_pad(rank) * 4, 256);
+    return round_256((size_t)p.splits * tokens * rank_pad(rank) * 4);
 }
 
 // Of low_plan for up to `tokens`: splits x tokens are at most kTargetBlocks x 128
@@ -145,10 +150,10 @@ inline size_t low_partial_bytes(const Low &p, int64_t tokens, int rank) {
 inline size_t most_low_partial(int64_t tokens, int64_t width, int rank) {
     const int64_t rows = std::min(cdiv(width, 2 * kLowStep) * tokens,
                                   (int64_t)kTargetBlocks * 128 / cdiv(rank, rank_tile(rank)));
-    return round_up((size_t)std::max(tokens, rows) * rank_pad(rank) * 4, 256);
+    return round_256((size_t)std::max(tokens, rows) * rank_pad(rank) * 4);
 }
 
-inline size_t low_bytes(int64_t tokens, int rank) { return round_up((size_t)tokens * 2 * low_pad(rank) * 2, 256); }
+inline size_t low_bytes(int64_t tokens, int rank) { return round_256((size_t)tokens * 2 * low_pad(rank) * 2); }
 
 struct FewPlan {
     int64_t k_split;
@@ -196,14 +201,14 @@ inline LinearPlan linear_plan(int64_t tokens, int64_t in, int64_t out, int count
     p.few = tokens <= kFewTokens;
     if (p.few) {
         p.base = few_plan(tokens, in, out, count, rank);
-        if (p.base.fused || p.base.splits > 1) p.partial = round_up((size_t)p.base.splits * tokens * out * 4, 256);
+        if (p.base.fused || p.base.splits > 1) p.partial = round_256((size_t)p.base.splits * tokens * out * 4);
     } else {
-        p.weights = round_up((size_t)out * in * 2, 256);
+        p.weights = round_256((size_t)out * in * 2);
         p.tile = split_plan(out, tokens, in, kTileSums);
         p.partial = sum_bytes(p.tile, out, tokens);
     }
     if (p.few && p.base.fused) {
-        p.low_partial = round_up((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4, 256);
+        p.low_partial = round_256((size_t)p.base.low_splits * tokens * rank_pad(rank) * 4);
     } else if (count > 0) {
         p.low = low_plan(tokens, in, count, rank);
         p.low_partial = low_partial_bytes(p.low, tokens, rank);
@@ -222,11 +227,11 @@ inline size_t most_linear(int64_t tokens, int64_t in, int64_t out, int count, in
         sums = std::max(sums, std::min(std::min(t, kFewTile) * out, kFewTileWork / (rank + 8)) * 4);
         sums = std::max(sums, std::min(t * out, kFewFusedWork / (rank + 8)) * 4);
         const size_t fused = (size_t)cdiv(in, kFewLowK) * std::min(t, kFewFused) * rank_pad(rank) * 4;
-        low = std::max(round_up(fused, 256), most_low_partial(t, in, rank)) + low_bytes(t, rank);
+        low = std::max(round_256(fused), most_low_partial(t, in, rank)) + low_bytes(t, rank);
     }
-    const size_t few = round_up((size_t)sums, 256) + low;
+    const size_t few = round_256((size_t)sums) + low;
     if (tokens <= kFewTokens) return few;
-    const size_t many = round_up((size_t)out * in * 2, 256) + most_sums(out, tokens, in, kTileSums) +
+    const size_t many = round_256((size_t)out * in * 2) + most_sums(out, tokens, in, kTileSums) +
                         (count > 0 ? most_low_partial(tokens, in, rank) + low_bytes(tokens, rank) : 0);
     return std::max(few, many);
 }
@@ -263,9 +268,9 @@ inline GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, in
     GradPlan p{};
     p.width = cdiv(out, 16) * 16;
     p.widen = widen;
-    p.weights = round_up((size_t)out * in * 2, 256);
-    p.dy = widen ? round_up((size_t)tokens * p.width * 2, 256) : 0;
-    p.turned = round_up((size_t)count * rank * p.width * 2, 256);
+    p.weights = round_256((size_t)out * in * 2);
+    p.dy = widen ? round_256((size_t)tokens * p.width * 2) : 0;
+    p.turned = round_256((size_t)count * rank * p.width * 2);
     p.v = low_plan(tokens, p.width, count, rank);
     p.u = low_plan(tokens, in, count, rank);
     p.low_partial = std::max(low_partial_bytes(p.v, tokens, rank), low_partial_bytes(p.u, tokens, rank));
@@ -274,7 +279,7 @@ inline GradPlan grad_plan(int64_t tokens, int64_t in, int64_t out, int count, in
     outer_plan(tokens, p.width, count, rank, p.split_b, p.splits_b);
     const size_t cols_a = p.splits_a > 1 ? (size_t)p.splits_a * in : 0;
     const size_t cols_b = p.splits_b > 1 ? (size_t)p.splits_b * p.width : 0;
-    p.outer = round_up(std::max(cols_a, cols_b) * count * rank * 4, 256);
+    p.outer = round_256(std::max(cols_a, cols_b) * count * rank * 4);
     p.tile = split_plan(in, tokens, p.width, kTileSums);
     p.outer = std::max(p.outer, sum_bytes(p.tile, in, tokens));  // in turn
     p.total = p.weights + p.dy + p.turned + p.low_partial + 2 * p.low + p.outer;
@@ -286,9 +291,9 @@ inline size_t most_grad(int64_t tokens, int64_t in, int64_t out, int count, int 
     const int64_t width = cdiv(out, 16) * 16;
     const int64_t a = most_outer_splits(tokens, in, count, rank), b = most_outer_splits(tokens, width, count, rank);
     const int64_t cols = std::max(a > 1 ? a * in : 0, b > 1 ? b * width : 0);
-    const size_t outer = round_up((size_t)cols * count * rank * 4, 256);
-    return round_up((size_t)out * in * 2, 256) + (widen ? round_up((size_t)tokens * width * 2, 256) : 0) +
-           round_up((size_t)count * rank * width * 2, 256) +
+    const size_t outer = round_256((size_t)cols * count * rank * 4);
+    return round_256((size_t)out * in * 2) + (widen ? round_256((size_t)tokens * width * 2) : 0) +
+           round_256((size_t)count * rank * width * 2) +
            std::max(most_low_partial(tokens, width, rank), most_low_partial(tokens, in, rank)) +
            2 * low_bytes(tokens, rank) + std::max(outer, most_sums(in, tokens, width, kTileSums));
 }
@@ -321,20 +326,20 @@ inline LossPlan loss_plan(int64_t tokens, int64_t d, int64_t vocab) {
     const int64_t words = cdiv(vocab, 4) * 4;
     p.tile = logit_plan(words, tokens, d, true);
     if (p.tile.splits > 1) {
-        p.parts = p.total = round_up((size_t)p.tile.splits * tokens * words * 4, 256);
+        p.parts = p.total = round_256((size_t)p.tile.splits * tokens * words * 4);
         p.at = 0;
         return p;
     }
-    p.parts = round_up((size_t)cdiv(vocab, p.tile.side_m()) * tokens * 2 * sizeof(float), 256);
-    p.at = round_up((size_t)tokens * 4, 256);
+    p.parts = round_256((size_t)cdiv(vocab, p.tile.side_m()) * tokens * 2 * sizeof(float));
+    p.at = round_256((size_t)tokens * 4);
     p.total = p.parts + p.at;
     return p;
 }
 
 // Of loss_plan for up to `tokens`.
 inline size_t most_loss(int64_t tokens, int64_t d, int64_t vocab) {
-    const size_t parts = round_up((size_t)cdiv(vocab, 128) * tokens * 2 * sizeof(float), 256);
-    return std::max(parts + round_up((size_t)tokens * 4, 256), most_logit_sums(cdiv(vocab, 4) * 4, tokens, d));
+    const size_t parts = round_256((size_t)cdiv(vocab, 128) * tokens * 2 * sizeof(float));
+    return std::max(parts + round_256((size_t)tokens * 4), most_logit_sums(cdiv(vocab, 4) * 4, tokens, d));
 }
 
 // Both parts of a piece of g take up to 380 MB, and at least 2048 of the
@@ -360,12 +365,12 @@ inline LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, boo
     p.dx.k = cdiv(cdiv(p.piece, p.dx.splits), 64) * 64;
     p.dx.splits = (int)cdiv(p.piece, p.dx.k);
     p.logits = logit_plan(p.piece, tokens, d, p.pieces == 1);
-    p.g = round_up((size_t)tokens * p.piece * 4, 256);
-    p.sum = round_up((size_t)p.dx.splits * tokens * d * 4, 256);
+    p.g = round_256((size_t)tokens * p.piece * 4);
+    p.sum = round_256((size_t)p.dx.splits * tokens * d * 4);
     if (p.logits.splits > 1)  // in turn
-        p.sum = std::max(p.sum, round_up((size_t)p.logits.splits * tokens * p.piece * 4, 256));
-    p.rows = dw ? round_up((size_t)tokens * d * 2, 256) : 0;
-    p.factor = round_up((size_t)tokens * sizeof(float), 256);
+        p.sum = std::max(p.sum, round_256((size_t)p.logits.splits * tokens * p.piece * 4));
+    p.rows = dw ? round_256((size_t)tokens * d * 2) : 0;
+    p.factor = round_256((size_t)tokens * sizeof(float));
     p.total = p.g + p.sum + p.rows + p.factor + kMost * sizeof(float);
     return p;
 }
@@ -374,9 +379,9 @@ inline LossGradPlan loss_grad_plan(int64_t tokens, int64_t d, int64_t vocab, boo
 inline size_t most_loss_grad(int64_t tokens, int64_t d, int64_t vocab, bool dw) {
     const int64_t words = cdiv(vocab, kPieceStep) * kPieceStep;
     const int64_t g = std::min(std::max(kPieceBytes, 4 * tokens * kLeastPiece), 4 * tokens * words);
-    const size_t sum = std::max(round_up((size_t)tokens * d * 4, 256), most_sums(d, tokens, 2 * words, kTileSums));
-    return round_up((size_t)g, 256) + std::max(sum, most_logit_sums(words, tokens, d)) +
-           (dw ? round_up((size_t)tokens * d * 2, 256) : 0) + round_up((size_t)tokens * sizeof(float), 256) +
+    const size_t sum = std::max(round_256((size_t)tokens * d * 4), most_sums(d, tokens, 2 * words, kTileSums));
+    return round_256((size_t)g) + std::max(sum, most_logit_sums(words, tokens, d)) +
+           (dw ? round_256((size_t)tokens * d * 2) : 0) + round_256((size_t)tokens * sizeof(float)) +
            kMost * sizeof(float);
 }
 
