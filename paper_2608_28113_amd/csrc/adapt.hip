@@ -1343,7 +1343,7 @@ int hscale_adapted_linear(const void *X, int64_t tokens, int64_t in, int64_t ldx
         if (p.base.fused) {
             a.low = FewLowArgs{a.X, tokens, ldx, in, ad.A, ad.count, ad.rank, rank_pad(ad.rank), ad.ids, low_sum,
                                p.base.low_splits, p.base.low_slots};
-            a.low_blocks = (int)cdiv(tokens, 32) * (rank_pad(ad.rank) / 32) * p.base.low_splits * p.base.low_slots;
+            a.low_blocks = (int)few_low_blocks(p.base, tokens, ad.rank);
         }
         const int nt = p.base.tile;
         const dim3 grid((unsigned)(a.low_blocks + (int64_t)a.row_blocks * a.splits * cdiv(tokens, 16 * nt)));

@@ -162,13 +162,23 @@ struct FewPlan {
     int tile;    // tokens a block, in sixteens
 };
 
+// A launch's threads are fewer than 2^32: of 512 each, half of that for these.
+constexpr int64_t kMostLowBlocks = (int64_t)1 << 22;
+
+// Blocks down to the rank: tiles of 32 tokens and 32 ranks, each split and slot.
+inline int64_t few_low_blocks(const FewPlan &p, int64_t tokens, int rank) {
+    return cdiv(tokens, 32) * (rank_pad(rank) / 32) * p.low_splits * p.low_slots;
+}
+
 // The splits of k of the least estimated time in us: rounds of one or two
 // blocks a CU, 256 k of a block in 1.2 to 2.4 us by its tokens (128 tokens
 // 2.3, measured at 512 tokens, 4096 -> 14336), partial sums at 5 TB/s.
 inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int rank) {
     FewPlan p;
     p.tile = tokens > 64 ? 8 : (int)cdiv(tokens, 16);
-    p.fused = count > 0 && tokens <= kFewFused &&
+    p.low_splits = (int)cdiv(in, kFewLowK);
+    p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
+    p.fused = count > 0 && tokens <= kFewFused && few_low_blocks(p, tokens, rank) <= kMostLowBlocks &&
               tokens * out * (rank + 8) <= (tokens <= kFewTile ? kFewTileWork : kFewFusedWork);
     const int64_t blocks = cdiv(out, kFewRows) * cdiv(tokens, 16 * p.tile), slots = p.tile > 4 ? kCUs : 2 * kCUs;
     double least = 0.0;
@@ -183,8 +193,6 @@ inline FewPlan few_plan(int64_t tokens, int64_t in, int64_t out, int count, int 
         p.k_split = k;
         p.splits = (int)n;
     }
-    p.low_splits = (int)cdiv(in, kFewLowK);
-    p.low_slots = (int)std::min<int64_t>(count, std::min<int64_t>(tokens, 32));
     return p;
 }
 

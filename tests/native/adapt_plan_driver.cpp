@@ -1,6 +1,7 @@
 // The plans behind the adapted layer, its gradients and the token loss, alone
 // (plan.h is plain C++).  Without arguments: over many sizes, what a plan uses
 // is at most what its call asks for, and that never falls with the tokens.
+// And no launch of one dimension has 2^32 threads.
 // With an argument: reads calls, one a line, from standard input and prints
 // the ways they take, one of a kernel a word.
 //   linear TOKENS IN OUT COUNT RANK | grad ... | loss TOKENS D VOCAB | loss_grad ...
@@ -54,6 +55,18 @@ static std::string loss_grad(int64_t t, int64_t d, int64_t vocab) {
 }
 
 static int bad = 0;
+
+// The blocks of 512 threads of the layer for few tokens: those down to the rank,
+// then those of the product.
+static void launchable(int64_t t, int64_t in, int64_t out, int count, int rank) {
+    const FewPlan p = few_plan(t, in, out, count, rank);
+    const int64_t blocks = (p.fused ? few_low_blocks(p, t, rank) : 0) +
+                           cdiv(out, kFewRows) * p.splits * cdiv(t, 16 * p.tile);
+    if (blocks * 512 >= (int64_t)1 << 32 && bad++ < 10)
+        std::printf("adapted_linear %lld x %lld, %d of rank %d, %lld tokens: %lld blocks\n", (long long)in,
+                    (long long)out, count, rank, (long long)t, (long long)blocks);
+}
+
 template <class Used, class Most>
 static void grows(const char *what, int64_t a, int64_t b, int count, int rank, const Used &used, const Most &most) {
     size_t before = 0;
@@ -87,6 +100,7 @@ int main(int argc, char **) {
         for (int64_t m : outs) {
             for (const auto &a : adapters) {
                 const int c = a[0], r = a[1];
+                for (int64_t t = 1; t <= kFewTokens; ++t) launchable(t, n, m, c, r);
                 grows("adapted_linear", n, m, c, r, [&](int64_t t) { return linear_plan(t, n, m, c, r).total; },
                       [&](int64_t t) { return most_linear(t, n, m, c, r); });
                 if (c)
