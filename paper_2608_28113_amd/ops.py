@@ -8,6 +8,11 @@ The C ABI cannot see buffer sizes or devices, so every tensor handed to it
 here (inputs, caller-provided outputs and workspaces) is checked for dtype,
 shape, contiguity and device first: a wrong buffer raises ValueError and
 nothing is launched.
+
+A call given `stream` runs there.  New outputs and scratch are allocated for
+it; the tensors that are passed in are the caller's to order and to keep: what
+wrote them comes before on that stream, and they are not dropped while it may
+still read them (torch.Tensor.record_stream).
 """
 from __future__ import annotations
 
