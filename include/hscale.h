@@ -584,6 +584,121 @@ int hscale_token_loss_grad(const void *X, int64_t tokens, int64_t d, int64_t ldx
                            const int64_t *target, const float *lse, const float *weight, void *dX, int64_t lddx,
                            void *dW, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * A decode step through stored experts and onto the vocabulary: layers whose
+ * experts are stored in NVFP4, and what is done to the logits of a request
+ * before a token is chosen.  As in the part above, values that are not finite
+ * in one token's or one row's inputs reach no other token's or row's result,
+ * and workspaces do not fall with the number of tokens.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Types of logits. */
+#define HSCALE_BF16 0
+#define HSCALE_F32 1
+
+/*
+ * The k largest logits of each token, in falling order and the lowest number
+ * first where they are equal, as its experts, and their shares of the softmax
+ * as the experts' weights: of the k alone if `normalize`, else of all experts.
+ *   weight[t, j] = exp(l[t, e_j] - max) / sum exp(l[t, .] - max),  fp32
+ * A logit of -inf or NaN is never chosen: a token with fewer than k others gets
+ * the number -1 and weight 0 for the rest.  A NaN or +inf among its logits
+ * makes the weights of that token NaN.
+ *
+ * logits     bf16 or fp32 (`type`) [tokens, experts], rows ld elements apart
+ * expert     int32 [tokens, k]
+ * weight     fp32 [tokens, k]
+ * tokens <= 2^24, experts in 1 .. 1024, k in 1 .. min(32, experts).
+ */
+int hscale_route_tokens(const void *logits, int32_t type, int64_t tokens, int32_t experts, int64_t ld, int32_t k,
+                        int32_t normalize, int32_t *expert, float *weight, hipStream_t stream);
+
+/*
+ * One matrix of every expert, stored as hscale_search or hscale_quantize store
+ * a layer, one after another.  The scales lie on the device and are not
+ * checked: each in the range that hscale_search accepts.
+ */
+typedef struct hscale_experts {
+    const float *global_scale;  /* fp32 [experts] */
+    const uint8_t *scale_codes; /* uint8 [experts, out, in / 16] */
+    const uint8_t *packed_e2m1; /* uint8 [experts, out, in / 2], 8-byte aligned */
+} hscale_experts;
+
+/* Workspace bytes hscale_expert_layer needs (0 when a size is 0 or invalid). */
+size_t hscale_expert_layer_workspace_bytes(int64_t tokens, int64_t in, int64_t hidden, int32_t experts, int32_t k);
+
+/*
+ * A gated layer of stored experts, each token through its own k of them:
+ *   Y[t] = sum_j weight[t, j] D_e (silu(G_e X[t]) * (U_e X[t])),  e = expert[t, j]
+ * with silu(g) = g / (1 + exp(-g)).  A number outside 0 .. experts - 1 means no
+ * expert: it adds weight[t, j] times 0, so that a token without any gets zeros.
+ * The same expert twice counts twice.
+ *
+ * X          bf16 [tokens, in] with rows ldx <= 2^21 elements apart, 16-byte
+ *            aligned rows
+ * gate, up   host structs, read during the call: [experts, hidden, in]
+ * down       [experts, in, hidden]
+ * expert     int32 [tokens, k], weight fp32 [tokens, k]
+ * Y          bf16 [tokens, in] with rows ldy elements apart
+ * workspace  256-byte aligned
+ * tokens <= 2^24, in and hidden multiples of 16 up to 2^21, experts in
+ * 1 .. 1024, k in 1 .. 32.
+ *
+ * Made for the few tokens of a decode step or a chunk of a prompt; longer calls
+ * go in pieces of up to 4096 / k tokens.  Products are bf16, sums fp32; the
+ * hidden values enter the second product in two bf16 parts (16 bits), Y is
+ * rounded once.  A token's bits do not depend on its place among the call's
+ * tokens.
+ */
+int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, int64_t hidden, int32_t experts,
+                        const hscale_experts *gate, const hscale_experts *up, const hscale_experts *down,
+                        const int32_t *expert, const float *weight, int32_t k, void *Y, int64_t ldy, void *workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * What a row of logits is changed by; every pointer may be NULL for none.
+ * Numbers outside their range mean none: words of the history outside
+ * 0 .. vocab - 1, lengths and prompts below 0 or past `history_length` (taken as
+ * 0 and history_length), rows of bias and mask.
+ */
+typedef struct hscale_logit_rules {
+    const int32_t *history;  /* int32 [rows, history_length], rows history_ld apart: words already said */
+    int64_t history_length;
+    int64_t history_ld;
+    const int32_t *length;   /* int32 [rows]: how many of them count; NULL: all */
+    const int32_t *prompt;   /* int32 [rows]: how many of these are the prompt's; NULL: none */
+    const float *repetition; /* fp32 [rows], > 0 */
+    const float *frequency;  /* fp32 [rows] */
+    const float *presence;   /* fp32 [rows] */
+    const float *bias;       /* fp32 [biases, vocab] */
+    int32_t biases;
+    const int32_t *bias_row; /* int32 [rows]: each row's bias; NULL with one: all use it */
+    const uint32_t *mask;    /* uint32 [masks, ceil(vocab / 32)]: bit v % 32 of number v / 32 set: word v is allowed */
+    int32_t masks;
+    const int32_t *mask_row; /* int32 [rows]: each row's mask; NULL with one: all use it */
+} hscale_logit_rules;
+
+/*
+ * Penalties for repeated words, biases and masks on logits, in this order and
+ * in fp32, each step rounded once:
+ *   l = l > 0 ? l / repetition : l * repetition    if v is in the history
+ *   l = l - frequency * count - presence           if it is in the answer,
+ *       the history behind its prompt, `count` times
+ *   l = l + bias[v]
+ *   l = -inf                                       if the mask's bit is clear
+ * What a mask forbids is -inf whatever it was; a mask may leave nothing.
+ *
+ * rules      host struct, read during the call
+ * logits     bf16 or fp32 (`type`) [rows, vocab], rows ld elements apart
+ * out        of the same type, rows ldo apart, rounded once; it may be `logits`
+ *            itself with the same ldo, and overlaps nothing else
+ * rows, vocab <= 2^24, history_length <= 2^30; biases, masks <= 2^24.
+ */
+int hscale_adjust_logits(const hscale_logit_rules *rules, const void *logits, int32_t type, int64_t rows, int64_t vocab,
+                         int64_t ld, void *out, int64_t ldo, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,6 +13,11 @@ pass, ``token_loss`` and ``token_loss_grad`` are the cross entropy over a large
 vocabulary and its gradient without stored logits, and ``adapted_linear_grad``
 returns the gradients of the adapters and of the layer's input.
 
+Layers of stored experts are served by ``route_tokens`` (the router's choice)
+and ``expert_layer`` (the experts' products, for the tokens of a decode step or
+a chunk of a prompt), and ``adjust_logits`` applies a request's penalties,
+biases and masks to the logits before a token is chosen.
+
 The compute is in ``libhscale.so`` (hand-written HIP, C ABI in
 ``include/hscale.h``); this package is its thin Python binding.
 """
@@ -21,4 +26,5 @@ from .ops import (hdiag, hdiag_accumulate, hdiag_finalize, hdiag_noalloc, hdiag_
                   output_error, output_error_workspace_bytes, search, search_block, search_layers, search_stats,
                   shift_summary, adapted_linear, adapted_linear_workspace_bytes, adapted_linear_grad,
                   adapted_linear_grad_workspace_bytes, pack_activations, unpack_activations, token_loss,
-                  token_loss_workspace_bytes, token_loss_grad, token_loss_grad_workspace_bytes)
+                  token_loss_workspace_bytes, token_loss_grad, token_loss_grad_workspace_bytes, route_tokens,
+                  expert_layer, expert_layer_workspace_bytes, adjust_logits)

@@ -48,9 +48,14 @@ EXPORTS = (
     "hscale_token_loss",
     "hscale_token_loss_grad_workspace_bytes",
     "hscale_token_loss_grad",
+    "hscale_route_tokens",
+    "hscale_expert_layer_workspace_bytes",
+    "hscale_expert_layer",
+    "hscale_adjust_logits",
 )
 
 HSCALE_INIT_MAXABS, HSCALE_INIT_4OVER6, HSCALE_INIT_GIVEN = 0, 1, 2
+HSCALE_BF16, HSCALE_F32 = 0, 1
 
 
 class HScaleLayer(ctypes.Structure):
@@ -65,6 +70,20 @@ class HScaleAdapters(ctypes.Structure):
     """struct hscale_adapters of include/hscale.h (natural C layout)."""
     _fields_ = [("count", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
                 ("alpha", ctypes.c_void_p), ("adapter", ctypes.c_void_p)]
+
+
+class HScaleExperts(ctypes.Structure):
+    """struct hscale_experts of include/hscale.h (natural C layout)."""
+    _fields_ = [("global_scale", ctypes.c_void_p), ("scale_codes", ctypes.c_void_p), ("packed_e2m1", ctypes.c_void_p)]
+
+
+class HScaleLogitRules(ctypes.Structure):
+    """struct hscale_logit_rules of include/hscale.h (natural C layout)."""
+    _fields_ = [("history", ctypes.c_void_p), ("history_length", ctypes.c_int64), ("history_ld", ctypes.c_int64),
+                ("length", ctypes.c_void_p), ("prompt", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("biases", ctypes.c_int32), ("bias_row", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("masks", ctypes.c_int32), ("mask_row", ctypes.c_void_p)]
 
 
 _lib = None
@@ -145,6 +164,15 @@ def load() -> ctypes.CDLL:
     lib.hscale_token_loss_grad_workspace_bytes.restype = sz
     lib.hscale_token_loss_grad.argtypes = [P, i64, i64, i64, P, i64, P, P, P, P, i64, P, P, sz, P]
     lib.hscale_token_loss_grad.restype = ctypes.c_int
+    EX = ctypes.POINTER(HScaleExperts)
+    lib.hscale_route_tokens.argtypes = [P, i32, i64, i32, i64, i32, i32, P, P, P]
+    lib.hscale_route_tokens.restype = ctypes.c_int
+    lib.hscale_expert_layer_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.hscale_expert_layer_workspace_bytes.restype = sz
+    lib.hscale_expert_layer.argtypes = [P, i64, i64, i64, i64, i32, EX, EX, EX, P, P, i32, P, i64, P, sz, P]
+    lib.hscale_expert_layer.restype = ctypes.c_int
+    lib.hscale_adjust_logits.argtypes = [ctypes.POINTER(HScaleLogitRules), P, i32, i64, i64, i64, P, i64, P]
+    lib.hscale_adjust_logits.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -320,3 +348,33 @@ def hscale_token_loss_grad(X: int, tokens: int, d: int, ldx: int, W: int, vocab:
                            stream: int) -> int:
     return (_lib or load()).hscale_token_loss_grad(X, tokens, d, ldx, W, vocab, target, lse, weight, dX, lddx, dW,
                                                    workspace, workspace_bytes, stream)
+
+
+def hscale_route_tokens(logits: int, type_: int, tokens: int, experts: int, ld: int, k: int, normalize: int,
+                        expert: int, weight: int, stream: int) -> int:
+    return (_lib or load()).hscale_route_tokens(logits, type_, tokens, experts, ld, k, normalize, expert, weight,
+                                                stream)
+
+
+def _experts(matrix):
+    """A pointer to struct hscale_experts of (global_scale, scale_codes, packed_e2m1), or NULL for None."""
+    return None if matrix is None else ctypes.byref(HScaleExperts(*matrix))
+
+
+def hscale_expert_layer_workspace_bytes(tokens: int, in_: int, hidden: int, experts: int, k: int) -> int:
+    return (_lib or load()).hscale_expert_layer_workspace_bytes(tokens, in_, hidden, experts, k)
+
+
+def hscale_expert_layer(X: int, tokens: int, in_: int, ldx: int, hidden: int, experts: int, gate, up, down,
+                        expert: int, weight: int, k: int, Y: int, ldy: int, workspace: int, workspace_bytes: int,
+                        stream: int) -> int:
+    return (_lib or load()).hscale_expert_layer(X, tokens, in_, ldx, hidden, experts, _experts(gate), _experts(up),
+                                                _experts(down), expert, weight, k, Y, ldy, workspace,
+                                                workspace_bytes, stream)
+
+
+def hscale_adjust_logits(rules, logits: int, type_: int, rows: int, vocab: int, ld: int, out: int, ldo: int,
+                         stream: int) -> int:
+    """rules: the fields of struct hscale_logit_rules in order, addresses as ints (0 for NULL), or None."""
+    r = None if rules is None else ctypes.byref(HScaleLogitRules(*rules))
+    return (_lib or load()).hscale_adjust_logits(r, logits, type_, rows, vocab, ld, out, ldo, stream)

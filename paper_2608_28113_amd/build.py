@@ -17,7 +17,8 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 CSRC = PKG / "csrc"
 SOURCES = [CSRC / "hdiag.hip", CSRC / "search.hip", CSRC / "diag.hip",  # share csrc/common.h
-           CSRC / "adapt.hip", CSRC / "loss.hip"]  # and csrc/matmul.h
+           CSRC / "adapt.hip", CSRC / "loss.hip", CSRC / "experts.hip",  # and csrc/matmul.h
+           CSRC / "logits.hip"]
 INCLUDE = ROOT / "include"
 LIB = PKG / "libhscale.so"
 PROBE_SOURCES = [CSRC / "probes.hip"]

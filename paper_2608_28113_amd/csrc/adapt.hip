@@ -19,6 +19,7 @@
 
 #include "checks.h"
 #include "matmul.h"
+#include "stored.h"
 
 #include <algorithm>
 
@@ -80,24 +81,6 @@ struct Distinct {
 // ---------------------------------------------------------------------------
 // Stored weights as bf16
 // ---------------------------------------------------------------------------
-
-// The E4M3 value of a scale code times 2^e, exact and without a branch: the
-// code's fields moved to those of an fp32 stand for the value times 2^-120, the
-// subnormal ones among them.
-__device__ __forceinline__ float scale_value(uint32_t code, int e) {
-    return ldexpf(__uint_as_float(code << 20), 120 + e);
-}
-
-// Two E2M1 values of byte K of `src` times l, as a pair of bf16: exact.
-template <int K>
-__device__ __forceinline__ uint32_t stored_pair(uint32_t src, float l) {
-    const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(src, 1.0f, K);
-    return __builtin_amdgcn_perm(__float_as_uint(v[1] * l), __float_as_uint(v[0] * l), 0x07060302);
-}
-
-__device__ __forceinline__ u32x4 stored_eight(uint32_t src, float l) {
-    return u32x4{stored_pair<0>(src, l), stored_pair<1>(src, l), stored_pair<2>(src, l), stored_pair<3>(src, l)};
-}
 
 // W^ [groups * 16] with 2^e in place of s_g, one group per thread.  HBM bounds
 // it: 14336 x 4096 in 31 us, 4.8 TB/s of 33 MB read and 117 MB written.  For

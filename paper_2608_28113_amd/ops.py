@@ -428,11 +428,14 @@ def output_error(X: torch.Tensor, W: torch.Tensor, global_scale: float, scale_co
 CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
 
 
-def _no_graph(where: str, *tensors) -> None:
+def _no_graph(where: str, *tensors, grad: bool = True) -> None:
     """Refuses tensors whose gradient would be expected and lost: the calls record no graph."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
+                if not grad:
+                    raise ValueError(f"{where} records no graph and has no gradient: call it under torch.no_grad() "
+                                     "or with detached tensors")
                 raise ValueError(f"{where} records no graph: call it under torch.no_grad(), in an autograd function "
                                  f"or with detached tensors, and take the gradients from {where}_grad")
 
@@ -655,3 +658,179 @@ def token_loss_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse:
                  0 if dW is None else dW.data_ptr(), ws_ptr, ws_bytes, _stream(stream, dev)),
            "hscale_token_loss_grad")
     return dX, dW
+
+
+# ---------------------------------------------------------------------------
+# A decode step through stored experts and onto the vocabulary
+# ---------------------------------------------------------------------------
+
+_LOGIT_TYPES = {torch.bfloat16: _lib.HSCALE_BF16, torch.float32: _lib.HSCALE_F32}
+
+
+def _logits(t, name: str) -> tuple[int, int]:
+    """t is a 2-D bf16 or fp32 CUDA view with unit column stride; the library's type and its row stride."""
+    if not _on_device(t) or t.dtype not in _LOGIT_TYPES or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D bf16 or fp32 CUDA tensor")
+    return _LOGIT_TYPES[t.dtype], _row_view(t, t.dtype, t.shape, t.device, name)
+
+
+def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: torch.Tensor | None = None,
+                 weight: torch.Tensor | None = None, stream=None):
+    """(expert int32 [tokens, k], weight fp32 [tokens, k]) of a router's logits,
+    bf16 or fp32 [tokens, experts] (rows may be strided): the k largest, the
+    lowest number first where they are equal, and their shares of the softmax
+    of the k (normalize) or of all experts.
+
+    A logit of -inf or NaN is never chosen; a token with fewer than k others
+    gets -1 and weight 0 for the rest.  NaN or +inf among a token's logits make
+    its weights NaN.  No graph is recorded: logits that require a gradient are
+    refused where torch would record one.
+    """
+    kind, ld = _logits(logits, "logits")
+    T, E = logits.shape
+    dev = logits.device
+    _no_graph("route_tokens", logits, grad=False)
+    k = int(k)
+    if not 1 <= k <= E:
+        raise ValueError(f"k must be in 1 .. {E}, the number of experts")
+    expert = _out(expert, "expert", torch.int32, (T, k), dev, stream)
+    weight = _out(weight, "weight", torch.float32, (T, k), dev, stream)
+    _check(_call(dev, _lib.hscale_route_tokens, logits.data_ptr(), kind, T, E, ld, k, int(bool(normalize)),
+                 expert.data_ptr(), weight.data_ptr(), _stream(stream, dev)), "hscale_route_tokens")
+    return expert, weight
+
+
+def _expert_matrix(matrix, name: str, device, shape=None):
+    """The checked addresses of (global_scale, scale_codes, packed_e2m1) and the shape [experts, out, in]."""
+    try:
+        scale, codes, packed = matrix
+    except (TypeError, ValueError):
+        raise ValueError(f"{name} must be (global_scale, scale_codes, packed_e2m1)") from None
+    if shape is None:
+        if not isinstance(packed, torch.Tensor) or packed.dim() != 3:
+            raise ValueError(f"{name}: packed_e2m1 must be a 3-D uint8 tensor [experts, out, in / 2]")
+        shape = (*packed.shape[:2], 2 * packed.shape[2])
+    E, m, n = shape
+    _tensor(packed, f"{name}: packed_e2m1", torch.uint8, (E, m, n // 2), device)
+    _tensor(codes, f"{name}: scale_codes", torch.uint8, (E, m, n // 16), device)
+    _tensor(scale, f"{name}: global_scale", torch.float32, (E,), device)
+    return (scale.data_ptr(), codes.data_ptr(), packed.data_ptr()), shape
+
+
+def expert_layer_workspace_bytes(tokens: int, in_features: int, hidden: int, experts: int, k: int) -> int:
+    """Bytes of scratch expert_layer needs."""
+    return _lib.hscale_expert_layer_workspace_bytes(tokens, in_features, hidden, experts, k)
+
+
+def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, gate, up, down,
+                 Y: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Y[t] = sum_j weight[t, j] D_e (silu(G_e X[t]) * (U_e X[t])), e = expert[t, j]:
+    a gated layer of experts stored in NVFP4, for the tokens of a decode step or
+    a chunk of a prompt.
+
+    X is bf16 [tokens, in] (rows may be strided, 16-byte aligned), expert int32
+    and weight fp32 [tokens, k] as route_tokens returns them; a number outside
+    0 .. experts - 1 means no expert.  gate, up (hidden x in) and down
+    (in x hidden) are each (global_scale fp32 [experts], scale_codes uint8
+    [experts, out, in / 16], packed_e2m1 uint8 [experts, out, in / 2]): what
+    search writes of each expert, stacked.  Y is bf16 [tokens, in] (rows may be
+    strided).
+
+    The stored experts are frozen and no graph is recorded: tensors that require
+    a gradient are refused where torch would record one.
+    """
+    ldx = _rows_in(X, "X")
+    T, n = X.shape
+    dev = X.device
+    if not isinstance(expert, torch.Tensor) or expert.dim() != 2:
+        raise ValueError("expert must be a 2-D int32 tensor [tokens, k]")
+    k = expert.shape[1]
+    _tensor(expert, "expert", torch.int32, (T, k), dev)
+    _tensor(weight, "weight", torch.float32, (T, k), dev)
+    gate, (E, hidden, width) = _expert_matrix(gate, "gate", dev)
+    if width != n:
+        raise ValueError(f"gate has {width} inputs, X {n}")
+    up, _ = _expert_matrix(up, "up", dev, (E, hidden, n))
+    down, _ = _expert_matrix(down, "down", dev, (E, n, hidden))
+    _no_graph("expert_layer", X, weight, grad=False)
+    Y, ldy = _rows_out(Y, "Y", (T, n), dev, stream)
+    need = expert_layer_workspace_bytes(T, n, hidden, E, k)
+    ws_ptr, ws_bytes, held = _workspace(workspace, need, dev, stream)
+    _check(_call(dev, _lib.hscale_expert_layer, X.data_ptr(), T, n, ldx, hidden, E, gate, up, down,
+                 expert.data_ptr(), weight.data_ptr(), k, Y.data_ptr(), ldy, ws_ptr, ws_bytes,
+                 _stream(stream, dev)), "hscale_expert_layer")
+    return Y
+
+
+def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, length: torch.Tensor | None = None,
+                  prompt: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
+                  frequency: torch.Tensor | None = None, presence: torch.Tensor | None = None,
+                  bias: torch.Tensor | None = None, bias_row: torch.Tensor | None = None,
+                  mask: torch.Tensor | None = None, mask_row: torch.Tensor | None = None,
+                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Logits, bf16 or fp32 [rows, vocab] (rows may be strided), with each row's
+    penalties for repeated words, its bias and its mask, in this order:
+
+        l > 0 ? l / repetition : l * repetition   of words in the history
+        l - frequency * count - presence          of words in the answer, said count times
+        l + bias[v],  -inf where the mask's bit is clear
+
+    history is int32 [rows, any length] (rows may be strided), of which the first
+    length[row] words count (all when None) and the first prompt[row] of those
+    are the prompt's, the rest the answer's (all when None); words outside the
+    vocabulary are passed over.  repetition (> 0), frequency and presence are
+    fp32 [rows].  bias is fp32 [biases, vocab], mask int32 [masks,
+    ceil(vocab / 32)] whose bit v % 32 of number v / 32 allows word v; bias_row
+    and mask_row (int32 [rows]) say which row uses which, any number outside
+    for none; with exactly one they may be None: all rows use it.
+
+    Returns `out`, new when None; out=logits works in place.  No graph is
+    recorded: tensors that require a gradient are refused where torch would
+    record one.
+    """
+    kind, ld = _logits(logits, "logits")
+    R, V = logits.shape
+    dev = logits.device
+    _no_graph("adjust_logits", logits, repetition, frequency, presence, bias, grad=False)
+    penalties = repetition is not None or frequency is not None or presence is not None
+    if history is None and (penalties or length is not None or prompt is not None):
+        raise ValueError("repetition, frequency, presence, length and prompt need a history")
+    words = ldh = 0
+    if history is not None:
+        if not isinstance(history, torch.Tensor) or history.dim() != 2:
+            raise ValueError("history must be a 2-D int32 tensor [rows, length]")
+        words = history.shape[1]
+        ldh = _row_view(history, torch.int32, (R, words), dev, "history")
+    for t, name, dtype in ((length, "length", torch.int32), (prompt, "prompt", torch.int32),
+                           (repetition, "repetition", torch.float32), (frequency, "frequency", torch.float32),
+                           (presence, "presence", torch.float32), (bias_row, "bias_row", torch.int32),
+                           (mask_row, "mask_row", torch.int32)):
+        if t is not None:
+            _tensor(t, name, dtype, (R,), dev)
+    sets = []
+    for t, at, name, dtype, width in ((bias, bias_row, "bias", torch.float32, V),
+                                      (mask, mask_row, "mask", torch.int32, -(-V // 32))):
+        if t is None:
+            if at is not None:
+                raise ValueError(f"{name}_row needs {name}")
+            sets.append(0)
+            continue
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise ValueError(f"{name} must be a 2-D {dtype} tensor")
+        sets.append(t.shape[0])
+        _tensor(t, name, dtype, (sets[-1], width), dev)
+        if at is None and sets[-1] != 1:
+            raise ValueError(f"{name}_row (int32, one number a row) is required unless there is exactly one {name}")
+    if out is None:
+        out, ldo = _new((R, V), logits.dtype, dev, stream), V
+    else:
+        ldo = _row_view(out, logits.dtype, (R, V), dev, "out")
+
+    def at(t):
+        return 0 if t is None else t.data_ptr()
+
+    rules = (at(history), words, ldh, at(length), at(prompt), at(repetition), at(frequency), at(presence), at(bias),
+             sets[0], at(bias_row), at(mask), sets[1], at(mask_row))
+    _check(_call(dev, _lib.hscale_adjust_logits, rules, logits.data_ptr(), kind, R, V, ld, out.data_ptr(), ldo,
+                 _stream(stream, dev)), "hscale_adjust_logits")
+    return out
