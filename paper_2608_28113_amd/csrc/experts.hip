@@ -171,234 +171,345 @@ struct ExpertArgs {
     const int32_t *order;  // with many slots
     const Share *shares;
     uint16_t *H;       // [slots, 2, rows]: gate and up
-    float *P;          // [slots, rows]: down
+    float *P;          // [splits, slots, rows]: down
+    int split;         // steps of a split of k: down
 };
 
 // s = f 2^e with 1 <= f < 2, or more where 2^e would take the largest weight
 // out of bf16's range.
-__device__ __forceinline__ void split_device_scale(float s, float &f, int &e) {
+__device__ __forceinline__ void split_device_scale(float s, float &f, float &two_e) {
     constexpr int kMostE = 100;
-    e = (int)(__float_as_uint(s) >> 23 & 0xFF) - 127;
+    int e = (int)(__float_as_uint(s) >> 23 & 0xFF) - 127;
     e = e > kMostE ? kMostE : e < -126 ? -126 : e;
+    two_e = ldexpf(1.0f, e);
     f = ldexpf(s, -e);
 }
 
-// 16 kRT rows of gate and of up (or 32 kRT of down) x up to 16 kNT slots of one
-// expert per block.  Its four waves take every fourth 128 k and add up through
-// LDS.  A wave's MFMA operand of weights comes straight from memory, 32
-// consecutive weights a lane: which k meets which place in a step does not
-// matter, as both operands agree.  The slots' rows come from L2 the same way;
-// each is read by one wave of the block.
-template <bool kDown, int kRT, int kNT, bool kEven>
+// The slots of a block's expert.  Up to 256 in all each wave finds them itself:
+// of one block for each expert, or for each slot where those are fewer (there
+// the block of an expert's first slot stays).
+struct Found {
+    int expert, count, first;  // first: in `order`, of many slots
+    uint64_t mask[kBlockSlots / 64];
+    bool many;
+
+    __device__ __forceinline__ bool find(const ExpertArgs &a, int y) {
+        const int lane = threadIdx.x & 63;
+        many = a.shares != nullptr;
+        if (many) {
+            const Share s = a.shares[y];
+            expert = s.expert, count = s.count, first = s.first;
+            return count > 0;
+        }
+        int id[kBlockSlots / 64];
+#pragma unroll
+        for (int i = 0; i < kBlockSlots / 64; ++i)
+            id[i] = i * 64 + lane < a.slots ? a.ids[i * 64 + lane] : kNoExpert;
+        expert = a.slots <= a.experts ? expert_of(a.ids, a.experts, y) : y;
+        if (expert == kNoExpert) return false;
+        count = 0;
+        int at = -1;  // the expert's first slot
+#pragma unroll
+        for (int i = 0; i < kBlockSlots / 64; ++i) {
+            mask[i] = __ballot(id[i] == expert);
+            if (at < 0 && mask[i]) at = i * 64 + __builtin_ctzll(mask[i]);
+            count += __popcll(mask[i]);
+        }
+        return count > 0 && (a.slots > a.experts || at == y);
+    }
+    // The c0 + lane th slot, -1 past the last.  `list` is the wave's own.
+    __device__ __forceinline__ int slot(const ExpertArgs &a, int c0, int *list) const {
+        const int lane = threadIdx.x & 63;
+        if (many) return c0 + lane < count ? a.order[first + c0 + lane] : -1;
+        int before = -c0;
+#pragma unroll
+        for (int i = 0; i < kBlockSlots / 64; ++i) {
+            const int n = before + __popcll(mask[i] & (((uint64_t)1 << lane) - 1));
+            if ((mask[i] >> lane & 1) && n >= 0 && n < 64) list[n] = i * 64 + lane;
+            before += __popcll(mask[i]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int got = c0 + lane < count ? list[lane] : -1;
+        __builtin_amdgcn_wave_barrier();
+        return got;
+    }
+};
+
+// Gate, up and silu: a lane's four rows of a slot's h, in two bf16 parts.
+__device__ __forceinline__ void store_hidden(uint16_t *h, int64_t rows, const float (&gate)[4], const float (&up)[4]) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float v = gate[q] / (1.0f + expf(-gate[q])) * up[q];
+        hi[q] = bf16_rne(v);
+        const float rest = v - bf16_value(hi[q]);
+        lo[q] = fabsf(rest) < INFINITY ? bf16_rne(rest) : 0;  // where v itself rounds to infinity
+    }
+    *reinterpret_cast<uint2 *>(h) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+    *reinterpret_cast<uint2 *>(h + rows) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+}
+
+__device__ __forceinline__ void own_writes_and_barrier() {  // loads stay under way
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// 16 kRT rows of gate and the same of up (or 32 kRT of down) a wave, x up to
+// kTok slots of one expert.  kW of the block's four waves share their rows: each
+// takes every kWth 256 k, and they add up through LDS.
+//
+// A wave's operand of weights comes straight from memory, 32 consecutive weights
+// of a row a lane (which k meets which place in a step does not matter, as both
+// operands agree).  The slots' rows go through LDS, 16-byte chunk c of row t at
+// c ^ (t % 16), two buffers of kW steps: straight from memory each wave's reads
+// of them kept the return path of loads 92 % busy, and a wait for them was one
+// for the weights behind them too.  Rows of a buffer that no slot has are columns
+// of the product that nothing reads.
+//
+// Scales are taken for four of the wave's steps at once, 16 bytes a lane, and
+// read back from LDS two at a time: as 2-byte loads for each step they took a
+// quarter of the time (64 tokens of 4096 over 128 experts of 1536: 363 us with
+// them, 275 without any scales).
+template <bool kDown, int kTok, int kRT, int kW, bool kWords>  // kWords: rows of scales are whole aligned words
 __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
-    constexpr int kSets = 2 * kRT, kMats = kDown ? 1 : 2, kParts = kDown ? 2 : 1;
-    constexpr int kRows = kDown ? 32 * kRT : 16 * kRT;  // of a matrix
-    constexpr int kStep = 128, kDepth = 2;
-    __shared__ __attribute__((aligned(16))) float4 red[4][kSets * kNT][64];
-    __shared__ int list[kBlockSlots];
-    __shared__ int found[4];
+    constexpr int kNT = (kTok + 15) / 16, kSets = 2 * kRT, kMats = kDown ? 1 : 2, kParts = kDown ? 2 : 1;
+    constexpr int kRows = kDown ? 32 * kRT : 16 * kRT;  // of a wave
+    constexpr int kStep = 256, kRowBytes = kStep * 2, kStepBytes = kTok * kRowBytes;
+    constexpr int kBuffer = kW * kParts * kStepBytes, kCopies = kBuffer / 4096;  // 16 bytes a thread
+    static_assert(kBuffer % 4096 == 0, "whole copies");
+    constexpr int kSums = kW > 1 ? 4 * kSets * kNT * 1024 : 0;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuffer > kSums ? 2 * kBuffer : kSums];
+    __shared__ int list[4][64];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t r0 = (int64_t)blockIdx.x * kRows;
-    const int rows = (int)(a.rows - r0 < kRows ? a.rows - r0 : kRows);
+    const int part = wave % kW;
+    const int64_t r0 = ((int64_t)blockIdx.x * (4 / kW) + wave / kW) * kRows;
+    const int rows = (int)(a.rows - r0 < 0 ? 0 : a.rows - r0 < kRows ? a.rows - r0 : kRows);
     const int K = (int)a.k;
 
-    int expert, count;
-    if (a.shares) {
-        const Share s = a.shares[blockIdx.y];
-        expert = s.expert, count = s.count;
-        if (count == 0) return;
-        if (tid < count) list[tid] = a.order[s.first + tid];
-    } else {
-        const int own = tid < a.slots ? expert_of(a.ids, a.experts, tid) : kNoExpert;
-        // As many blocks as slots: that of an expert's first slot.  Else one of each expert.
-        expert = a.slots <= a.experts ? expert_of(a.ids, a.experts, blockIdx.y) : (int)blockIdx.y;
-        if (expert == kNoExpert) return;
-        const uint64_t mask = __ballot(own == expert);
-        if (lane == 0) found[wave] = __popcll(mask);
-        __syncthreads();
-        int before = __popcll(mask & (((uint64_t)1 << lane) - 1));
-        count = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) before += found[w];
-            count += found[w];
-        }
-        if (own == expert) list[before] = tid;
-        __syncthreads();
-        if (count == 0 || (a.slots <= a.experts && list[0] != (int)blockIdx.y)) return;
-    }
-    __syncthreads();
-    expert = __builtin_amdgcn_readfirstlane(expert);
-    count = __builtin_amdgcn_readfirstlane(count);
+    Found own;
+    if (!own.find(a, blockIdx.y)) return;
+    const int expert = __builtin_amdgcn_readfirstlane(own.expert), count = __builtin_amdgcn_readfirstlane(own.count);
 
-    float f[2];
-    int e[2];
-    __amdgpu_buffer_rsrc_t rp[2], rc[2];
+    float f[2], two_e[2];
+    const uint8_t *packed[2], *codes[2];
 #pragma unroll
     for (int m = 0; m < kMats; ++m) {
-        split_device_scale(a.w[m].scale[expert], f[m], e[m]);
-        const int64_t row = (int64_t)expert * a.rows + r0;
-        rp[m] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.w[m].packed) + row * (K / 2), 0,
-                                                  rows * (K / 2), kRawWord3);
-        rc[m] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.w[m].codes) + row * (K / 16), 0,
-                                                  rows * (K / 16), kRawWord3);
+        split_device_scale(a.w[m].scale[expert], f[m], two_e[m]);
+        const int64_t row = (int64_t)expert * a.rows + (rows ? r0 : 0);
+        packed[m] = a.w[m].packed + row * (K / 2);
+        codes[m] = a.w[m].codes + row * (K / 16);
     }
-    const __amdgpu_buffer_rsrc_t rx =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.in), 0, (int)a.in_bytes, kRawWord3);
-    const uint32_t prow = (uint32_t)(l16 * (K / 2) + g * 16), crow = (uint32_t)(l16 * (K / 16) + g * 2);
+    const uint32_t prow = (uint32_t)(l16 * (K / 2) + g * 16), crow = (uint32_t)(l16 * (K / 16) + g * 16 * kW);
+    const int step0 = kDown ? (int)blockIdx.z * a.split : 0;
+    const int steps = kDown && step0 + a.split < (K + kStep - 1) / kStep ? step0 + a.split : (K + kStep - 1) / kStep;
+    const int rounds = (steps - step0 + kW - 1) / kW;
 
-    struct Weights {
-        u32x4 p[kSets];
-        uint32_t c[kSets];
+    struct Weights {  // of a row's 256 k: twice 32
+        u32x4 p[kSets][2];
     };
-    struct Inputs {
-        u32x4 x[kNT][kParts][4];
-    };
+    // What lies past the last k meets zeros of the slots' rows; steps past the
+    // last are not read.
     auto load_weights = [&](Weights &w, int step) {
-        const uint32_t k = step * kStep;
-        const uint32_t skip = (int)(k + g * 32) < K ? 0 : kNoRead;
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
             const int m = kDown ? 0 : s / kRT, tile = kDown ? s : s % kRT;
-            const uint32_t c = crow + tile * 16 * (K / 16) + k / 16 + skip;
-            w.p[s] = __builtin_amdgcn_raw_buffer_load_b128(rp[m], prow + tile * 16 * (K / 2) + k / 2 + skip, 0, 0);
-            if (kEven) {
-                w.c[s] = __builtin_amdgcn_raw_buffer_load_b16(rc[m], c, 0, 0);
+            const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<uint8_t *>(packed[m]) + step * (kStep / 2), 0,
+                step < steps ? rows * (K / 2) - step * (kStep / 2) : 0, kRawWord3);
+            const uint32_t p = prow + tile * 16 * (K / 2);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w.p[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rp, p + 64 * h, 0, 0);
+        }
+    };
+    struct Scales {  // of one of four steps
+        u32x4 c[kSets];
+    };
+    auto load_scales = [&](Scales &w, int step) {
+#pragma unroll
+        for (int s = 0; s < kSets; ++s) {
+            const int m = kDown ? 0 : s / kRT, tile = kDown ? s : s % kRT;
+            const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<uint8_t *>(codes[m]) + step * (kStep / 16), 0,
+                step < steps ? rows * (K / 16) - step * (kStep / 16) : 0, kRawWord3);
+            const uint32_t c = crow + tile * 16 * (K / 16);
+            if (kWords) {
+                w.c[s] = __builtin_amdgcn_raw_buffer_load_b128(rc, c, 0, 0);
             } else {
-                w.c[s] = __builtin_amdgcn_raw_buffer_load_b8(rc[m], c, 0, 0);
-                w.c[s] |= (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rc[m], c + 1, 0, 0) << 8;
+#pragma unroll
+                for (int b = 0; b < 16; ++b) {
+                    const uint32_t one = __builtin_amdgcn_raw_buffer_load_b8(rc, c + b, 0, 0);
+                    w.c[s][b / 4] = b % 4 ? w.c[s][b / 4] | one << (8 * (b % 4)) : one;
+                }
             }
         }
     };
-
-    const int steps = (K + kStep - 1) / kStep;
-    for (int c0 = 0; c0 < count; c0 += 16 * kNT) {
-        uint32_t xrow[kNT];
+    constexpr int kScaleRow = 80, kScaleSet = 16 * kScaleRow, kScales = 2 * kSets * kScaleSet;  // 64 bytes a row, in other banks
+    __shared__ __attribute__((aligned(16))) uint8_t scale_lds[4 * kScales];
+    uint8_t *scales = scale_lds + wave * kScales;
+    auto write_scales = [&](const Scales &w, int buffer) {
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-            const int i = c0 + n * 16 + l16;
-            xrow[n] = kNoRead;
-            if (i < count) xrow[n] = (uint32_t)((kDown ? list[i] : list[i] / a.choices) * a.ld * 2) + g * 64;
+        for (int s = 0; s < kSets; ++s)
+            *reinterpret_cast<u32x4 *>(scales + (buffer * kSets + s) * kScaleSet + l16 * kScaleRow + g * 16) = w.c[s];
+    };
+    const __amdgpu_buffer_rsrc_t rx =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.in), 0, (int)a.in_bytes, kRawWord3);
+
+    for (int c0 = 0; c0 < count; c0 += kTok) {
+        const int held = own.slot(a, c0, list[wave]);
+        // A thread's places in a buffer: chunk tid % 32 of row tid / 32 + 8 i, of step and part i / (kTok / 8).
+        constexpr int kOfRows = kTok > 8 ? kTok / 8 : 1;
+        uint32_t from[kOfRows];
+#pragma unroll
+        for (int i = 0; i < kOfRows; ++i) {
+            const int row = (tid >> 5) % kTok + 8 * i;
+            const int slot = row < 64 ? __shfl(held, row) : -1;
+            from[i] = slot < 0 ? kNoRead
+                               : (uint32_t)((kDown ? slot : slot / a.choices) * a.ld * 2) +
+                                     (((tid & 31) ^ (row & 15)) << 4);
         }
+        struct Rows {
+            u32x4 v[kCopies];
+        };
+        auto load_rows = [&](Rows &x, int round) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                // Units of kTok rows: the steps of the round, part by part.
+                const int unit = kTok < 8 ? (i * 8 + (tid >> 5)) / kTok : i / kOfRows, row8 = kTok < 8 ? 0 : i % kOfRows;
+                const int step = step0 + round * kW + unit / kParts;
+                const int chunk = (tid & 31) ^ (((tid >> 5) % kTok + 8 * row8) & 15);
+                const bool past = step * kStep + chunk * 8 >= K;
+                const uint32_t at = from[row8] + (uint32_t)(step * kRowBytes + unit % kParts * K * 2);
+                x.v[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, past || from[row8] == kNoRead ? kNoRead : at, 0, 0);
+            }
+        };
+        auto write_rows = [&](const Rows &x, int round) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                *reinterpret_cast<u32x4 *>(lds + (round & 1) * kBuffer + i * 4096 + tid * 16) = x.v[i];
+        };
         f32x4 acc[kSets][kNT];
 #pragma unroll
         for (int s = 0; s < kSets; ++s)
 #pragma unroll
             for (int n = 0; n < kNT; ++n) acc[s][n] = f32x4{0, 0, 0, 0};
-        auto load_inputs = [&](Inputs &x, int step) {
-            const int k = step * kStep + g * 32;
+
+        Weights w[2];
+        Scales c;
+        Rows x;
+        load_scales(c, step0 + part);
+        load_rows(x, 0);
+        load_weights(w[0], step0 + part);
+        write_scales(c, 0);
+        write_rows(x, 0);
+        load_rows(x, 1);
+        load_weights(w[1], step0 + kW + part);
+        own_writes_and_barrier();
+        const int row = l16 % kTok;
+        for (int first = 0; first < rounds; first += 4) {
+            const int buffer = first >> 2 & 1;
+            load_scales(c, step0 + (first + 4) * kW + part);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t skip = k + i * 8 < K ? 0 : kNoRead;
+            for (int d = 0; d < 4; ++d) {
+                const int round = first + d;
+                if (d > 0 && round >= rounds) break;
+                const uint8_t *buf = lds + (d & 1) * kBuffer + part * kParts * kStepBytes + row * kRowBytes;
+                const uint8_t *from = scales + buffer * kSets * kScaleSet + l16 * kScaleRow + d * 16 + g * 2;
+                uint32_t code[kSets][2];
 #pragma unroll
-                for (int n = 0; n < kNT; ++n)
+                for (int s = 0; s < kSets; ++s)
 #pragma unroll
-                    for (int p = 0; p < kParts; ++p) {
-                        const uint32_t at = xrow[n] + (uint32_t)(step * kStep * 2 + i * 16 + p * K * 2);
-                        x.x[n][p][i] = __builtin_amdgcn_raw_buffer_load_b128(rx, skip ? kNoRead : at, 0, 0);
-                    }
-            }
-        };
-        auto multiply = [&](const Weights &w, const Inputs &x) {
+                    for (int h = 0; h < 2; ++h)
+                        code[s][h] = *reinterpret_cast<const uint16_t *>(from + s * kScaleSet + 8 * h);
 #pragma unroll
-            for (int s = 0; s < kSets; ++s) {
-                const int m = kDown ? 0 : s / kRT;
-                const float l[2] = {scale_value(w.c[s] & 0x7F, e[m]), scale_value(w.c[s] >> 8 & 0x7F, e[m])};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 fw = __builtin_bit_cast(bf16x8, stored_eight(w.p[s][i], l[i >> 1]));
+                for (int i = 0; i < 8; ++i) {
+                    bf16x8 fx[kNT][kParts];
 #pragma unroll
                     for (int n = 0; n < kNT; ++n)
 #pragma unroll
                         for (int p = 0; p < kParts; ++p)
-                            acc[s][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                fw, __builtin_bit_cast(bf16x8, x.x[n][p][i]), acc[s][n], 0, 0, 0);
+                            fx[n][p] = *reinterpret_cast<const bf16x8 *>(
+                                buf + p * kStepBytes + n * 16 * kRowBytes + (((i / 4 * 16 + 4 * g + i % 4) ^ row) << 4));
+#pragma unroll
+                    for (int s = 0; s < kSets; ++s) {
+                        const float l = i & 2 ? __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 1)
+                                              : __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 0);
+                        const bf16x8 fw = __builtin_bit_cast(
+                            bf16x8, scaled_eight(w[d & 1].p[s][i / 4][i % 4], two_e[kDown ? 0 : s / kRT], l));
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                            for (int p = 0; p < kParts; ++p)
+                                acc[s][n] =
+                                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw, fx[n][p], acc[s][n], 0, 0, 0);
+                    }
                 }
-            }
-        };
-        // Loads past the last step read nothing.
-        Weights w[kDepth];
-        if constexpr (kNT * kParts <= 2) {
-            Inputs x[kDepth];
-#pragma unroll
-            for (int d = 0; d < kDepth; ++d) load_weights(w[d], wave + 4 * d), load_inputs(x[d], wave + 4 * d);
-            for (int step = wave; step < steps; step += 4 * kDepth) {
-#pragma unroll
-                for (int d = 0; d < kDepth; ++d) {
-                    multiply(w[d], x[d]);
-                    load_weights(w[d], step + 4 * (d + kDepth));
-                    load_inputs(x[d], step + 4 * (d + kDepth));
-                }
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < kDepth; ++d) load_weights(w[d], wave + 4 * d);
-            for (int step = wave; step < steps; step += 4 * kDepth) {
-#pragma unroll
-                for (int d = 0; d < kDepth; ++d) {
-                    Inputs x;
-                    load_inputs(x, step + 4 * d);
-                    multiply(w[d], x);
-                    load_weights(w[d], step + 4 * (d + kDepth));
-                }
+                write_rows(x, round + 1);
+                load_rows(x, round + 2);
+                load_weights(w[d & 1], step0 + (round + 2) * kW + part);
+                if (d == 3) write_scales(c, buffer ^ 1);
+                own_writes_and_barrier();
             }
         }
 
-        // The four quarters of k, then out: a lane holds four consecutive rows of a slot.
-        __syncthreads();
+        // A lane holds four consecutive rows of a slot.
+        int slot[kNT];
 #pragma unroll
-        for (int s = 0; s < kSets; ++s)
-#pragma unroll
-            for (int n = 0; n < kNT; ++n)
-                red[wave][s * kNT + n][lane] = make_float4(acc[s][n][0], acc[s][n][1], acc[s][n][2], acc[s][n][3]);
-        __syncthreads();
-        auto sum = [&](int unit) {
-            float4 v = red[0][unit][lane];
-#pragma unroll
-            for (int q = 1; q < 4; ++q) {
-                const float4 o = red[q][unit][lane];
-                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-            }
-            return v;
-        };
-        constexpr int kUnits = (kDown ? kSets : kRT) * kNT;
-        for (int u = wave; u < kUnits; u += 4) {
-            const int tile = u / kNT, i = c0 + (u % kNT) * 16 + l16;
-            const int row = tile * 16 + 4 * g;
-            if (i >= count || row >= rows) continue;
-            const int64_t slot = list[i];
+        for (int n = 0; n < kNT; ++n) slot[n] = n * 16 + l16 < kTok ? __shfl(held, n * 16 + l16) : -1;
+        auto out = [&](int s, int n, float4 v, float4 o) {
+            const int at = s * 16 + 4 * g;
+            if (slot[n] < 0 || at >= rows) return;
             if constexpr (kDown) {
-                const float4 v = sum(u);
-                const float by = a.weight[slot];
-                *reinterpret_cast<float4 *>(a.P + slot * a.rows + r0 + row) =
+                const float by = a.weight[slot[n]];
+                *reinterpret_cast<float4 *>(a.P + ((int64_t)blockIdx.z * a.slots + slot[n]) * a.rows + r0 + at) =
                     make_float4(v.x * f[0] * by, v.y * f[0] * by, v.z * f[0] * by, v.w * f[0] * by);
             } else {
-                const float4 vg = sum(u), vu = sum(kRT * kNT + u);
-                const float gate[4] = {vg.x * f[0], vg.y * f[0], vg.z * f[0], vg.w * f[0]};
-                const float up[4] = {vu.x * f[1], vu.y * f[1], vu.z * f[1], vu.w * f[1]};
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float h = gate[q] / (1.0f + expf(-gate[q])) * up[q];
-                    hi[q] = bf16_rne(h);
-                    const float rest = h - bf16_value(hi[q]);
-                    lo[q] = fabsf(rest) < INFINITY ? bf16_rne(rest) : 0;  // where h itself rounds to infinity
-                }
-                uint16_t *h = a.H + slot * 2 * a.rows + r0 + row;
-                *reinterpret_cast<uint2 *>(h) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                *reinterpret_cast<uint2 *>(h + a.rows) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                const float gate[4] = {v.x * f[0], v.y * f[0], v.z * f[0], v.w * f[0]};
+                const float up[4] = {o.x * f[1], o.y * f[1], o.z * f[1], o.w * f[1]};
+                store_hidden(a.H + (int64_t)slot[n] * 2 * a.rows + r0 + at, a.rows, gate, up);
             }
+        };
+        constexpr int kOuts = kDown ? kSets : kRT;  // tiles of 16 rows
+        auto four = [&](int s, int n) { return make_float4(acc[s][n][0], acc[s][n][1], acc[s][n][2], acc[s][n][3]); };
+        if constexpr (kW == 1) {
+#pragma unroll
+            for (int s = 0; s < kOuts; ++s)
+#pragma unroll
+                for (int n = 0; n < kNT; ++n) out(s, n, four(s, n), four(kDown ? s : kRT + s, n));
+        } else {
+            float4 *red = reinterpret_cast<float4 *>(lds);  // [4 waves][kSets * kNT][64]
+#pragma unroll
+            for (int s = 0; s < kSets; ++s)
+#pragma unroll
+                for (int n = 0; n < kNT; ++n) red[(wave * kSets * kNT + s * kNT + n) * 64 + lane] = four(s, n);
+            own_writes_and_barrier();
+            auto sum = [&](int unit) {
+                const float4 *from = red + (wave / kW * kW * kSets * kNT + unit) * 64 + lane;
+                float4 v = from[0];
+#pragma unroll
+                for (int q = 1; q < kW; ++q) {
+                    const float4 o = from[q * kSets * kNT * 64];
+                    v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                }
+                return v;
+            };
+#pragma unroll
+            for (int s = 0; s < kOuts; ++s)
+#pragma unroll
+                for (int n = 0; n < kNT; ++n)
+                    if ((s * kNT + n) % kW == part)
+                        out(s, n, sum(s * kNT + n), kDown ? float4{} : sum((kRT + s) * kNT + n));
+            own_writes_and_barrier();
         }
-        __syncthreads();
     }
 }
 
-// Y[t] = the sum of the token's slots in their order; eight outputs a thread.
-// A slot without an expert adds its weight times 0.
-__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, const int32_t *__restrict__ ids,
-                                                   const float *__restrict__ weight, int choices, int experts,
-                                                   int64_t out, uint16_t *__restrict__ Y, int64_t ldy, bool wide) {
+// Y[t] = the sum of the token's slots in their order, each over the splits of k;
+// eight outputs a thread.  A slot without an expert adds its weight times 0.
+__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, int splits, int64_t slots,
+                                                   const int32_t *__restrict__ ids, const float *__restrict__ weight,
+                                                   int choices, int experts, int64_t out, uint16_t *__restrict__ Y,
+                                                   int64_t ldy, bool wide) {
     const int64_t t = blockIdx.y, m = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (m >= out) return;
     float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -409,10 +520,13 @@ __global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, 
             for (int i = 0; i < 8; ++i) y[i] += weight[s] * 0.0f;
             continue;
         }
-        const float4 a = *reinterpret_cast<const float4 *>(P + s * out + m);
-        const float4 b = *reinterpret_cast<const float4 *>(P + s * out + m + 4);
-        y[0] += a.x, y[1] += a.y, y[2] += a.z, y[3] += a.w;
-        y[4] += b.x, y[5] += b.y, y[6] += b.z, y[7] += b.w;
+#pragma unroll 4
+        for (int z = 0; z < splits; ++z) {
+            const float *p = P + (z * slots + s) * out + m;
+            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+            y[0] += a.x, y[1] += a.y, y[2] += a.z, y[3] += a.w;
+            y[4] += b.x, y[5] += b.y, y[6] += b.z, y[7] += b.w;
+        }
     }
     uint16_t *dst = Y + t * ldy + m;
     const u32x4 v{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])};
@@ -443,6 +557,9 @@ int64_t piece_tokens(int64_t hidden, int32_t k, int64_t ldx) {
     return std::max<int64_t>(1, std::min(n, ((int64_t)1 << 28) / (hidden * k)));
 }
 
+constexpr int kDownSplits = 16;
+constexpr int64_t kSplitBytes = (int64_t)32 << 20;  // of their sums, unless one takes more
+
 struct LayerSpace {
     size_t h, p, order, shares, total;
 };
@@ -451,7 +568,8 @@ LayerSpace layer_space(int64_t tokens, int64_t in, int64_t hidden, int32_t exper
     const int64_t slots = std::min(tokens, piece_tokens(hidden, k, 1)) * k;
     LayerSpace s{};
     s.h = round_256((size_t)(slots * hidden * 4));
-    s.p = round_256((size_t)(slots * in * 4));
+    // Splits of few tokens are more: a bound that does not fall with the tokens.
+    s.p = round_256((size_t)std::min(slots * in * 4 * kDownSplits, std::max(slots * in * 4, kSplitBytes)));
     s.order = round_256((size_t)slots * 4);
     s.shares = round_256((size_t)(slots + experts) * sizeof(Share));
     s.total = s.h + s.p + s.order + s.shares;
@@ -466,26 +584,48 @@ int check_matrix(const hscale_experts *w) {
 
 Matrices matrices(const hscale_experts *w) { return Matrices{w->global_scale, w->scale_codes, w->packed_e2m1}; }
 
-template <bool kDown, int kRT, int kNT>
-void launch_experts(const ExpertArgs &a, int shares, bool even, hipStream_t stream) {
-    const dim3 grid((unsigned)cdiv(a.rows, (kDown ? 32 : 16) * kRT), (unsigned)shares);
-    if (even)
-        hipLaunchKernelGGL((expert_kernel<kDown, kRT, kNT, true>), grid, dim3(256), 0, stream, a);
+template <bool kDown, int kTok, int kRT, int kW>
+int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
+    const dim3 grid((unsigned)cdiv(a.rows, (kDown ? 32 : 16) * kRT * (4 / kW)), (unsigned)shares, (unsigned)splits);
+    bool words = a.k % 64 == 0;
+    for (int m = 0; m < (kDown ? 1 : 2); ++m) words = words && aligned(a.w[m].codes, 4);
+    if (words)
+        hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, true>), grid, dim3(256), 0, stream, a);
     else
-        hipLaunchKernelGGL((expert_kernel<kDown, kRT, kNT, false>), grid, dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, false>), grid, dim3(256), 0, stream, a);
+    return launch_status();
 }
 
-template <bool kDown>
-int experts_product(const ExpertArgs &a, int shares, int tiles, hipStream_t stream) {
-    bool even = a.k % 32 == 0;
-    for (int m = 0; m < (kDown ? 1 : 2); ++m) even = even && aligned(a.w[m].codes, 2);
-    if (tiles == 1)
-        launch_experts<kDown, 1, 1>(a, shares, even, stream);
-    else if (tiles == 2)
-        launch_experts<kDown, 1, 2>(a, shares, even, stream);
-    else
-        launch_experts<kDown, 2, 4>(a, shares, even, stream);
-    return launch_status();
+// A wave alone has its rows where there are many; with fewer, two or four share
+// them.
+int gate_and_up(const ExpertArgs &a, int shares, int tile, hipStream_t stream) {
+    const int64_t units = cdiv(a.rows, 16) * shares;
+    if (tile == 4) return launch_experts<false, 4, 1, 4>(a, shares, 1, stream);
+    if (tile == 16)
+        return units >= 4096   ? launch_experts<false, 16, 1, 1>(a, shares, 1, stream)
+               : units >= 2048 ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
+                               : launch_experts<false, 16, 1, 4>(a, shares, 1, stream);
+    if (tile == 32) return launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
+    return launch_experts<false, 64, 2, 1>(a, shares, 1, stream);
+}
+
+int down_product(const ExpertArgs &a, int shares, int tile, int splits, hipStream_t stream) {
+    if (tile == 4) return launch_experts<true, 4, 1, 1>(a, shares, splits, stream);
+    if (tile == 16) return launch_experts<true, 16, 1, 1>(a, shares, splits, stream);
+    if (tile == 32) return launch_experts<true, 32, 1, 1>(a, shares, splits, stream);
+    return launch_experts<true, 64, 1, 1>(a, shares, splits, stream);
+}
+
+// Splits of the down product's k, for `shares` shares of experts: two blocks a CU
+// (37 tokens over 8 experts of 4096 x 14336, 256 blocks: 192 us in two splits, 204
+// in one, 197 in four; one token over two of them, 64 blocks: 64 us in eight, 66 in
+// four, 110 in one).
+int down_splits(int64_t slots, int64_t in, int64_t hidden, int64_t shares) {
+    const int64_t steps = cdiv(hidden, 256), blocks = cdiv(in, 128) * shares;
+    int64_t n = cdiv(512, blocks);
+    n = std::min({n, steps, (int64_t)kDownSplits, std::max<int64_t>(1, kSplitBytes / (slots * in * 4))});
+    n = std::max<int64_t>(1, n);
+    return (int)cdiv(steps, cdiv(steps, n));
 }
 
 }  // namespace
@@ -574,13 +714,13 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         const int64_t n = std::min(piece, tokens - t0);
         const int slots = (int)(n * k);
         const int32_t *ids = expert + t0 * k;
-        // Columns of 16 slots: as many as an expert's share, on average, is likely to need.
-        const int tiles = slots <= 2 * experts ? 1 : slots <= 16 * experts ? 2 : 4;
+        // Slots of a block: as many as an expert's share, on average, is likely to need.
+        const int tile = n <= 4 ? 4 : slots <= 12 * experts ? 16 : slots <= 28 * experts ? 32 : 64;
         int count = std::min(slots, (int)experts);
         const bool many = slots > kBlockSlots;
         if (many) {
-            count = std::min(slots, slots / (16 * tiles) + (int)experts);
-            hipLaunchKernelGGL(share_kernel, dim3(1), dim3(1024), 0, stream, ids, slots, (int)experts, 16 * tiles,
+            count = std::min(slots, slots / tile + (int)experts);
+            hipLaunchKernelGGL(share_kernel, dim3(1), dim3(1024), 0, stream, ids, slots, (int)experts, tile,
                                order, shares, count);
             if (const int st = launch_status()) return st;
         }
@@ -598,16 +738,18 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         a.shares = many ? shares : nullptr;
         a.H = H;
         a.P = P;
-        if (const int st = experts_product<false>(a, count, tiles, stream)) return st;
+        if (const int st = gate_and_up(a, count, tile, stream)) return st;
         a.w[0] = a.w[1] = matrices(down);
         a.rows = in, a.k = hidden;
         a.in = H;
         a.ld = 2 * hidden;
         a.in_bytes = (int64_t)slots * hidden * 4;
-        if (const int st = experts_product<true>(a, count, tiles, stream)) return st;
+        const int splits = down_splits(slots, in, hidden, count);
+        a.split = (int)cdiv(cdiv(hidden, 256), splits);
+        if (const int st = down_product(a, count, tile, splits, stream)) return st;
         uint16_t *y = static_cast<uint16_t *>(Y) + t0 * ldy;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 2048), (unsigned)n), dim3(256), 0, stream, P, ids,
-                           a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 16) && ldy % 8 == 0);
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 2048), (unsigned)n), dim3(256), 0, stream, P, splits,
+                           (int64_t)slots, ids, a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 16) && ldy % 8 == 0);
         if (const int st = launch_status()) return st;
     }
     return HSCALE_OK;

@@ -24,4 +24,17 @@ __device__ __forceinline__ u32x4 stored_eight(uint32_t src, float l) {
     return u32x4{stored_pair<0>(src, l), stored_pair<1>(src, l), stored_pair<2>(src, l), stored_pair<3>(src, l)};
 }
 
+// The same with 2^e on the values' side, where the conversion multiplies by it
+// at no cost: `two_e` is 2^e, `l` an E4M3 value.
+template <int K>
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t src, float two_e, float l) {
+    const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(src, two_e, K);
+    return __builtin_amdgcn_perm(__float_as_uint(v[1] * l), __float_as_uint(v[0] * l), 0x07060302);
+}
+
+__device__ __forceinline__ u32x4 scaled_eight(uint32_t src, float two_e, float l) {
+    return u32x4{scaled_pair<0>(src, two_e, l), scaled_pair<1>(src, two_e, l), scaled_pair<2>(src, two_e, l),
+                 scaled_pair<3>(src, two_e, l)};
+}
+
 }  // namespace

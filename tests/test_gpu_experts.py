@@ -83,7 +83,8 @@ def test_pieces(hs):
 
 
 def test_a_token_does_not_depend_on_its_neighbours(hs):
-    """The same bits alone, among others, at every size of the call's tiles and in any order."""
+    """The same bits alone, among others, at every size of the call's tiles and in
+    any order, for widths up to 256, which no call splits."""
     p = _problem(600, 144, 112, 12, 3)
     whole = hs.expert_layer(**p)
     for a, b in ((0, 1), (0, 5), (7, 60), (100, 200), (599, 600)):
