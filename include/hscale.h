@@ -669,7 +669,7 @@ typedef struct hscale_logit_rules {
     int64_t history_ld;
     const int32_t *length;   /* int32 [rows]: how many of them count; NULL: all */
     const int32_t *prompt;   /* int32 [rows]: how many of these are the prompt's; NULL: none */
-    const float *repetition; /* fp32 [rows], > 0 */
+    const float *repetition; /* fp32 [rows], normal and > 0 */
     const float *frequency;  /* fp32 [rows] */
     const float *presence;   /* fp32 [rows] */
     const float *bias;       /* fp32 [biases, vocab] */
@@ -683,7 +683,7 @@ typedef struct hscale_logit_rules {
 /*
  * Penalties for repeated words, biases and masks on logits, in this order and
  * in fp32, each step rounded once:
- *   l = l > 0 ? l / repetition : l * repetition    if v is in the history
+ *   l = l * (l > 0 ? fp32(1 / repetition) : repetition)   if v is in the history
  *   l = l - frequency * count - presence           if it is in the answer,
  *       the history behind its prompt, `count` times
  *   l = l + bias[v]

@@ -164,12 +164,11 @@ def load() -> ctypes.CDLL:
     lib.hscale_token_loss_grad_workspace_bytes.restype = sz
     lib.hscale_token_loss_grad.argtypes = [P, i64, i64, i64, P, i64, P, P, P, P, i64, P, P, sz, P]
     lib.hscale_token_loss_grad.restype = ctypes.c_int
-    EX = ctypes.POINTER(HScaleExperts)
     lib.hscale_route_tokens.argtypes = [P, i32, i64, i32, i64, i32, i32, P, P, P]
     lib.hscale_route_tokens.restype = ctypes.c_int
     lib.hscale_expert_layer_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
     lib.hscale_expert_layer_workspace_bytes.restype = sz
-    lib.hscale_expert_layer.argtypes = [P, i64, i64, i64, i64, i32, EX, EX, EX, P, P, i32, P, i64, P, sz, P]
+    lib.hscale_expert_layer.argtypes = [P, i64, i64, i64, i64, i32, P, P, P, P, P, i32, P, i64, P, sz, P]
     lib.hscale_expert_layer.restype = ctypes.c_int
     lib.hscale_adjust_logits.argtypes = [ctypes.POINTER(HScaleLogitRules), P, i32, i64, i64, i64, P, i64, P]
     lib.hscale_adjust_logits.restype = ctypes.c_int
@@ -356,21 +355,23 @@ def hscale_route_tokens(logits: int, type_: int, tokens: int, experts: int, ld: 
                                                 stream)
 
 
-def _experts(matrix):
-    """A pointer to struct hscale_experts of (global_scale, scale_codes, packed_e2m1), or NULL for None."""
-    return None if matrix is None else ctypes.byref(HScaleExperts(*matrix))
-
-
 def hscale_expert_layer_workspace_bytes(tokens: int, in_: int, hidden: int, experts: int, k: int) -> int:
     return (_lib or load()).hscale_expert_layer_workspace_bytes(tokens, in_, hidden, experts, k)
+
+
+_ThreeExperts = HScaleExperts * 3
+_EXPERTS_BYTES = ctypes.sizeof(HScaleExperts)
 
 
 def hscale_expert_layer(X: int, tokens: int, in_: int, ldx: int, hidden: int, experts: int, gate, up, down,
                         expert: int, weight: int, k: int, Y: int, ldy: int, workspace: int, workspace_bytes: int,
                         stream: int) -> int:
-    return (_lib or load()).hscale_expert_layer(X, tokens, in_, ldx, hidden, experts, _experts(gate), _experts(up),
-                                                _experts(down), expert, weight, k, Y, ldy, workspace,
-                                                workspace_bytes, stream)
+    """gate, up, down: (global_scale, scale_codes, packed_e2m1) as addresses, or None for NULL."""
+    m = _ThreeExperts(gate or (), up or (), down or ())
+    at = ctypes.addressof(m)
+    return (_lib or load()).hscale_expert_layer(X, tokens, in_, ldx, hidden, experts, at if gate else 0,
+                                                at + _EXPERTS_BYTES if up else 0, at + 2 * _EXPERTS_BYTES if down else 0,
+                                                expert, weight, k, Y, ldy, workspace, workspace_bytes, stream)
 
 
 def hscale_adjust_logits(rules, logits: int, type_: int, rows: int, vocab: int, ld: int, out: int, ldo: int,

@@ -32,16 +32,41 @@ constexpr int kNoExpert = -1;
 // Routing
 // ---------------------------------------------------------------------------
 
-// A number that orders as (logit, lowest index first), 0 for what is never
-// chosen: -inf and NaN.  -0 and +0 are equal.
-__device__ __forceinline__ uint64_t choice_key(float l, int e) {
+// A number that orders as the logit does, 0 for what is never chosen: -inf and
+// NaN.  -0 and +0 are equal.
+__device__ __forceinline__ uint32_t choice_key(float l) {
     if (!(l > -INFINITY)) return 0;
     const uint32_t u = __float_as_uint(l + 0.0f);
-    return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~e;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// The largest of a wave's numbers, in all its lanes: within 16 lanes, then over
+// the rows of 16.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    uint32_t o;
+#define MAX_OF(ctrl, rows)                                                                          \
+    o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false);                   \
+    v = o > v ? o : v
+    MAX_OF(0x111, 0xF);  // row_shr:1, 2, 4, 8
+    MAX_OF(0x112, 0xF);
+    MAX_OF(0x114, 0xF);
+    MAX_OF(0x118, 0xF);
+    MAX_OF(0x142, 0xA);  // row_bcast:15, 31
+    MAX_OF(0x143, 0xC);
+#undef MAX_OF
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
 }
 
 // A wave per token, kN logits a lane.  k rounds of the wave's largest key, each
-// taken out where it lies; the softmax is relative to the first.
+// taken out where it first lies; the softmax is relative to the first.  Latency
+// bounds it: 48 tokens of 64 experts take 2.9 us, 8190 of 160 7.1
+// (4.3 and 13.7 with the largest key by shuffles of 64 bits).
 template <int kN, bool kWide>
 __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ logits, int64_t tokens, int experts,
                                                     int64_t ld, int k, bool normalize, int32_t *__restrict__ expert,
@@ -50,7 +75,7 @@ __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ log
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= tokens) return;
     float l[kN];
-    uint64_t key[kN];
+    uint32_t key[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
         const int e = i * 64 + lane;
@@ -58,39 +83,41 @@ __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ log
         if (e < experts)
             l[i] = kWide ? static_cast<const float *>(logits)[t * ld + e]
                          : bf16_value(static_cast<const uint16_t *>(logits)[t * ld + e]);
-        key[i] = choice_key(l[i], e);
     }
-    float top = 0.0f, all = 0.0f, some = 0.0f, mine = 0.0f;
-    int which = kNoExpert;  // lane j holds the j-th choice
+#pragma unroll
+    for (int i = 0; i < kN; ++i) key[i] = choice_key(l[i]);
+    uint32_t mine = 0;      // lane j holds the j-th choice
+    int which = kNoExpert;
     for (int j = 0; j < k; ++j) {
-        uint64_t best = 0;
+        uint32_t best = key[0];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) best = key[i] > best ? key[i] : best;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint64_t other = __shfl_xor((unsigned long long)best, o);
-            best = other > best ? other : best;
-        }
+        for (int i = 1; i < kN; ++i) best = key[i] > best ? key[i] : best;
+        best = wave_max(best);
         if (best == 0) break;  // fewer than k can be chosen
+        int at = -1;
 #pragma unroll
-        for (int i = 0; i < kN; ++i)
-            if (key[i] == best) key[i] = 0;
-        const uint32_t u = (uint32_t)(best >> 32);
-        const float v = __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
-        if (j == 0) top = v;
-        const float p = expf(v - top);
-        some += p;
-        if (lane == j) which = (int)~(uint32_t)best, mine = p;
+        for (int i = 0; i < kN; ++i) {
+            const uint64_t mask = __ballot(key[i] == best);
+            if (at < 0 && mask) {
+                at = i * 64 + __builtin_ctzll(mask);
+                if (lane == (at & 63)) key[i] = 0;
+            }
+        }
+        if (lane == j) mine = best, which = at;
     }
+    const float v = __uint_as_float(mine & 0x80000000u ? mine & 0x7FFFFFFFu : ~mine);
+    const float top = which == kNoExpert ? 0.0f : v, first = __shfl(top, 0);
+    const float p = which == kNoExpert ? 0.0f : expf(v - first);
     // Over all experts too where the k alone are asked for: a NaN anywhere shows.
+    float all = 0.0f;
 #pragma unroll
     for (int i = 0; i < kN; ++i)
-        if (!(l[i] == -INFINITY)) all += expf(l[i] - top);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+        if (!(l[i] == -INFINITY)) all += expf(l[i] - first);
+    all = wave_sum(all);
+    const float some = wave_sum(p);
     if (lane >= k) return;
     expert[t * k + lane] = which;
-    weight[t * k + lane] = all != all ? all : which == kNoExpert ? 0.0f : mine / (normalize ? some : all);
+    weight[t * k + lane] = all != all ? all : which == kNoExpert ? 0.0f : p / (normalize ? some : all);
 }
 
 // ---------------------------------------------------------------------------
@@ -270,11 +297,12 @@ __device__ __forceinline__ void own_writes_and_barrier() {  // loads stay under 
 // read back from LDS two at a time: as 2-byte loads for each step they took a
 // quarter of the time (64 tokens of 4096 over 128 experts of 1536: 363 us with
 // them, 275 without any scales).
-template <bool kDown, int kTok, int kRT, int kW, bool kWords>  // kWords: rows of scales are whole aligned words
-__global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
+template <bool kDown, int kTok, int kRT, int kW, int kStep, bool kWords>  // kWords: rows of scales are whole aligned words
+__global__ __launch_bounds__(256, 2) void expert_kernel(const ExpertArgs a) {
     constexpr int kNT = (kTok + 15) / 16, kSets = 2 * kRT, kMats = kDown ? 1 : 2, kParts = kDown ? 2 : 1;
     constexpr int kRows = kDown ? 32 * kRT : 16 * kRT;  // of a wave
-    constexpr int kStep = 256, kRowBytes = kStep * 2, kStepBytes = kTok * kRowBytes;
+    constexpr int kHalves = kStep / 128, kRowBytes = kStep * 2, kStepBytes = kTok * kRowBytes;
+    constexpr int kRowLanes = kStep / 8, kCopyRows = 256 / kRowLanes;  // threads of a row, rows of a copy
     constexpr int kBuffer = kW * kParts * kStepBytes, kCopies = kBuffer / 4096;  // 16 bytes a thread
     static_assert(kBuffer % 4096 == 0, "whole copies");
     constexpr int kSums = kW > 1 ? 4 * kSets * kNT * 1024 : 0;
@@ -300,13 +328,13 @@ __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
         packed[m] = a.w[m].packed + row * (K / 2);
         codes[m] = a.w[m].codes + row * (K / 16);
     }
-    const uint32_t prow = (uint32_t)(l16 * (K / 2) + g * 16), crow = (uint32_t)(l16 * (K / 16) + g * 16 * kW);
+    const uint32_t prow = (uint32_t)(l16 * (K / 2) + g * 16), crow = (uint32_t)(l16 * (K / 16) + g * (kStep / 16) * kW);
     const int step0 = kDown ? (int)blockIdx.z * a.split : 0;
     const int steps = kDown && step0 + a.split < (K + kStep - 1) / kStep ? step0 + a.split : (K + kStep - 1) / kStep;
     const int rounds = (steps - step0 + kW - 1) / kW;
 
-    struct Weights {  // of a row's 256 k: twice 32
-        u32x4 p[kSets][2];
+    struct Weights {  // 32 of each 128 of a row's
+        u32x4 p[kSets][kHalves];
     };
     // What lies past the last k meets zeros of the slots' rows; steps past the
     // last are not read.
@@ -319,11 +347,11 @@ __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
                 step < steps ? rows * (K / 2) - step * (kStep / 2) : 0, kRawWord3);
             const uint32_t p = prow + tile * 16 * (K / 2);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w.p[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rp, p + 64 * h, 0, 0);
+            for (int h = 0; h < kHalves; ++h) w.p[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rp, p + 64 * h, 0, 0);
         }
     };
     struct Scales {  // of one of four steps
-        u32x4 c[kSets];
+        uint32_t c[kSets][kStep / 64];
     };
     auto load_scales = [&](Scales &w, int step) {
 #pragma unroll
@@ -333,40 +361,46 @@ __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
                 const_cast<uint8_t *>(codes[m]) + step * (kStep / 16), 0,
                 step < steps ? rows * (K / 16) - step * (kStep / 16) : 0, kRawWord3);
             const uint32_t c = crow + tile * 16 * (K / 16);
-            if (kWords) {
-                w.c[s] = __builtin_amdgcn_raw_buffer_load_b128(rc, c, 0, 0);
+            if (kWords && kHalves == 2) {
+                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rc, c, 0, 0);
+#pragma unroll
+                for (int q = 0; q < kStep / 64; ++q) w.c[s][q] = v[q];
+            } else if (kWords) {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(rc, c, 0, 0);
+                w.c[s][0] = v[0], w.c[s][1] = v[1];
             } else {
 #pragma unroll
-                for (int b = 0; b < 16; ++b) {
+                for (int b = 0; b < kStep / 16; ++b) {
                     const uint32_t one = __builtin_amdgcn_raw_buffer_load_b8(rc, c + b, 0, 0);
                     w.c[s][b / 4] = b % 4 ? w.c[s][b / 4] | one << (8 * (b % 4)) : one;
                 }
             }
         }
     };
-    constexpr int kScaleRow = 80, kScaleSet = 16 * kScaleRow, kScales = 2 * kSets * kScaleSet;  // 64 bytes a row, in other banks
-    __shared__ __attribute__((aligned(16))) uint8_t scale_lds[4 * kScales];
-    uint8_t *scales = scale_lds + wave * kScales;
-    auto write_scales = [&](const Scales &w, int buffer) {
+    constexpr int kScaleRow = kStep / 4 + kStep / 16, kScaleSet = 16 * kScaleRow;  // a row in other banks than its neighbours
+    __shared__ __attribute__((aligned(16))) uint8_t scale_lds[4 * kSets * kScaleSet];
+    uint8_t *scales = scale_lds + wave * kSets * kScaleSet;  // the wave's own
+    auto write_scales = [&](const Scales &w) {
 #pragma unroll
         for (int s = 0; s < kSets; ++s)
-            *reinterpret_cast<u32x4 *>(scales + (buffer * kSets + s) * kScaleSet + l16 * kScaleRow + g * 16) = w.c[s];
+            __builtin_memcpy(__builtin_assume_aligned(scales + s * kScaleSet + l16 * kScaleRow + g * (kStep / 16), kStep / 16),
+                             w.c[s], kStep / 16);
     };
     const __amdgpu_buffer_rsrc_t rx =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.in), 0, (int)a.in_bytes, kRawWord3);
 
     for (int c0 = 0; c0 < count; c0 += kTok) {
         const int held = own.slot(a, c0, list[wave]);
-        // A thread's places in a buffer: chunk tid % 32 of row tid / 32 + 8 i, of step and part i / (kTok / 8).
-        constexpr int kOfRows = kTok > 8 ? kTok / 8 : 1;
+        // A thread's places in a buffer: a chunk of rows tid / kRowLanes, kCopyRows further on, ...
+        constexpr int kOfRows = kTok > kCopyRows ? kTok / kCopyRows : 1;  // copies of a step's rows
+        const int chunk0 = tid % kRowLanes, row0 = tid / kRowLanes;
         uint32_t from[kOfRows];
 #pragma unroll
         for (int i = 0; i < kOfRows; ++i) {
-            const int row = (tid >> 5) % kTok + 8 * i;
-            const int slot = row < 64 ? __shfl(held, row) : -1;
+            const int row = row0 % kTok + kCopyRows * i;
+            const int slot = __shfl(held, row);
             from[i] = slot < 0 ? kNoRead
-                               : (uint32_t)((kDown ? slot : slot / a.choices) * a.ld * 2) +
-                                     (((tid & 31) ^ (row & 15)) << 4);
+                               : (uint32_t)((kDown ? slot : slot / a.choices) * a.ld * 2) + ((chunk0 ^ (row & 15)) << 4);
         }
         struct Rows {
             u32x4 v[kCopies];
@@ -375,12 +409,12 @@ __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) {
                 // Units of kTok rows: the steps of the round, part by part.
-                const int unit = kTok < 8 ? (i * 8 + (tid >> 5)) / kTok : i / kOfRows, row8 = kTok < 8 ? 0 : i % kOfRows;
+                const int unit = kTok < kCopyRows ? (i * kCopyRows + row0) / kTok : i / kOfRows, of = i % kOfRows;
                 const int step = step0 + round * kW + unit / kParts;
-                const int chunk = (tid & 31) ^ (((tid >> 5) % kTok + 8 * row8) & 15);
+                const int chunk = chunk0 ^ ((row0 % kTok + kCopyRows * of) & 15);
                 const bool past = step * kStep + chunk * 8 >= K;
-                const uint32_t at = from[row8] + (uint32_t)(step * kRowBytes + unit % kParts * K * 2);
-                x.v[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, past || from[row8] == kNoRead ? kNoRead : at, 0, 0);
+                const uint32_t at = from[of] + (uint32_t)(step * kRowBytes + unit % kParts * K * 2);
+                x.v[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, past || from[of] == kNoRead ? kNoRead : at, 0, 0);
             }
         };
         auto write_rows = [&](const Rows &x, int round) {
@@ -397,57 +431,65 @@ __global__ __launch_bounds__(256) void expert_kernel(const ExpertArgs a) {
         Weights w[2];
         Scales c;
         Rows x;
+        // Loads are waited for in the order in which they were issued: what the
+        // loop's first round needs comes first.
         load_scales(c, step0 + part);
         load_rows(x, 0);
         load_weights(w[0], step0 + part);
-        write_scales(c, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        write_scales(c);
         write_rows(x, 0);
         load_rows(x, 1);
+        __builtin_amdgcn_sched_barrier(0);
         load_weights(w[1], step0 + kW + part);
         own_writes_and_barrier();
         const int row = l16 % kTok;
         for (int first = 0; first < rounds; first += 4) {
-            const int buffer = first >> 2 & 1;
             load_scales(c, step0 + (first + 4) * kW + part);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 const int round = first + d;
-                if (d > 0 && round >= rounds) break;
-                const uint8_t *buf = lds + (d & 1) * kBuffer + part * kParts * kStepBytes + row * kRowBytes;
-                const uint8_t *from = scales + buffer * kSets * kScaleSet + l16 * kScaleRow + d * 16 + g * 2;
-                uint32_t code[kSets][2];
+                if (d == 0 || round < rounds) {  // a branch that jumps over no load leaves their order known
+                    const uint8_t *buf = lds + (d & 1) * kBuffer + part * kParts * kStepBytes + row * kRowBytes;
+                    const uint8_t *from = scales + l16 * kScaleRow + d * (kStep / 16) + g * 2;
+                    uint32_t code[kSets][kHalves];
 #pragma unroll
-                for (int s = 0; s < kSets; ++s)
+                    for (int s = 0; s < kSets; ++s)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        code[s][h] = *reinterpret_cast<const uint16_t *>(from + s * kScaleSet + 8 * h);
+                        for (int h = 0; h < kHalves; ++h)
+                            code[s][h] = *reinterpret_cast<const uint16_t *>(from + s * kScaleSet + 8 * h);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    bf16x8 fx[kNT][kParts];
-#pragma unroll
-                    for (int n = 0; n < kNT; ++n)
-#pragma unroll
-                        for (int p = 0; p < kParts; ++p)
-                            fx[n][p] = *reinterpret_cast<const bf16x8 *>(
-                                buf + p * kStepBytes + n * 16 * kRowBytes + (((i / 4 * 16 + 4 * g + i % 4) ^ row) << 4));
-#pragma unroll
-                    for (int s = 0; s < kSets; ++s) {
-                        const float l = i & 2 ? __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 1)
-                                              : __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 0);
-                        const bf16x8 fw = __builtin_bit_cast(
-                            bf16x8, scaled_eight(w[d & 1].p[s][i / 4][i % 4], two_e[kDown ? 0 : s / kRT], l));
+                    for (int i = 0; i < kStep / 32; ++i) {
+                        bf16x8 fx[kNT][kParts];
 #pragma unroll
                         for (int n = 0; n < kNT; ++n)
 #pragma unroll
                             for (int p = 0; p < kParts; ++p)
-                                acc[s][n] =
-                                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw, fx[n][p], acc[s][n], 0, 0, 0);
+                                fx[n][p] = *reinterpret_cast<const bf16x8 *>(
+                                    buf + p * kStepBytes + n * 16 * kRowBytes +
+                                    (((i / 4 * 16 + 4 * g + i % 4) ^ row) << 4));
+#pragma unroll
+                        for (int s = 0; s < kSets; ++s) {
+                            const float l = i & 2 ? __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 1)
+                                                  : __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 0);
+                            const bf16x8 fw = __builtin_bit_cast(
+                                bf16x8, scaled_eight(w[d & 1].p[s][i / 4][i % 4], two_e[kDown ? 0 : s / kRT], l));
+#pragma unroll
+                            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                                for (int p = 0; p < kParts; ++p)
+                                    acc[s][n] =
+                                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw, fx[n][p], acc[s][n], 0, 0, 0);
+                        }
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
                 write_rows(x, round + 1);
                 load_rows(x, round + 2);
+                __builtin_amdgcn_sched_barrier(0);
                 load_weights(w[d & 1], step0 + (round + 2) * kW + part);
-                if (d == 3) write_scales(c, buffer ^ 1);
+                if (d == 3) write_scales(c);
                 own_writes_and_barrier();
             }
         }
@@ -584,16 +626,23 @@ int check_matrix(const hscale_experts *w) {
 
 Matrices matrices(const hscale_experts *w) { return Matrices{w->global_scale, w->scale_codes, w->packed_e2m1}; }
 
-template <bool kDown, int kTok, int kRT, int kW>
-int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
+// Whether rows of scales are whole aligned words.
+template <bool kDown>
+bool whole_words(const ExpertArgs &a) {
+    return a.k % 64 == 0 && aligned(a.w[0].codes, 4) && (kDown || aligned(a.w[1].codes, 4));
+}
+
+template <bool kDown, int kTok, int kRT, int kW, int kStep, bool kWords>
+int launch_one(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
     const dim3 grid((unsigned)cdiv(a.rows, (kDown ? 32 : 16) * kRT * (4 / kW)), (unsigned)shares, (unsigned)splits);
-    bool words = a.k % 64 == 0;
-    for (int m = 0; m < (kDown ? 1 : 2); ++m) words = words && aligned(a.w[m].codes, 4);
-    if (words)
-        hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, true>), grid, dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, false>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, kStep, kWords>), grid, dim3(256), 0, stream, a);
     return launch_status();
+}
+
+template <bool kDown, int kTok, int kRT, int kW, int kStep = 256>
+int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
+    return whole_words<kDown>(a) ? launch_one<kDown, kTok, kRT, kW, kStep, true>(a, shares, splits, stream)
+                                 : launch_one<kDown, kTok, kRT, kW, kStep, false>(a, shares, splits, stream);
 }
 
 // A wave alone has its rows where there are many; with fewer, two or four share
@@ -606,14 +655,15 @@ int gate_and_up(const ExpertArgs &a, int shares, int tile, hipStream_t stream) {
                : units >= 2048 ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
                                : launch_experts<false, 16, 1, 4>(a, shares, 1, stream);
     if (tile == 32) return launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
-    return launch_experts<false, 64, 2, 1>(a, shares, 1, stream);
+    return launch_experts<false, 64, 2, 1, 128>(a, shares, 1, stream);
 }
 
 int down_product(const ExpertArgs &a, int shares, int tile, int splits, hipStream_t stream) {
     if (tile == 4) return launch_experts<true, 4, 1, 1>(a, shares, splits, stream);
     if (tile == 16) return launch_experts<true, 16, 1, 1>(a, shares, splits, stream);
-    if (tile == 32) return launch_experts<true, 32, 1, 1>(a, shares, splits, stream);
-    return launch_experts<true, 64, 1, 1>(a, shares, splits, stream);
+    // Single bytes of scales beside 64 slots would not fit the registers: 32 at a time there.
+    if (tile == 64 && whole_words<true>(a)) return launch_one<true, 64, 2, 1, 128, true>(a, shares, splits, stream);
+    return launch_experts<true, 32, 2, 1, 128>(a, shares, splits, stream);
 }
 
 // Splits of the down product's k, for `shares` shares of experts: two blocks a CU
@@ -656,6 +706,8 @@ int hscale_route_tokens(const void *logits, int32_t type, int64_t tokens, int32_
         ROUTE(1);
     } else if (experts <= 128) {
         ROUTE(2);
+    } else if (experts <= 192) {
+        ROUTE(3);
     } else if (experts <= 256) {
         ROUTE(4);
     } else {
@@ -745,7 +797,7 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         a.ld = 2 * hidden;
         a.in_bytes = (int64_t)slots * hidden * 4;
         const int splits = down_splits(slots, in, hidden, count);
-        a.split = (int)cdiv(cdiv(hidden, 256), splits);
+        a.split = (int)cdiv(cdiv(hidden, 256), splits) * (tile >= 32 ? 2 : 1);
         if (const int st = down_product(a, count, tile, splits, stream)) return st;
         uint16_t *y = static_cast<uint16_t *>(Y) + t0 * ldy;
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 2048), (unsigned)n), dim3(256), 0, stream, P, splits,

@@ -39,45 +39,88 @@ __device__ __forceinline__ T load_any(const void *p) {
     return v;
 }
 
-// kWords words of one row per block.  Their counts in the row's history are
-// made in LDS, by integer additions whose order does not show; every block of a
-// row reads the whole history.
-template <bool kWide, int kWords>
-__global__ __launch_bounds__(256) void adjust_kernel(const LogitArgs a) {
+struct Eight {  // words of one row
+    u32x4 v[2];  // bf16: the first alone
+};
+
+template <bool kWide>
+__device__ __forceinline__ void unpack(const Eight &w, float (&l)[8]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (kWide) {
+            l[q] = __uint_as_float(w.v[0][q]), l[q + 4] = __uint_as_float(w.v[1][q]);
+        } else {
+            l[2 * q] = __uint_as_float(w.v[0][q] << 16), l[2 * q + 1] = __uint_as_float(w.v[0][q] & 0xFFFF0000u);
+        }
+    }
+}
+
+// kWords words of one row per block, eight a thread at a time.  Their counts in
+// the row's history are made in LDS, by integer additions whose order does not
+// show; every block of a row reads the whole history, while its logits are under
+// way.
+template <bool kWide, int kWords, int kThreads>
+__global__ __launch_bounds__(kThreads) void adjust_kernel(const LogitArgs a) {
+    constexpr int kSize = kWide ? 4 : 2, kUnits = kWords / (8 * kThreads), kAhead = 4;
+    static_assert(kUnits * 8 * kThreads == kWords, "whole units");
     __shared__ __attribute__((aligned(16))) uint32_t said[kWords];
     const int tid = threadIdx.x;
     const int64_t v0 = (int64_t)blockIdx.x * kWords;
     const int words = (int)(a.vocab - v0 < kWords ? a.vocab - v0 : kWords);
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        int length = 0;
-        if (a.penalties) {
-            const int most = (int)a.r.history_length;
-            length = a.r.length ? clamped(a.r.length, row, 0, most) : most;
-            const int prompt = a.r.prompt ? clamped(a.r.prompt, row, 0, most) : 0;
-            if (length > 0) {
-                for (int i = tid * 4; i < kWords; i += 1024)
-                    *reinterpret_cast<u32x4 *>(said + i) = u32x4{0, 0, 0, 0};
-                __syncthreads();
-                const int32_t *h = a.r.history + row * a.r.history_ld;
-                auto count = [&](int i, int32_t word) {
-                    const uint32_t at = (uint32_t)word - (uint32_t)v0;
-                    if (word < 0 || at >= (uint32_t)words) return;
-                    if (i < prompt)
-                        atomicOr(&said[at], kInPrompt);
-                    else
-                        atomicAdd(&said[at], 1u);
-                };
-                int i = tid * 4;
-                for (; i + 4 <= length; i += 1024) {
-                    const u32x4 w = load_any<u32x4>(h + i);
+        const char *src = static_cast<const char *>(a.logits) + (row * a.ld + v0) * kSize;
+        char *dst = static_cast<char *>(a.out) + (row * a.ldo + v0) * kSize;
+        // The history's first words, then the logits, under way together.
+        const int most = a.penalties ? (int)a.r.history_length : 0;
+        const int32_t *h = a.r.history + row * a.r.history_ld;
+        u32x4 w[kAhead];
+        auto load_words = [&](int i0) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) count(i + q, (int32_t)w[q]);
-                }
-                for (; i < length; ++i) count(i, h[i]);  // the last ones, three at most
-                __syncthreads();
+            for (int b = 0; b < kAhead; ++b) {
+                const int i = i0 + (b * kThreads + tid) * 4;
+                if (i + 4 <= most) w[b] = load_any<u32x4>(h + i);
             }
+        };
+        load_words(0);
+        Eight x[kUnits];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int v = (u * kThreads + tid) * 8;
+            if (v + 8 > words) continue;
+            x[u].v[0] = load_any<u32x4>(src + v * kSize);
+            if (kWide) x[u].v[1] = load_any<u32x4>(src + v * kSize + 16);
         }
-        const float rho = a.r.repetition ? a.r.repetition[row] : 1.0f;
+        const int length = a.penalties && a.r.length ? clamped(a.r.length, row, 0, most) : most;
+        if (length > 0) {
+            const int prompt = a.r.prompt ? clamped(a.r.prompt, row, 0, most) : 0;
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4 * kThreads)
+                *reinterpret_cast<u32x4 *>(said + i + tid * 4) = u32x4{0, 0, 0, 0};
+            __syncthreads();
+            auto count = [&](int i, int32_t word) {
+                const uint32_t at = (uint32_t)word - (uint32_t)v0;
+                if (i >= length || word < 0 || at >= (uint32_t)words) return;
+                if (i < prompt)
+                    atomicOr(&said[at], kInPrompt);
+                else
+                    atomicAdd(&said[at], 1u);
+            };
+            for (int i0 = 0; i0 < length; i0 += kAhead * 4 * kThreads) {
+                if (i0 > 0) load_words(i0);
+#pragma unroll
+                for (int b = 0; b < kAhead; ++b) {
+                    const int i = i0 + (b * kThreads + tid) * 4;
+                    if (i + 4 <= most) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) count(i + q, (int32_t)w[b][q]);
+                    } else {
+                        for (int q = i; q < most; ++q) count(q, h[q]);  // the last ones, three at most
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        const float rho = a.r.repetition ? a.r.repetition[row] : 1.0f, inv = 1.0f / rho;
         const float frequency = a.r.frequency ? a.r.frequency[row] : 0.0f;
         const float presence = a.r.presence ? a.r.presence[row] : 0.0f;
         const int bias_row = !a.r.bias ? -1 : a.r.bias_row ? a.r.bias_row[row] : 0;
@@ -86,40 +129,25 @@ __global__ __launch_bounds__(256) void adjust_kernel(const LogitArgs a) {
         const uint8_t *mask = mask_row >= 0 && mask_row < a.r.masks
                                   ? reinterpret_cast<const uint8_t *>(a.r.mask + mask_row * ((a.vocab + 31) / 32)) + v0 / 8
                                   : nullptr;
-        auto changed = [&](float l, uint32_t n, float b, bool allowed) {
-            if (n) {
-                if (a.r.repetition) l = l > 0.0f ? l / rho : l * rho;
-                const uint32_t c = n & ~kInPrompt;
-                if (c) {
-                    if (a.r.frequency) l -= frequency * (float)c;
-                    if (a.r.presence) l -= presence;
-                }
-            }
-            if (bias) l += b;
-            return allowed ? l : -INFINITY;
+        // A division for each word would take most of the time.
+        auto penalized = [&](float l, uint32_t n) {
+            l *= l > 0.0f ? inv : rho;
+            const uint32_t c = n & ~kInPrompt;
+            return c ? l - frequency * (float)c - presence : l;
         };
-        constexpr int kSize = kWide ? 4 : 2;
-        const char *src = static_cast<const char *>(a.logits) + (row * a.ld + v0) * kSize;
-        char *dst = static_cast<char *>(a.out) + (row * a.ldo + v0) * kSize;
-        for (int v = tid * 8; v < words; v += 2048) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int v = (u * kThreads + tid) * 8;
+            if (v >= words) continue;
             const int n = words - v < 8 ? words - v : 8;
-            float l[8], b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             const uint32_t bits = mask ? mask[v >> 3] : 0xFFu;
+            float l[8], b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (n == 8) {
-                if (kWide) {
-                    const u32x4 x = load_any<u32x4>(src + v * 4), y = load_any<u32x4>(src + v * 4 + 16);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) l[q] = __uint_as_float(x[q]), l[q + 4] = __uint_as_float(y[q]);
-                } else {
-                    const u32x4 x = load_any<u32x4>(src + v * 2);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        l[2 * q] = __uint_as_float(x[q] << 16), l[2 * q + 1] = __uint_as_float(x[q] & 0xFFFF0000u);
-                }
+                unpack<kWide>(x[u], l);
                 if (bias) {
-                    const u32x4 x = load_any<u32x4>(bias + v), y = load_any<u32x4>(bias + v + 4);
+                    const u32x4 x0 = load_any<u32x4>(bias + v), x1 = load_any<u32x4>(bias + v + 4);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) b[q] = __uint_as_float(x[q]), b[q + 4] = __uint_as_float(y[q]);
+                    for (int q = 0; q < 4; ++q) b[q] = __uint_as_float(x0[q]), b[q + 4] = __uint_as_float(x1[q]);
                 }
             } else {
 #pragma unroll
@@ -133,13 +161,23 @@ __global__ __launch_bounds__(256) void adjust_kernel(const LogitArgs a) {
                     if (bias) b[q] = bias[v + q];
                 }
             }
+            u32x4 n0{0, 0, 0, 0}, n1{0, 0, 0, 0};
             if (length > 0) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(said + v), y = *reinterpret_cast<const u32x4 *>(said + v + 4);
+                n0 = *reinterpret_cast<const u32x4 *>(said + v);
+                n1 = *reinterpret_cast<const u32x4 *>(said + v + 4);
+            }
 #pragma unroll
-                for (int q = 0; q < 8; ++q) l[q] = changed(l[q], q < 4 ? x[q & 3] : y[q & 3], b[q], bits >> q & 1);
-            } else {
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t said_q = q < 4 ? n0[q & 3] : n1[q & 3];
+                if (said_q) l[q] = penalized(l[q], said_q);
+            }
+            if (bias) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) l[q] = changed(l[q], 0, b[q], bits >> q & 1);
+                for (int q = 0; q < 8; ++q) l[q] += b[q];
+            }
+            if (mask) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) l[q] = bits >> q & 1 ? l[q] : -INFINITY;
             }
             if (kWide) {
                 if (n == 8) {
@@ -162,8 +200,30 @@ __global__ __launch_bounds__(256) void adjust_kernel(const LogitArgs a) {
                 }
             }
         }
-        __syncthreads();
+        if (gridDim.y < a.rows) __syncthreads();
     }
+}
+
+template <bool kWide, int kWords, int kThreads>
+int launch_adjust(const LogitArgs &a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.vocab + kWords - 1) / kWords), (unsigned)std::min<int64_t>(a.rows, 65535));
+    hipLaunchKernelGGL((adjust_kernel<kWide, kWords, kThreads>), grid, dim3(kThreads), 0, stream, a);
+    return launch_status();
+}
+
+// Blocks of a row read its whole history each, so a long one goes to fewer and
+// larger blocks (its length on the host is the most that a row may have).  In
+// us with bf16 logits, blocks of 2048, 4096, 8192 words by 512 threads and by 1024:
+//   1 row of 128000, 1000 said       3.6   4.4   4.6   4.4
+//   1 row of 128000, 16384 said      7.4   8.4   6.7   5.6
+//   64 rows of 128000, 1000 said    12.8  11.9  12.2  15.5
+//   64 rows of 128000, 16384 said   29.5  22.9  20.2  24.1
+template <bool kWide>
+int adjust(const LogitArgs &a, hipStream_t stream) {
+    const bool few = a.rows * a.vocab <= (int64_t)1 << 21;
+    if (a.penalties && a.r.history_length > 4096)
+        return few ? launch_adjust<kWide, 8192, 1024>(a, stream) : launch_adjust<kWide, 8192, 512>(a, stream);
+    return few ? launch_adjust<kWide, 2048, 256>(a, stream) : launch_adjust<kWide, 4096, 256>(a, stream);
 }
 
 }  // namespace
@@ -209,19 +269,7 @@ int hscale_adjust_logits(const hscale_logit_rules *rules, const void *logits, in
     for (const Range &x : in)
         if (x.p && overlaps(w[0].p, w[0].n, x.p, x.n)) return HSCALE_ERR_OVERLAP;
     const LogitArgs a{r, logits, out, rows, vocab, ld, ldo, penalties && r.history_length > 0};
-    constexpr int kFew = 2048, kMany = 8192;
-    const bool few = rows * vocab <= (int64_t)256 * kMany;
-    const dim3 grid((unsigned)((vocab + (few ? kFew : kMany) - 1) / (few ? kFew : kMany)),
-                    (unsigned)std::min<int64_t>(rows, 65535));
-    if (type == HSCALE_F32 && few)
-        hipLaunchKernelGGL((adjust_kernel<true, kFew>), grid, dim3(256), 0, stream, a);
-    else if (type == HSCALE_F32)
-        hipLaunchKernelGGL((adjust_kernel<true, kMany>), grid, dim3(256), 0, stream, a);
-    else if (few)
-        hipLaunchKernelGGL((adjust_kernel<false, kFew>), grid, dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((adjust_kernel<false, kMany>), grid, dim3(256), 0, stream, a);
-    return launch_status();
+    return type == HSCALE_F32 ? adjust<true>(a, stream) : adjust<false>(a, stream);
 }
 
 }  // extern "C"

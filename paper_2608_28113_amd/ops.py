@@ -669,9 +669,13 @@ _LOGIT_TYPES = {torch.bfloat16: _lib.HSCALE_BF16, torch.float32: _lib.HSCALE_F32
 
 def _logits(t, name: str) -> tuple[int, int]:
     """t is a 2-D bf16 or fp32 CUDA view with unit column stride; the library's type and its row stride."""
-    if not _on_device(t) or t.dtype not in _LOGIT_TYPES or t.dim() != 2:
+    if not _on_device(t) or (kind := _LOGIT_TYPES.get(t.dtype)) is None or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D bf16 or fp32 CUDA tensor")
-    return _LOGIT_TYPES[t.dtype], _row_view(t, t.dtype, t.shape, t.device, name)
+    row, col = t.stride()
+    rows, cols = t.shape
+    if col != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return kind, row if rows > 1 else cols
 
 
 def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: torch.Tensor | None = None,
@@ -700,21 +704,20 @@ def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: t
     return expert, weight
 
 
-def _expert_matrix(matrix, name: str, device, shape=None):
-    """The checked addresses of (global_scale, scale_codes, packed_e2m1) and the shape [experts, out, in]."""
+def _expert_matrix(matrix, name: str, device, E: int, m: int, n: int) -> tuple[int, int, int]:
+    """The checked addresses of (global_scale, scale_codes, packed_e2m1) of E matrices of m x n."""
     try:
         scale, codes, packed = matrix
-    except (TypeError, ValueError):
-        raise ValueError(f"{name} must be (global_scale, scale_codes, packed_e2m1)") from None
-    if shape is None:
-        if not isinstance(packed, torch.Tensor) or packed.dim() != 3:
-            raise ValueError(f"{name}: packed_e2m1 must be a 3-D uint8 tensor [experts, out, in / 2]")
-        shape = (*packed.shape[:2], 2 * packed.shape[2])
-    E, m, n = shape
-    _tensor(packed, f"{name}: packed_e2m1", torch.uint8, (E, m, n // 2), device)
-    _tensor(codes, f"{name}: scale_codes", torch.uint8, (E, m, n // 16), device)
-    _tensor(scale, f"{name}: global_scale", torch.float32, (E,), device)
-    return (scale.data_ptr(), codes.data_ptr(), packed.data_ptr()), shape
+        # One pass over what must hold: a call has nine of these tensors, and a token's time for them.
+        if (packed.dtype is torch.uint8 and codes.dtype is torch.uint8 and scale.dtype is torch.float32
+                and packed.shape == (E, m, n // 2) and codes.shape == (E, m, n // 16) and scale.shape == (E,)
+                and packed.device == device and codes.device == device and scale.device == device
+                and packed.is_contiguous() and codes.is_contiguous() and scale.is_contiguous()):
+            return scale.data_ptr(), codes.data_ptr(), packed.data_ptr()
+    except (TypeError, ValueError, AttributeError):
+        raise ValueError(f"{name} must be three tensors (global_scale, scale_codes, packed_e2m1)") from None
+    raise ValueError(f"{name} must be contiguous (global_scale fp32 [{E}], scale_codes uint8 [{E}, {m}, {n // 16}], "
+                     f"packed_e2m1 uint8 [{E}, {m}, {n // 2}]) on {device}")
 
 
 def expert_layer_workspace_bytes(tokens: int, in_features: int, hidden: int, experts: int, k: int) -> int:
@@ -747,11 +750,12 @@ def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, ga
     k = expert.shape[1]
     _tensor(expert, "expert", torch.int32, (T, k), dev)
     _tensor(weight, "weight", torch.float32, (T, k), dev)
-    gate, (E, hidden, width) = _expert_matrix(gate, "gate", dev)
-    if width != n:
-        raise ValueError(f"gate has {width} inputs, X {n}")
-    up, _ = _expert_matrix(up, "up", dev, (E, hidden, n))
-    down, _ = _expert_matrix(down, "down", dev, (E, n, hidden))
+    if not isinstance(gate, (tuple, list)) or len(gate) != 3 or not isinstance(gate[2], torch.Tensor) or gate[2].dim() != 3:
+        raise ValueError("gate must be (global_scale, scale_codes, packed_e2m1), the last uint8 [experts, hidden, in / 2]")
+    E, hidden, _ = gate[2].shape
+    gate = _expert_matrix(gate, "gate", dev, E, hidden, n)
+    up = _expert_matrix(up, "up", dev, E, hidden, n)
+    down = _expert_matrix(down, "down", dev, E, n, hidden)
     _no_graph("expert_layer", X, weight, grad=False)
     Y, ldy = _rows_out(Y, "Y", (T, n), dev, stream)
     need = expert_layer_workspace_bytes(T, n, hidden, E, k)
