@@ -297,8 +297,8 @@ __device__ __forceinline__ void own_writes_and_barrier() {  // loads stay under 
 // read back from LDS two at a time: as 2-byte loads for each step they took a
 // quarter of the time (64 tokens of 4096 over 128 experts of 1536: 363 us with
 // them, 275 without any scales).
-template <bool kDown, int kTok, int kRT, int kW, int kStep, bool kWords>  // kWords: rows of scales are whole aligned words
-__global__ __launch_bounds__(256, 2) void expert_kernel(const ExpertArgs a) {
+template <bool kDown, int kTok, int kRT, int kW, int kStep>
+__global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 64 && kW == 4 ? 1 : 2) void expert_kernel(const ExpertArgs a) {
     constexpr int kNT = (kTok + 15) / 16, kSets = 2 * kRT, kMats = kDown ? 1 : 2, kParts = kDown ? 2 : 1;
     constexpr int kRows = kDown ? 32 * kRT : 16 * kRT;  // of a wave
     constexpr int kHalves = kStep / 128, kRowBytes = kStep * 2, kStepBytes = kTok * kRowBytes;
@@ -350,31 +350,30 @@ __global__ __launch_bounds__(256, 2) void expert_kernel(const ExpertArgs a) {
             for (int h = 0; h < kHalves; ++h) w.p[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rp, p + 64 * h, 0, 0);
         }
     };
+    // Rows of scales lie at any byte: whole words from the one that the first byte
+    // is in to the one that the last is in, put in place when they are written.
+    constexpr int kScaleWords = kStep / 64;
     struct Scales {  // of one of four steps
-        uint32_t c[kSets][kStep / 64];
+        uint32_t c[kSets][kScaleWords + 1];
     };
     auto load_scales = [&](Scales &w, int step) {
 #pragma unroll
         for (int s = 0; s < kSets; ++s) {
             const int m = kDown ? 0 : s / kRT, tile = kDown ? s : s % kRT;
+            const uintptr_t from = reinterpret_cast<uintptr_t>(codes[m]) + step * (kStep / 16);
+            const int bytes = rows * (K / 16) - step * (kStep / 16) + (int)(from & 3);
             const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
-                const_cast<uint8_t *>(codes[m]) + step * (kStep / 16), 0,
-                step < steps ? rows * (K / 16) - step * (kStep / 16) : 0, kRawWord3);
-            const uint32_t c = crow + tile * 16 * (K / 16);
-            if (kWords && kHalves == 2) {
+                reinterpret_cast<void *>(from & ~(uintptr_t)3), 0, step < steps ? (bytes + 3) & ~3 : 0, kRawWord3);
+            const uint32_t c = (crow + tile * 16 * (K / 16) + (uint32_t)(from & 3)) & ~3u;
+            if constexpr (kScaleWords == 4) {
                 const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rc, c, 0, 0);
 #pragma unroll
-                for (int q = 0; q < kStep / 64; ++q) w.c[s][q] = v[q];
-            } else if (kWords) {
+                for (int q = 0; q < 4; ++q) w.c[s][q] = v[q];
+            } else {
                 const auto v = __builtin_amdgcn_raw_buffer_load_b64(rc, c, 0, 0);
                 w.c[s][0] = v[0], w.c[s][1] = v[1];
-            } else {
-#pragma unroll
-                for (int b = 0; b < kStep / 16; ++b) {
-                    const uint32_t one = __builtin_amdgcn_raw_buffer_load_b8(rc, c + b, 0, 0);
-                    w.c[s][b / 4] = b % 4 ? w.c[s][b / 4] | one << (8 * (b % 4)) : one;
-                }
             }
+            w.c[s][kScaleWords] = __builtin_amdgcn_raw_buffer_load_b32(rc, c + 4 * kScaleWords, 0, 0);
         }
     };
     constexpr int kScaleRow = kStep / 4 + kStep / 16, kScaleSet = 16 * kScaleRow;  // a row in other banks than its neighbours
@@ -382,14 +381,26 @@ __global__ __launch_bounds__(256, 2) void expert_kernel(const ExpertArgs a) {
     uint8_t *scales = scale_lds + wave * kSets * kScaleSet;  // the wave's own
     auto write_scales = [&](const Scales &w) {
 #pragma unroll
-        for (int s = 0; s < kSets; ++s)
+        for (int s = 0; s < kSets; ++s) {
+            const uint32_t by = crow + (uint32_t)reinterpret_cast<uintptr_t>(codes[kDown ? 0 : s / kRT]);
+            uint32_t v[kScaleWords];
+#pragma unroll
+            for (int q = 0; q < kScaleWords; ++q) v[q] = __builtin_amdgcn_alignbyte(w.c[s][q + 1], w.c[s][q], by & 3);
             __builtin_memcpy(__builtin_assume_aligned(scales + s * kScaleSet + l16 * kScaleRow + g * (kStep / 16), kStep / 16),
-                             w.c[s], kStep / 16);
+                             v, kStep / 16);
+        }
     };
     const __amdgpu_buffer_rsrc_t rx =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.in), 0, (int)a.in_bytes, kRawWord3);
 
     for (int c0 = 0; c0 < count; c0 += kTok) {
+        // Loads are waited for in the order in which they were issued: what the
+        // loop's first round needs comes first.
+        Weights w[2];
+        Scales c;
+        load_scales(c, step0 + part);
+        load_weights(w[0], step0 + part);
+        __builtin_amdgcn_sched_barrier(0);
         const int held = own.slot(a, c0, list[wave]);
         // A thread's places in a buffer: a chunk of rows tid / kRowLanes, kCopyRows further on, ...
         constexpr int kOfRows = kTok > kCopyRows ? kTok / kCopyRows : 1;  // copies of a step's rows
@@ -428,14 +439,8 @@ __global__ __launch_bounds__(256, 2) void expert_kernel(const ExpertArgs a) {
 #pragma unroll
             for (int n = 0; n < kNT; ++n) acc[s][n] = f32x4{0, 0, 0, 0};
 
-        Weights w[2];
-        Scales c;
         Rows x;
-        // Loads are waited for in the order in which they were issued: what the
-        // loop's first round needs comes first.
-        load_scales(c, step0 + part);
         load_rows(x, 0);
-        load_weights(w[0], step0 + part);
         __builtin_amdgcn_sched_barrier(0);
         write_scales(c);
         write_rows(x, 0);
@@ -626,43 +631,39 @@ int check_matrix(const hscale_experts *w) {
 
 Matrices matrices(const hscale_experts *w) { return Matrices{w->global_scale, w->scale_codes, w->packed_e2m1}; }
 
-// Whether rows of scales are whole aligned words.
-template <bool kDown>
-bool whole_words(const ExpertArgs &a) {
-    return a.k % 64 == 0 && aligned(a.w[0].codes, 4) && (kDown || aligned(a.w[1].codes, 4));
-}
-
-template <bool kDown, int kTok, int kRT, int kW, int kStep, bool kWords>
-int launch_one(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
+template <bool kDown, int kTok, int kRT, int kW, int kStep = 256>
+int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
     const dim3 grid((unsigned)cdiv(a.rows, (kDown ? 32 : 16) * kRT * (4 / kW)), (unsigned)shares, (unsigned)splits);
-    hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, kStep, kWords>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((expert_kernel<kDown, kTok, kRT, kW, kStep>), grid, dim3(256), 0, stream, a);
     return launch_status();
 }
 
-template <bool kDown, int kTok, int kRT, int kW, int kStep = 256>
-int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stream) {
-    return whole_words<kDown>(a) ? launch_one<kDown, kTok, kRT, kW, kStep, true>(a, shares, splits, stream)
-                                 : launch_one<kDown, kTok, kRT, kW, kStep, false>(a, shares, splits, stream);
-}
-
-// A wave alone has its rows where there are many; with fewer, two or four share
-// them.
+// A wave alone has its rows where they are many.  Where they are few, two waves
+// share them, or four where slots are many (us of the whole call, one, two and
+// four waves):
+//   1 token through 6 of 64 experts of 2048 x 1024     28.4  24.2  25.2
+//   12 tokens through 6 of 64 of 2048 x 1408           70.1  75.9  115
+//   48 tokens through 2 of 8 of 1024 x 1024            29.8  27.6  32.4
+//   75 tokens through 3 of 5 of 3152 x 848             67.5        56.7
+//   200 tokens through 2 of 8 of 1024 x 4096           58.4        109
 int gate_and_up(const ExpertArgs &a, int shares, int tile, hipStream_t stream) {
-    const int64_t units = cdiv(a.rows, 16) * shares;
-    if (tile == 4) return launch_experts<false, 4, 1, 4>(a, shares, 1, stream);
-    if (tile == 16)
-        return units >= 4096   ? launch_experts<false, 16, 1, 1>(a, shares, 1, stream)
-               : units >= 2048 ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
-                               : launch_experts<false, 16, 1, 4>(a, shares, 1, stream);
-    if (tile == 32) return launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
-    return launch_experts<false, 64, 2, 1, 128>(a, shares, 1, stream);
+    const int64_t units = cdiv(a.rows, 16) * shares, steps = cdiv(a.k, 256);
+    const bool two = units < 4096 && steps >= 2, four = cdiv(a.rows, 128) * shares < 128 && steps >= 4;
+    if (tile == 4 && two) return launch_experts<false, 4, 1, 2>(a, shares, 1, stream);
+    if (tile <= 16)
+        return two ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
+                   : launch_experts<false, 16, 1, 1>(a, shares, 1, stream);
+    if (tile == 32)
+        return four ? launch_experts<false, 32, 1, 4, 128>(a, shares, 1, stream)
+                    : launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
+    return four ? launch_experts<false, 64, 1, 4, 128>(a, shares, 1, stream)
+                : launch_experts<false, 64, 2, 1, 128>(a, shares, 1, stream);
 }
 
 int down_product(const ExpertArgs &a, int shares, int tile, int splits, hipStream_t stream) {
     if (tile == 4) return launch_experts<true, 4, 1, 1>(a, shares, splits, stream);
     if (tile == 16) return launch_experts<true, 16, 1, 1>(a, shares, splits, stream);
-    // Single bytes of scales beside 64 slots would not fit the registers: 32 at a time there.
-    if (tile == 64 && whole_words<true>(a)) return launch_one<true, 64, 2, 1, 128, true>(a, shares, splits, stream);
+    if (tile == 64) return launch_experts<true, 64, 2, 1, 128>(a, shares, splits, stream);
     return launch_experts<true, 32, 2, 1, 128>(a, shares, splits, stream);
 }
 
@@ -767,7 +768,7 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         const int slots = (int)(n * k);
         const int32_t *ids = expert + t0 * k;
         // Slots of a block: as many as an expert's share, on average, is likely to need.
-        const int tile = n <= 4 ? 4 : slots <= 12 * experts ? 16 : slots <= 28 * experts ? 32 : 64;
+        const int tile = n <= 4 ? 4 : n <= 16 || slots <= 12 * experts ? 16 : n <= 32 || slots <= 28 * experts ? 32 : 64;
         int count = std::min(slots, (int)experts);
         const bool many = slots > kBlockSlots;
         if (many) {
