@@ -390,6 +390,9 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
                              v, kStep / 16);
         }
     };
+    // What lies behind a row's last scale may be of another array: an E4M3 NaN
+    // would not vanish beside the zeros of the slots' rows, and becomes a number.
+    auto scale_of = [](float l) { return __builtin_amdgcn_fmed3f(l, -448.0f, 448.0f); };
     const __amdgpu_buffer_rsrc_t rx =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(a.in), 0, (int)a.in_bytes, kRawWord3);
 
@@ -476,8 +479,8 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
                                     (((i / 4 * 16 + 4 * g + i % 4) ^ row) << 4));
 #pragma unroll
                         for (int s = 0; s < kSets; ++s) {
-                            const float l = i & 2 ? __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 1)
-                                                  : __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 0);
+                            const float l = scale_of(i & 2 ? __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 1)
+                                                           : __builtin_amdgcn_cvt_f32_fp8(code[s][i / 4], 0));
                             const bf16x8 fw = __builtin_bit_cast(
                                 bf16x8, scaled_eight(w[d & 1].p[s][i / 4][i % 4], two_e[kDown ? 0 : s / kRT], l));
 #pragma unroll

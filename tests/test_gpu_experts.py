@@ -76,6 +76,30 @@ def test_layer(hs, T, n, hidden, E, k, ids):
     _check(hs.expert_layer(**p), p)
 
 
+# Every tile of slots (4, 16, 32, 64), one, two and four waves to a row, with
+# several rounds of k, and splits of the down product.
+ROUTES = [(1, 64, 96, 8, 3), (1, 528, 4112, 8, 2), (4, 1040, 528, 64, 6), (12, 528, 1056, 64, 6), (16, 1104, 272, 7, 3),
+          (40, 528, 1056, 100, 8), (160, 528, 1040, 12, 2), (160, 1040, 272, 12, 2), (160, 80, 2064, 12, 2),
+          (256, 528, 1040, 8, 2), (256, 1040, 272, 8, 2), (300, 96, 3088, 6, 2)]
+
+
+@pytest.mark.parametrize("T,n,hidden,E,k", ROUTES)
+@pytest.mark.parametrize("odd", [0, 1])
+def test_every_route(hs, T, n, hidden, E, k, odd):
+    """`odd`: scales that start at an odd byte, packed weights at 8 bytes."""
+    p = _problem(T, n, hidden, E, k)
+    if odd:
+        for m in ("gate", "up", "down"):
+            s, c, w = p[m]
+            codes = torch.full((c.numel() + 9,), 255, dtype=torch.uint8, device=DEV)  # a NaN on either side
+            packed = torch.full((w.numel() + 16,), 0x77, dtype=torch.uint8, device=DEV)
+            codes[1:-8] = c.flatten()
+            packed[8:-8] = w.flatten()
+            p[m] = s, codes[1:-8].view(c.shape), packed[8:-8].view(w.shape)
+    print(f"[route {T} {n} {hidden} {E} {k} {odd}]", flush=True)
+    _check(hs.expert_layer(**p), p)
+
+
 def test_pieces(hs):
     """More slots than one piece of 4096 takes, the last piece a short one."""
     p = _problem(1500, 32, 48, 7, 3)
@@ -271,3 +295,18 @@ def test_route_strided_rows_and_given_outputs(hs):
     assert (expert[21] == 99).all() and (weight[21] == 9.0).all()
     none = hs.route_tokens(big[:0], 3)
     assert none[0].shape == none[1].shape == (0, 3)
+
+
+@pytest.mark.parametrize("T,n,hidden,E,k", [(1, 2048, 1024, 64, 6), (1, 4096, 2048, 8, 2), (9, 640, 1040, 33, 4)])
+def test_many_small_calls_in_a_row(hs, T, n, hidden, E, k):
+    """Calls that follow one another in the same workspace with other inputs give
+    what each gives alone."""
+    p = [_problem(T, n, hidden, E, k, seed=s) for s in (1, 2, 3)]
+    for q in p[1:]:
+        q.update(gate=p[0]["gate"], up=p[0]["up"], down=p[0]["down"])
+    ws = torch.empty(hs.expert_layer_workspace_bytes(T, n, hidden, E, k), dtype=torch.uint8, device=DEV)
+    want = [hs.expert_layer(**q, workspace=ws).clone() for q in p]
+    for q, w in zip(p, want):
+        _check(w, q)
+    got = [hs.expert_layer(**p[i % 3], workspace=ws) for i in range(600)]
+    assert all(torch.equal(y, want[i % 3]) for i, y in enumerate(got))
