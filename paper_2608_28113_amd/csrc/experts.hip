@@ -554,37 +554,46 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
     }
 }
 
-// Y[t] = the sum of the token's slots in their order, each over the splits of k;
-// eight outputs a thread.  A slot without an expert adds its weight times 0.
+// Y[t] = the sum over the splits of k of the token's slots, both in their order;
+// four outputs a thread.  A slot without an expert adds its weight times 0; what
+// lies in its place is read with the others', so that all are under way at once,
+// and left out.
 __global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, int splits, int64_t slots,
                                                    const int32_t *__restrict__ ids, const float *__restrict__ weight,
                                                    int choices, int experts, int64_t out, uint16_t *__restrict__ Y,
                                                    int64_t ldy, bool wide) {
-    const int64_t t = blockIdx.y, m = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int64_t t = blockIdx.y, m = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (m >= out) return;
-    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int j = 0; j < choices; ++j) {
-        const int64_t s = t * choices + j;
-        if (expert_of(ids, experts, (int)s) == kNoExpert) {
+    constexpr int kAhead = 8;
+    float y[4] = {0, 0, 0, 0};
+    const float *p = P + t * choices * out + m;
+    int j = 0, z = 0;
+    while (z < splits) {
+        float4 a[kAhead];
+        float other[kAhead];  // in its place, if there is no expert
+        bool none[kAhead], some[kAhead];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] += weight[s] * 0.0f;
-            continue;
+        for (int q = 0; q < kAhead; ++q) {
+            some[q] = z < splits;
+            const int jq = some[q] ? j : 0;
+            a[q] = *reinterpret_cast<const float4 *>(p + ((some[q] ? z : 0) * slots + jq) * out);
+            none[q] = expert_of(ids, experts, (int)(t * choices) + jq) == kNoExpert;
+            other[q] = z == 0 ? weight[t * choices + jq] * 0.0f : 0.0f;
+            if (++j == choices) j = 0, ++z;
         }
-#pragma unroll 4
-        for (int z = 0; z < splits; ++z) {
-            const float *p = P + (z * slots + s) * out + m;
-            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-            y[0] += a.x, y[1] += a.y, y[2] += a.z, y[3] += a.w;
-            y[4] += b.x, y[5] += b.y, y[6] += b.z, y[7] += b.w;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            if (!some[q]) continue;
+            y[0] += none[q] ? other[q] : a[q].x, y[1] += none[q] ? other[q] : a[q].y;
+            y[2] += none[q] ? other[q] : a[q].z, y[3] += none[q] ? other[q] : a[q].w;
         }
     }
     uint16_t *dst = Y + t * ldy + m;
-    const u32x4 v{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7])};
+    const uint32_t lo = bf16_pair(y[0], y[1]), hi = bf16_pair(y[2], y[3]);
     if (wide) {
-        *reinterpret_cast<u32x4 *>(dst) = v;
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dst[i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
+        dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16), dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
     }
 }
 
@@ -804,8 +813,8 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         a.split = (int)cdiv(cdiv(hidden, 256), splits) * (tile >= 32 ? 2 : 1);
         if (const int st = down_product(a, count, tile, splits, stream)) return st;
         uint16_t *y = static_cast<uint16_t *>(Y) + t0 * ldy;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 2048), (unsigned)n), dim3(256), 0, stream, P, splits,
-                           (int64_t)slots, ids, a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 16) && ldy % 8 == 0);
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 1024), (unsigned)n), dim3(256), 0, stream, P, splits,
+                           (int64_t)slots, ids, a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 8) && ldy % 4 == 0);
         if (const int st = launch_status()) return st;
     }
     return HSCALE_OK;
