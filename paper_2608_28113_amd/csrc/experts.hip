@@ -131,7 +131,7 @@ __device__ __forceinline__ int expert_of(const int32_t *ids, int experts, int s)
     return e >= 0 && e < experts ? e : kNoExpert;
 }
 
-// Up to 16 kNT slots of one expert; count 0: none.
+// Up to a block's slots of one expert; count 0: none.
 struct Share {
     int expert, first, count;
 };
@@ -283,7 +283,16 @@ __device__ __forceinline__ void own_writes_and_barrier() {  // loads stay under 
 
 // 16 kRT rows of gate and the same of up (or 32 kRT of down) a wave, x up to
 // kTok slots of one expert.  kW of the block's four waves share their rows: each
-// takes every kWth 256 k, and they add up through LDS.
+// takes every kWth step of k, and they add up through LDS.
+//
+// Reading the weights bounds it while slots are few: 64 tokens over 128 experts
+// of 4096 x 1536 take 178 and 120 us, 5.1 and 3.8 TB/s; 37 over 8 of 4096 x 14336
+// 109 and 69, 4.9 and 3.8; one token over two of these 33 and 20, 4.0 and 3.4.
+// With many the conversion of the weights, the products and the loads each keep
+// a third of the time and two waves a SIMD overlap them only in part: 512 tokens
+// over 64 experts of 2048 x 1024, 48 slots each, 57 and 48 us (MFMA 0.21, VALU
+// 0.35 busy).  Four sets of weights under way in place of two measured equal
+// there, 256 k of weights with 128 of the rows 138 us a call for 130.
 //
 // A wave's operand of weights comes straight from memory, 32 consecutive weights
 // of a row a lane (which k meets which place in a step does not matter, as both
@@ -635,6 +644,19 @@ LayerSpace layer_space(int64_t tokens, int64_t in, int64_t hidden, int32_t exper
     return s;
 }
 
+// Slots of a block: as many as an expert's share is likely to need.  us of the
+// whole call in blocks of 16, 32 and 64, for 32 experts of 2048 x 1024 with on
+// average
+//   9 slots   48.3  49.0  62.4       24 slots  67.0  59.0  65.7
+//   12 slots  52.4  49.4  63.0       32 slots  78.3  66.6  70.6
+//   16 slots  55.5  51.3  64.8       40 slots  88.5  76.9  72.6
+// and for 16 of 4096 x 1536 59.7, 69.6, 89.1 with 9 and 128, 101, 101 with 40.
+int slots_of_block(int64_t tokens, int64_t slots, int64_t experts) {
+    if (tokens <= 4) return 4;
+    if (tokens <= 16 || slots <= 10 * experts) return 16;
+    return tokens <= 32 || slots <= 34 * experts ? 32 : 64;
+}
+
 int check_matrix(const hscale_experts *w) {
     if (!w || !w->global_scale || !w->scale_codes || !w->packed_e2m1) return HSCALE_ERR_NULL;
     if (!aligned(w->global_scale, 4) || !aligned(w->packed_e2m1, 8)) return HSCALE_ERR_ALIGN;
@@ -779,8 +801,7 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         const int64_t n = std::min(piece, tokens - t0);
         const int slots = (int)(n * k);
         const int32_t *ids = expert + t0 * k;
-        // Slots of a block: as many as an expert's share, on average, is likely to need.
-        const int tile = n <= 4 ? 4 : n <= 16 || slots <= 12 * experts ? 16 : n <= 32 || slots <= 28 * experts ? 32 : 64;
+        const int tile = slots_of_block(n, slots, experts);
         int count = std::min(slots, (int)experts);
         const bool many = slots > kBlockSlots;
         if (many) {

@@ -80,7 +80,7 @@ def test_layer(hs, T, n, hidden, E, k, ids):
 # several rounds of k, and splits of the down product.
 ROUTES = [(1, 64, 96, 8, 3), (1, 528, 4112, 8, 2), (4, 1040, 528, 64, 6), (12, 528, 1056, 64, 6), (16, 1104, 272, 7, 3),
           (40, 528, 1056, 100, 8), (160, 528, 1040, 12, 2), (160, 1040, 272, 12, 2), (160, 80, 2064, 12, 2),
-          (256, 528, 1040, 8, 2), (256, 1040, 272, 8, 2), (300, 96, 3088, 6, 2)]
+          (300, 528, 1040, 8, 2), (300, 1040, 272, 8, 2), (300, 96, 3088, 6, 2)]
 
 
 @pytest.mark.parametrize("T,n,hidden,E,k", ROUTES)
