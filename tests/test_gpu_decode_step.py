@@ -18,7 +18,8 @@ pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(),
 @pytest.fixture(scope="module")
 def served():
     import serve_experts
-    return serve_experts.main(steps=12)
+    yield serve_experts.main(steps=12)
+    torch.cuda.empty_cache()
 
 
 def test_the_rules_hold(served):

@@ -17,7 +17,8 @@ def hs():
     import paper_2608_28113_amd as hs
     from paper_2608_28113_amd import _lib
     _lib.load()
-    return hs
+    yield hs
+    torch.cuda.empty_cache()  # what is cached here would serve later tests that bound the memory left
 
 
 def _gen(seed):
