@@ -618,11 +618,12 @@ bool layer_sizes_ok(int64_t tokens, int64_t in, int64_t hidden, int32_t experts,
            k <= kMaxChoices;
 }
 
-// Tokens of a piece: its rows of X and of h are addressed in 32 bits.
-int64_t piece_tokens(int64_t hidden, int32_t k, int64_t ldx) {
+// Tokens of a piece: its rows of X and of h are addressed in 32 bits, and its
+// sums take no more than h may.
+int64_t piece_tokens(int64_t in, int64_t hidden, int32_t k, int64_t ldx) {
     int64_t n = kPieceSlots / k;
     n = std::min(n, ((int64_t)1 << 29) / std::max<int64_t>(1, ldx));
-    return std::max<int64_t>(1, std::min(n, ((int64_t)1 << 28) / (hidden * k)));
+    return std::max<int64_t>(1, std::min(n, ((int64_t)1 << 28) / (std::max(in, hidden) * k)));
 }
 
 constexpr int kDownSplits = 16;
@@ -633,7 +634,7 @@ struct LayerSpace {
 };
 
 LayerSpace layer_space(int64_t tokens, int64_t in, int64_t hidden, int32_t experts, int32_t k) {
-    const int64_t slots = std::min(tokens, piece_tokens(hidden, k, 1)) * k;
+    const int64_t slots = std::min(tokens, piece_tokens(in, hidden, k, 1)) * k;
     LayerSpace s{};
     s.h = round_256((size_t)(slots * hidden * 4));
     // Splits of few tokens are more: a bound that does not fall with the tokens.
@@ -796,7 +797,7 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
     float *P = reinterpret_cast<float *>(ws += space.h);
     int32_t *order = reinterpret_cast<int32_t *>(ws += space.p);
     Share *shares = reinterpret_cast<Share *>(ws + space.order);
-    const int64_t piece = piece_tokens(hidden, k, ldx);
+    const int64_t piece = piece_tokens(in, hidden, k, ldx);
     for (int64_t t0 = 0; t0 < tokens; t0 += piece) {
         const int64_t n = std::min(piece, tokens - t0);
         const int slots = (int)(n * k);
