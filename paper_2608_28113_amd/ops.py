@@ -766,6 +766,29 @@ def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, ga
     return Y
 
 
+def _each_row(t, name: str, dtype, rows: int, device) -> int:
+    """The checked address of one number a row, 0 for None."""
+    if t is None:
+        return 0
+    return _tensor(t, name, dtype, (rows,), device).data_ptr()
+
+
+def _rows_of(t, row, name: str, dtype, width: int, rows: int, device) -> tuple[int, int, int]:
+    """How many biases or masks [count, width] there are, and the checked
+    addresses of them and of each row's number."""
+    if t is None:
+        if row is not None:
+            raise ValueError(f"{name}_row needs {name}")
+        return 0, 0, 0
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D {dtype} tensor")
+    count = t.shape[0]
+    _tensor(t, name, dtype, (count, width), device)
+    if row is None and count != 1:
+        raise ValueError(f"{name}_row (int32, one number a row) is required unless there is exactly one {name}")
+    return count, t.data_ptr(), _each_row(row, f"{name}_row", torch.int32, rows, device)
+
+
 def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, length: torch.Tensor | None = None,
                   prompt: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
                   frequency: torch.Tensor | None = None, presence: torch.Tensor | None = None,
@@ -775,7 +798,7 @@ def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, len
     """Logits, bf16 or fp32 [rows, vocab] (rows may be strided), with each row's
     penalties for repeated words, its bias and its mask, in this order:
 
-        l > 0 ? l / repetition : l * repetition   of words in the history
+        l > 0 ? l * (1 / repetition) : l * repetition   of words in the history
         l - frequency * count - presence          of words in the answer, said count times
         l + bias[v],  -inf where the mask's bit is clear
 
@@ -796,45 +819,27 @@ def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, len
     R, V = logits.shape
     dev = logits.device
     _no_graph("adjust_logits", logits, repetition, frequency, presence, bias, grad=False)
-    penalties = repetition is not None or frequency is not None or presence is not None
-    if history is None and (penalties or length is not None or prompt is not None):
+    if history is None and not (length is None and prompt is None and repetition is None and frequency is None
+                                and presence is None):
         raise ValueError("repetition, frequency, presence, length and prompt need a history")
-    words = ldh = 0
+    words = ldh = at_history = 0
     if history is not None:
         if not isinstance(history, torch.Tensor) or history.dim() != 2:
             raise ValueError("history must be a 2-D int32 tensor [rows, length]")
         words = history.shape[1]
         ldh = _row_view(history, torch.int32, (R, words), dev, "history")
-    for t, name, dtype in ((length, "length", torch.int32), (prompt, "prompt", torch.int32),
-                           (repetition, "repetition", torch.float32), (frequency, "frequency", torch.float32),
-                           (presence, "presence", torch.float32), (bias_row, "bias_row", torch.int32),
-                           (mask_row, "mask_row", torch.int32)):
-        if t is not None:
-            _tensor(t, name, dtype, (R,), dev)
-    sets = []
-    for t, at, name, dtype, width in ((bias, bias_row, "bias", torch.float32, V),
-                                      (mask, mask_row, "mask", torch.int32, -(-V // 32))):
-        if t is None:
-            if at is not None:
-                raise ValueError(f"{name}_row needs {name}")
-            sets.append(0)
-            continue
-        if not isinstance(t, torch.Tensor) or t.dim() != 2:
-            raise ValueError(f"{name} must be a 2-D {dtype} tensor")
-        sets.append(t.shape[0])
-        _tensor(t, name, dtype, (sets[-1], width), dev)
-        if at is None and sets[-1] != 1:
-            raise ValueError(f"{name}_row (int32, one number a row) is required unless there is exactly one {name}")
+        at_history = history.data_ptr()
+    biases, at_bias, at_bias_row = _rows_of(bias, bias_row, "bias", torch.float32, V, R, dev)
+    masks, at_mask, at_mask_row = _rows_of(mask, mask_row, "mask", torch.int32, -(-V // 32), R, dev)
+    rules = (at_history, words, ldh, _each_row(length, "length", torch.int32, R, dev),
+             _each_row(prompt, "prompt", torch.int32, R, dev), _each_row(repetition, "repetition", torch.float32, R, dev),
+             _each_row(frequency, "frequency", torch.float32, R, dev),
+             _each_row(presence, "presence", torch.float32, R, dev), at_bias, biases, at_bias_row, at_mask, masks,
+             at_mask_row)
     if out is None:
         out, ldo = _new((R, V), logits.dtype, dev, stream), V
     else:
         ldo = _row_view(out, logits.dtype, (R, V), dev, "out")
-
-    def at(t):
-        return 0 if t is None else t.data_ptr()
-
-    rules = (at(history), words, ldh, at(length), at(prompt), at(repetition), at(frequency), at(presence), at(bias),
-             sets[0], at(bias_row), at(mask), sets[1], at(mask_row))
     _check(_call(dev, _lib.hscale_adjust_logits, rules, logits.data_ptr(), kind, R, V, ld, out.data_ptr(), ldo,
                  _stream(stream, dev)), "hscale_adjust_logits")
     return out
