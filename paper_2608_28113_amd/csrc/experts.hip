@@ -341,6 +341,7 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
     const int step0 = kDown ? (int)blockIdx.z * a.split : 0;
     const int steps = kDown && step0 + a.split < (K + kStep - 1) / kStep ? step0 + a.split : (K + kStep - 1) / kStep;
     const int rounds = (steps - step0 + kW - 1) / kW;
+    const int read = rows > 0 ? steps : 0;  // a wave behind the last row only keeps step
 
     struct Weights {  // 32 of each 128 of a row's
         u32x4 p[kSets][kHalves];
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
             const int m = kDown ? 0 : s / kRT, tile = kDown ? s : s % kRT;
             const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc(
                 const_cast<uint8_t *>(packed[m]) + step * (kStep / 2), 0,
-                step < steps ? rows * (K / 2) - step * (kStep / 2) : 0, kRawWord3);
+                step < read ? rows * (K / 2) - step * (kStep / 2) : 0, kRawWord3);
             const uint32_t p = prow + tile * 16 * (K / 2);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) w.p[s][h] = __builtin_amdgcn_raw_buffer_load_b128(rp, p + 64 * h, 0, 0);
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(256, !kDown && kTok == 16 && kW == 1 ? 4 : kTok == 
             const uintptr_t from = reinterpret_cast<uintptr_t>(codes[m]) + step * (kStep / 16);
             const int bytes = rows * (K / 16) - step * (kStep / 16) + (int)(from & 3);
             const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(
-                reinterpret_cast<void *>(from & ~(uintptr_t)3), 0, step < steps ? (bytes + 3) & ~3 : 0, kRawWord3);
+                reinterpret_cast<void *>(from & ~(uintptr_t)3), 0, step < read ? (bytes + 3) & ~3 : 0, kRawWord3);
             const uint32_t c = (crow + tile * 16 * (K / 16) + (uint32_t)(from & 3)) & ~3u;
             if constexpr (kScaleWords == 4) {
                 const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rc, c, 0, 0);
