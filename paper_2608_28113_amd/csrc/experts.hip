@@ -124,7 +124,10 @@ __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ log
 // Which slots an expert has
 // ---------------------------------------------------------------------------
 
-constexpr int kBlockSlots = 256;  // up to so many, each block finds its expert's slots itself
+// Up to so many, each block finds its expert's slots itself: at 512 slots as fast
+// as sorting them in a launch (306 us, 64 tokens over 128 experts of 4096 x 1536),
+// and with room for 1024 all calls take 3 to 8 % longer.
+constexpr int kBlockSlots = 256;
 
 __device__ __forceinline__ int expert_of(const int32_t *ids, int experts, int s) {
     const int e = ids[s];
