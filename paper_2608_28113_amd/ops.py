@@ -693,7 +693,7 @@ def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: t
     kind, ld = _logits(logits, "logits")
     T, E = logits.shape
     dev = logits.device
-    _no_graph("route_tokens", logits, grad=False)
+    _no_graph("route_tokens", logits, weight, grad=False)
     k = int(k)
     if not 1 <= k <= E:
         raise ValueError(f"k must be in 1 .. {E}, the number of experts")
@@ -704,8 +704,8 @@ def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: t
     return expert, weight
 
 
-def _expert_matrix(matrix, name: str, device, E: int, m: int, n: int) -> tuple[int, int, int]:
-    """The checked addresses of (global_scale, scale_codes, packed_e2m1) of E matrices of m x n."""
+def _expert_matrix(matrix, name: str, device, E: int, m: int, n: int) -> tuple[torch.Tensor, tuple[int, int, int]]:
+    """The checked (global_scale, scale_codes, packed_e2m1) of E matrices of m x n: the scales, and the addresses."""
     try:
         scale, codes, packed = matrix
         # One pass over what must hold: a call has nine of these tensors, and a token's time for them.
@@ -713,7 +713,7 @@ def _expert_matrix(matrix, name: str, device, E: int, m: int, n: int) -> tuple[i
                 and packed.shape == (E, m, n // 2) and codes.shape == (E, m, n // 16) and scale.shape == (E,)
                 and packed.device == device and codes.device == device and scale.device == device
                 and packed.is_contiguous() and codes.is_contiguous() and scale.is_contiguous()):
-            return scale.data_ptr(), codes.data_ptr(), packed.data_ptr()
+            return scale, (scale.data_ptr(), codes.data_ptr(), packed.data_ptr())
     except (TypeError, ValueError, AttributeError):
         raise ValueError(f"{name} must be three tensors (global_scale, scale_codes, packed_e2m1)") from None
     raise ValueError(f"{name} must be contiguous (global_scale fp32 [{E}], scale_codes uint8 [{E}, {m}, {n // 16}], "
@@ -740,7 +740,8 @@ def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, ga
     strided).
 
     The stored experts are frozen and no graph is recorded: tensors that require
-    a gradient are refused where torch would record one.
+    a gradient, the experts' scales among them, are refused where torch would
+    record one.
     """
     ldx = _rows_in(X, "X")
     T, n = X.shape
@@ -753,10 +754,10 @@ def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, ga
     if not isinstance(gate, (tuple, list)) or len(gate) != 3 or not isinstance(gate[2], torch.Tensor) or gate[2].dim() != 3:
         raise ValueError("gate must be (global_scale, scale_codes, packed_e2m1), the last uint8 [experts, hidden, in / 2]")
     E, hidden, _ = gate[2].shape
-    gate = _expert_matrix(gate, "gate", dev, E, hidden, n)
-    up = _expert_matrix(up, "up", dev, E, hidden, n)
-    down = _expert_matrix(down, "down", dev, E, n, hidden)
-    _no_graph("expert_layer", X, weight, grad=False)
+    gate_scale, gate = _expert_matrix(gate, "gate", dev, E, hidden, n)
+    up_scale, up = _expert_matrix(up, "up", dev, E, hidden, n)
+    down_scale, down = _expert_matrix(down, "down", dev, E, n, hidden)
+    _no_graph("expert_layer", X, weight, gate_scale, up_scale, down_scale, Y, grad=False)
     Y, ldy = _rows_out(Y, "Y", (T, n), dev, stream)
     need = expert_layer_workspace_bytes(T, n, hidden, E, k)
     ws_ptr, ws_bytes, held = _workspace(workspace, need, dev, stream)
@@ -818,7 +819,7 @@ def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, len
     kind, ld = _logits(logits, "logits")
     R, V = logits.shape
     dev = logits.device
-    _no_graph("adjust_logits", logits, repetition, frequency, presence, bias, grad=False)
+    _no_graph("adjust_logits", logits, repetition, frequency, presence, bias, out, grad=False)
     if history is None and not (length is None and prompt is None and repetition is None and frequency is None
                                 and presence is None):
         raise ValueError("repetition, frequency, presence, length and prompt need a history")
