@@ -17,6 +17,7 @@ still read them (torch.Tensor.record_stream).
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import HScaleError
@@ -429,7 +430,7 @@ CHECKPOINT_BLOCK = 128  # activations per checkpoint scale
 
 
 def _no_graph(where: str, *tensors, grad: bool = True) -> None:
-    """Refuses tensors whose gradient would be expected and lost: the calls record no graph."""
+    """Refuses tensors whose gradient or tangent would be expected and lost: the calls record no graph."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
@@ -438,6 +439,12 @@ def _no_graph(where: str, *tensors, grad: bool = True) -> None:
                                      "or with detached tensors")
                 raise ValueError(f"{where} records no graph: call it under torch.no_grad(), in an autograd function "
                                  f"or with detached tensors, and take the gradients from {where}_grad")
+    # Forward mode: no_grad leaves it on, an autograd function's forward turns it off.
+    if forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled():
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{where} would lose a tangent: call it with torch.autograd.forward_ad.unpack_dual's "
+                                 "primal, or in an autograd function with a jvp")
 
 
 def _rows_in(t, name: str) -> int:
@@ -741,7 +748,7 @@ def expert_layer(X: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, ga
 
     The stored experts are frozen and no graph is recorded: tensors that require
     a gradient, the experts' scales among them, are refused where torch would
-    record one.
+    record one, and tensors with a tangent where torch would carry it on.
     """
     ldx = _rows_in(X, "X")
     T, n = X.shape
