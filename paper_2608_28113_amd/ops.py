@@ -433,7 +433,7 @@ def _no_graph(where: str, *tensors, grad: bool = True) -> None:
     """Refuses tensors whose gradient or tangent would be expected and lost: the calls record no graph."""
     if torch.is_grad_enabled():
         for t in tensors:
-            if t is not None and t.requires_grad:
+            if isinstance(t, torch.Tensor) and t.requires_grad:
                 if not grad:
                     raise ValueError(f"{where} records no graph and has no gradient: call it under torch.no_grad() "
                                      "or with detached tensors")
@@ -442,7 +442,7 @@ def _no_graph(where: str, *tensors, grad: bool = True) -> None:
     # Forward mode: no_grad leaves it on, an autograd function's forward turns it off.
     if forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled():
         for t in tensors:
-            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
                 raise ValueError(f"{where} would lose a tangent: call it with torch.autograd.forward_ad.unpack_dual's "
                                  "primal, or in an autograd function with a jvp")
 

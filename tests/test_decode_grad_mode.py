@@ -72,3 +72,10 @@ def test_matrices_may_come_as_any_three(fake_gpu):  # noqa: F811
     gate, up, down = (tuple(a[m + f] for f in "scp") for m in "gud")
     with pytest.raises(Reached):
         ops.expert_layer(a["X"], a["expert"], a["weight"], gate, dict(zip("abc", up)).values(), iter(down), stream=0)
+
+
+@pytest.mark.parametrize("arg", ["repetition", "frequency", "presence", "bias", "out"])
+def test_numbers_in_place_of_tensors_are_refused(fake_gpu, arg):  # noqa: F811
+    f, good, _ = CASES["adjust_logits"]
+    with pytest.raises(ValueError):
+        f(**{**good(), arg: 1.5})
