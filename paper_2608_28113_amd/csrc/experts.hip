@@ -15,6 +15,7 @@
 // reads 6.9 TB/s and large bf16 products 1.4 to 1.5 PFLOP/s.
 
 #include "checks.h"
+#include "expert_plan.h"
 #include "matmul.h"
 #include "stored.h"
 
@@ -22,10 +23,6 @@
 
 namespace {
 
-constexpr int kMaxExperts = 1024;
-constexpr int kMaxChoices = 32;
-constexpr int64_t kMaxWidth = (int64_t)1 << 21;
-constexpr int64_t kMaxTokens = (int64_t)1 << 24;
 constexpr int kNoExpert = -1;
 
 // ---------------------------------------------------------------------------
@@ -124,20 +121,10 @@ __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ log
 // Which slots an expert has
 // ---------------------------------------------------------------------------
 
-// Up to so many, each block finds its expert's slots itself: at 512 slots as fast
-// as sorting them in a launch (306 us, 64 tokens over 128 experts of 4096 x 1536),
-// and with room for 1024 all calls take 3 to 8 % longer.
-constexpr int kBlockSlots = 256;
-
 __device__ __forceinline__ int expert_of(const int32_t *ids, int experts, int s) {
     const int e = ids[s];
     return e >= 0 && e < experts ? e : kNoExpert;
 }
-
-// Up to a block's slots of one expert; count 0: none.
-struct Share {
-    int expert, first, count;
-};
 
 // Many slots, sorted by expert once: a block of 1024 counts the slots of each
 // expert, adds the counts up and puts every slot at its place.  In which order
@@ -614,54 +601,6 @@ __global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, 
 // Host side
 // ---------------------------------------------------------------------------
 
-constexpr int kPieceSlots = 4096;  // a call of more goes piece by piece
-
-bool layer_sizes_ok(int64_t tokens, int64_t in, int64_t hidden, int32_t experts, int32_t k) {
-    return tokens >= 0 && tokens <= kMaxTokens && in >= 0 && in % kGroup == 0 && in <= kMaxWidth && hidden >= 0 &&
-           hidden % kGroup == 0 && hidden <= kMaxWidth && experts >= 1 && experts <= kMaxExperts && k >= 1 &&
-           k <= kMaxChoices;
-}
-
-// Tokens of a piece: its rows of X and of h are addressed in 32 bits, and its
-// sums take no more than h may.
-int64_t piece_tokens(int64_t in, int64_t hidden, int32_t k, int64_t ldx) {
-    int64_t n = kPieceSlots / k;
-    n = std::min(n, ((int64_t)1 << 29) / std::max<int64_t>(1, ldx));
-    return std::max<int64_t>(1, std::min(n, ((int64_t)1 << 28) / (std::max(in, hidden) * k)));
-}
-
-constexpr int kDownSplits = 16;
-constexpr int64_t kSplitBytes = (int64_t)32 << 20;  // of their sums, unless one takes more
-
-struct LayerSpace {
-    size_t h, p, order, shares, total;
-};
-
-LayerSpace layer_space(int64_t tokens, int64_t in, int64_t hidden, int32_t experts, int32_t k) {
-    const int64_t slots = std::min(tokens, piece_tokens(in, hidden, k, 1)) * k;
-    LayerSpace s{};
-    s.h = round_256((size_t)(slots * hidden * 4));
-    // Splits of few tokens are more: a bound that does not fall with the tokens.
-    s.p = round_256((size_t)std::min(slots * in * 4 * kDownSplits, std::max(slots * in * 4, kSplitBytes)));
-    s.order = round_256((size_t)slots * 4);
-    s.shares = round_256((size_t)(slots + experts) * sizeof(Share));
-    s.total = s.h + s.p + s.order + s.shares;
-    return s;
-}
-
-// Slots of a block: as many as an expert's share is likely to need.  us of the
-// whole call in blocks of 16, 32 and 64, for 32 experts of 2048 x 1024 with on
-// average
-//   9 slots   48.3  49.0  62.4       24 slots  67.0  59.0  65.7
-//   12 slots  52.4  49.4  63.0       32 slots  78.3  66.6  70.6
-//   16 slots  55.5  51.3  64.8       40 slots  88.5  76.9  72.6
-// and for 16 of 4096 x 1536 59.7, 69.6, 89.1 with 9 and 128, 101, 101 with 40.
-int slots_of_block(int64_t tokens, int64_t slots, int64_t experts) {
-    if (tokens <= 4) return 4;
-    if (tokens <= 16 || slots <= 10 * experts) return 16;
-    return tokens <= 32 || slots <= 34 * experts ? 32 : 64;
-}
-
 int check_matrix(const hscale_experts *w) {
     if (!w || !w->global_scale || !w->scale_codes || !w->packed_e2m1) return HSCALE_ERR_NULL;
     if (!aligned(w->global_scale, 4) || !aligned(w->packed_e2m1, 8)) return HSCALE_ERR_ALIGN;
@@ -677,26 +616,16 @@ int launch_experts(const ExpertArgs &a, int shares, int splits, hipStream_t stre
     return launch_status();
 }
 
-// A wave alone has its rows where they are many.  Where they are few, two waves
-// share them, or four where slots are many (us of the whole call, one, two and
-// four waves):
-//   1 token through 6 of 64 experts of 2048 x 1024     28.4  24.2  25.2
-//   12 tokens through 6 of 64 of 2048 x 1408           70.1  75.9  115
-//   48 tokens through 2 of 8 of 1024 x 1024            29.8  27.6  32.4
-//   75 tokens through 3 of 5 of 3152 x 848             67.5        56.7
-//   200 tokens through 2 of 8 of 1024 x 4096           58.4        109
-int gate_and_up(const ExpertArgs &a, int shares, int tile, hipStream_t stream) {
-    const int64_t units = cdiv(a.rows, 16) * shares, steps = cdiv(a.k, 256);
-    const bool two = units < 4096 && steps >= 2, four = cdiv(a.rows, 128) * shares < 128 && steps >= 4;
-    if (tile == 4 && two) return launch_experts<false, 4, 1, 2>(a, shares, 1, stream);
+int gate_and_up(const ExpertArgs &a, int shares, int tile, int waves, hipStream_t stream) {
+    if (tile == 4 && waves == 2) return launch_experts<false, 4, 1, 2>(a, shares, 1, stream);
     if (tile <= 16)
-        return two ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
-                   : launch_experts<false, 16, 1, 1>(a, shares, 1, stream);
+        return waves == 2 ? launch_experts<false, 16, 1, 2>(a, shares, 1, stream)
+                          : launch_experts<false, 16, 1, 1>(a, shares, 1, stream);
     if (tile == 32)
-        return four ? launch_experts<false, 32, 1, 4, 128>(a, shares, 1, stream)
-                    : launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
-    return four ? launch_experts<false, 64, 1, 4, 128>(a, shares, 1, stream)
-                : launch_experts<false, 64, 2, 1, 128>(a, shares, 1, stream);
+        return waves == 4 ? launch_experts<false, 32, 1, 4, 128>(a, shares, 1, stream)
+                          : launch_experts<false, 32, 1, 1>(a, shares, 1, stream);
+    return waves == 4 ? launch_experts<false, 64, 1, 4, 128>(a, shares, 1, stream)
+                      : launch_experts<false, 64, 2, 1, 128>(a, shares, 1, stream);
 }
 
 int down_product(const ExpertArgs &a, int shares, int tile, int splits, hipStream_t stream) {
@@ -704,18 +633,6 @@ int down_product(const ExpertArgs &a, int shares, int tile, int splits, hipStrea
     if (tile == 16) return launch_experts<true, 16, 1, 1>(a, shares, splits, stream);
     if (tile == 64) return launch_experts<true, 64, 2, 1, 128>(a, shares, splits, stream);
     return launch_experts<true, 32, 2, 1, 128>(a, shares, splits, stream);
-}
-
-// Splits of the down product's k, for `shares` shares of experts: two blocks a CU
-// (37 tokens over 8 experts of 4096 x 14336, 256 blocks: 192 us in two splits, 204
-// in one, 197 in four; one token over two of them, 64 blocks: 64 us in eight, 66 in
-// four, 110 in one).
-int down_splits(int64_t slots, int64_t in, int64_t hidden, int64_t shares) {
-    const int64_t steps = cdiv(hidden, 256), blocks = cdiv(in, 128) * shares;
-    int64_t n = cdiv(512, blocks);
-    n = std::min({n, steps, (int64_t)kDownSplits, std::max<int64_t>(1, kSplitBytes / (slots * in * 4))});
-    n = std::max<int64_t>(1, n);
-    return (int)cdiv(steps, cdiv(steps, n));
 }
 
 }  // namespace
@@ -801,18 +718,14 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
     float *P = reinterpret_cast<float *>(ws += space.h);
     int32_t *order = reinterpret_cast<int32_t *>(ws += space.p);
     Share *shares = reinterpret_cast<Share *>(ws + space.order);
-    const int64_t piece = piece_tokens(in, hidden, k, ldx);
-    for (int64_t t0 = 0; t0 < tokens; t0 += piece) {
-        const int64_t n = std::min(piece, tokens - t0);
-        const int slots = (int)(n * k);
+    const LayerPlan plan = plan_layer(tokens, in, hidden, experts, k, ldx);
+    for (int64_t t0 = 0; t0 < tokens; t0 += plan.piece) {
+        const int64_t n = std::min(plan.piece, tokens - t0);
+        const PiecePlan piece = plan_piece(plan, n, experts, k);
         const int32_t *ids = expert + t0 * k;
-        const int tile = slots_of_block(n, slots, experts);
-        int count = std::min(slots, (int)experts);
-        const bool many = slots > kBlockSlots;
-        if (many) {
-            count = std::min(slots, slots / tile + (int)experts);
-            hipLaunchKernelGGL(share_kernel, dim3(1), dim3(1024), 0, stream, ids, slots, (int)experts, tile,
-                               order, shares, count);
+        if (piece.many) {
+            hipLaunchKernelGGL(share_kernel, dim3(1), dim3(1024), 0, stream, ids, piece.slots, (int)experts, piece.tile,
+                               order, shares, piece.shares);
             if (const int st = launch_status()) return st;
         }
         ExpertArgs a{};
@@ -824,23 +737,22 @@ int hscale_expert_layer(const void *X, int64_t tokens, int64_t in, int64_t ldx, 
         a.in_bytes = (int64_t)span(n, ldx, in, 2);
         a.ids = ids;
         a.weight = weight + t0 * k;
-        a.slots = slots, a.choices = k, a.experts = experts;
-        a.order = many ? order : nullptr;
-        a.shares = many ? shares : nullptr;
+        a.slots = piece.slots, a.choices = k, a.experts = experts;
+        a.order = piece.many ? order : nullptr;
+        a.shares = piece.many ? shares : nullptr;
         a.H = H;
         a.P = P;
-        if (const int st = gate_and_up(a, count, tile, stream)) return st;
+        if (const int st = gate_and_up(a, piece.shares, piece.tile, plan.waves, stream)) return st;
         a.w[0] = a.w[1] = matrices(down);
         a.rows = in, a.k = hidden;
         a.in = H;
         a.ld = 2 * hidden;
-        a.in_bytes = (int64_t)slots * hidden * 4;
-        const int splits = down_splits(slots, in, hidden, count);
-        a.split = (int)cdiv(cdiv(hidden, 256), splits) * (tile >= 32 ? 2 : 1);
-        if (const int st = down_product(a, count, tile, splits, stream)) return st;
+        a.in_bytes = (int64_t)piece.slots * hidden * 4;
+        a.split = plan.split * (piece.tile >= 32 ? 2 : 1);  // steps of 128 there
+        if (const int st = down_product(a, piece.shares, piece.tile, plan.splits, stream)) return st;
         uint16_t *y = static_cast<uint16_t *>(Y) + t0 * ldy;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 1024), (unsigned)n), dim3(256), 0, stream, P, splits,
-                           (int64_t)slots, ids, a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 8) && ldy % 4 == 0);
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)cdiv(in, 1024), (unsigned)n), dim3(256), 0, stream, P, plan.splits,
+                           (int64_t)piece.slots, ids, a.weight, (int)k, (int)experts, in, y, ldy, aligned(y, 8) && ldy % 4 == 0);
         if (const int st = launch_status()) return st;
     }
     return HSCALE_OK;
