@@ -26,7 +26,10 @@ constexpr int kPieceSlots = 4096;  // a call of more goes piece by piece
 
 // Up to so many, each block finds its expert's slots itself: at 512 slots as fast
 // as sorting them in a launch (306 us, 64 tokens over 128 experts of 4096 x 1536),
-// and with room for 1024 all calls take 3 to 8 % longer.
+// and with room for 1024 all calls take 3 to 8 % longer.  One column of blocks
+// then takes all slots of an expert, a tile after the other: 128 tokens over 2 of
+// 8 experts of 4096 x 14336 take 371 us, 429 where all choose the same two, and
+// 129 tokens, sorted, 324 and 281.
 constexpr int kBlockSlots = 256;
 
 // Up to a block's slots of one expert; count 0: none.
@@ -85,16 +88,24 @@ inline int shares_of(int64_t slots, int tile, int32_t experts) {
 }
 
 // Waves of gate and up that share their rows.  A wave alone has its rows where
-// they are many.  Where they are few, two waves share them, or four where slots
-// are many (us of the whole call, one, two and four waves):
+// they are many.  Where they are few, two waves share them, or four in blocks of
+// 32 and 64 slots.  us of the whole call, one, two and four waves:
 //   1 token through 6 of 64 experts of 2048 x 1024     28.4  24.2  25.2
 //   12 tokens through 6 of 64 of 2048 x 1408           70.1  75.9  115
-//   48 tokens through 2 of 8 of 1024 x 1024            29.8  27.6  32.4
-//   75 tokens through 3 of 5 of 3152 x 848             67.5        56.7
-//   200 tokens through 2 of 8 of 1024 x 4096           58.4        109
+// Blocks of four waves take 16 rows: 512 of them, two a CU, are one round of 32
+// slots.  More are two, and one wave alone is faster by then.  Blocks of 64
+// slots have a CU each, and a few rounds of them still gain where k is long.
+// In a graph, one and four waves, `u` rows / 128 x shares:
+//   32 slots  in 1024  u 64  26.5  26.5     64 slots  in 1040  u 49  45.7  46.2
+//             in 1040  u 64  28.2  26.9               in 1536  u 80  50.5  47.0
+//             in 4096  u 64  42.1  35.9               in 2048  u 98  56.0  48.8
+//             in 1040  u 66  29.2  32.4               in 4096  u 99  91.0  89.1
+//             in 4096  u 66  44.7  46.4               in 2048 u 110  57.8  69.8
+//             in 4096 u 110  52.9  61.1               in 4096 u 110  91.6   105
 inline int waves_of_row(int64_t in, int64_t hidden, int shares, int tile) {
-    if (tile <= 16) return cdiv(hidden, 16) * shares < 4096 && cdiv(in, 256) >= 2 ? 2 : 1;
-    return cdiv(hidden, 128) * shares < 128 && cdiv(in, 256) >= 4 ? 4 : 1;
+    const int64_t u = cdiv(hidden, 128) * shares, steps = cdiv(in, 256);
+    if (tile <= 16) return cdiv(hidden, 16) * shares < 4096 && steps >= 2 ? 2 : 1;
+    return (tile == 32 ? u <= 64 && steps >= 4 : u <= 100 && steps >= 6) ? 4 : 1;
 }
 
 // Splits of the down product's k, for `shares` shares of experts: two blocks a CU

@@ -3,6 +3,8 @@
 // workspace that is meant for it, every token has a piece and every step of k a
 // split, all pieces of a call add in one order, and what the kernels address in
 // 32 bits and launch in one dimension fits.
+// With an argument: reads calls from standard input, TOKENS IN HIDDEN EXPERTS K
+// a line, and prints the ways they take, one of a kernel a word.
 #include <cstdio>
 #include <cstdlib>
 
@@ -52,7 +54,25 @@ static void call_holds(int64_t tokens, int64_t in, int64_t hidden, int experts, 
     HOLDS(near.waves == p.waves && near.splits == p.splits && near.split == p.split && near.piece >= p.piece);
 }
 
-int main() {
+static void ways(int64_t tokens, int64_t in, int64_t hidden, int experts, int k) {
+    const LayerPlan p = plan_layer(tokens, in, hidden, experts, k, in);
+    for (int64_t n : {p.piece, tokens % p.piece}) {
+        if (n == 0) continue;
+        const PiecePlan q = plan_piece(p, n, experts, k);
+        const int gate = q.tile == 4 && p.waves == 1 ? 16 : q.tile;  // four slots alone are built for two waves
+        std::printf("slots:%s gate:%d:%d down:%d:%s ", q.many ? "sorted" : experts < q.slots ? "found" : "found-by-slot", gate,
+                    p.waves, q.tile, p.splits > 1 ? "split" : "whole");
+    }
+    std::printf("\n");
+}
+
+int main(int argc, char **) {
+    if (argc > 1) {
+        long long t, in, hidden;
+        int e, k;
+        while (std::scanf("%lld %lld %lld %d %d", &t, &in, &hidden, &e, &k) == 5) ways(t, in, hidden, e, k);
+        return 0;
+    }
     const int64_t widths[] = {16, 32, 48, 112, 256, 272, 528, 1024, 1040, 2048, 4096, 14336, 1 << 16, (1 << 20) + 16, 1 << 21};
     const int64_t counts[] = {1, 2, 3, 4, 5, 12, 16, 17, 32, 33, 64, 100, 127, 128, 129, 255, 256, 257, 341, 342, 512, 682,
                               683, 1023, 1024, 1025, 2048, 2100, 4095, 4096, 4097, 5000, 8192, 8193, 100001, 1 << 24};

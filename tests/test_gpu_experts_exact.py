@@ -68,7 +68,7 @@ def _on_gpu(*matrices):
 
 SMALL = [c for c in SIZES + ROUTES if c[1] * c[2] * c[3] < 10 ** 8]
 WIDE = [(1, 2048, 1024, 7, 6), (3, 1024, 2064, 3, 2), (12, 2048, 1424, 9, 6), (64, 1024, 1536, 9, 8), (37, 1040, 3088, 4, 2),
-        (300, 2048, 1024, 9, 6), (300, 2048, 528, 4, 4)]
+        (300, 2048, 1024, 9, 6), (300, 2048, 528, 4, 4), (300, 2048, 272, 8, 2), (75, 3152, 848, 5, 3), (40, 2048, 528, 4, 2)]
 
 
 @pytest.mark.parametrize("T,n,hidden,E,k", SMALL + WIDE)

@@ -13,7 +13,7 @@ pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(),
 # last piece short enough that alone it would take another tile, other waves a
 # row or other splits of the down product.
 CALLS = [(2100, 2048, 2048, 8, 2), (683, 2048, 1024, 64, 6), (686, 1040, 1024, 5, 6), (4097, 528, 1296, 3, 1),
-         (2051, 1296, 528, 2, 2), (130, 528, 1040, 9, 32)]
+         (2051, 1296, 528, 2, 2), (130, 528, 1040, 9, 32), (2100, 2048, 128, 5, 2), (2100, 528, 64, 500, 2)]
 
 
 @pytest.mark.parametrize("T,n,hidden,E,k", CALLS)
