@@ -618,7 +618,10 @@ int hscale_route_tokens(const void *logits, int32_t type, int64_t tokens, int32_
 /*
  * One matrix of every expert, stored as hscale_search or hscale_quantize store
  * a layer, one after another.  The scales lie on the device and are not
- * checked: each in the range that hscale_search accepts.
+ * checked: each global scale in the range that hscale_search accepts, each code
+ * in 0 .. 126.  Codes are read in whole aligned words of 4 bytes: up to three
+ * bytes on either side of the array are read too and change nothing, whatever
+ * they hold.
  */
 typedef struct hscale_experts {
     const float *global_scale;  /* fp32 [experts] */

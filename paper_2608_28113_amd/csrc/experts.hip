@@ -61,9 +61,10 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // A wave per token, kN logits a lane.  k rounds of the wave's largest key, each
-// taken out where it first lies; the softmax is relative to the first.  Latency
-// bounds it: 48 tokens of 64 experts take 2.9 us, 8190 of 160 7.1
-// (4.3 and 13.7 with the largest key by shuffles of 64 bits).
+// taken out where it first lies; the softmax is relative to the first.  48
+// tokens of 64 experts take 2.8 us, a launch; 8190 of 160 6.9, bound by vector
+// instructions: 370 a wave, eight waves a SIMD, are 4.9 us of issue (4.3 and
+// 13.7 us with the largest key by shuffles of 64 bits).
 template <int kN, bool kWide>
 __global__ __launch_bounds__(256) void route_kernel(const void *__restrict__ logits, int64_t tokens, int experts,
                                                     int64_t ld, int k, bool normalize, int32_t *__restrict__ expert,
@@ -278,10 +279,10 @@ __device__ __forceinline__ void own_writes_and_barrier() {  // loads stay under 
 // Reading the weights bounds it while slots are few: 64 tokens over 128 experts
 // of 4096 x 1536 take 178 and 120 us, 5.1 and 3.8 TB/s; 37 over 8 of 4096 x 14336
 // 109 and 69, 4.9 and 3.8; one token over two of these 33 and 20, 4.0 and 3.4.
-// With many the conversion of the weights, the products and the loads each keep
-// a third of the time and two waves a SIMD overlap them only in part: 512 tokens
-// over 64 experts of 2048 x 1024, 48 slots each, 57 and 48 us (MFMA 0.21, VALU
-// 0.35 busy).  Four sets of weights under way in place of two measured equal
+// With many it is the loads' return path, 0.62 and 0.57 busy, beside the
+// conversion of the weights (VALU 0.36 and 0.24) and the products (MFMA 0.21 and
+// 0.25), which two waves a SIMD overlap only in part: 512 tokens over 64 experts
+// of 2048 x 1024, 48 slots each, 57 and 48 us.  Four sets of weights under way in place of two measured equal
 // there, 256 k of weights with 128 of the rows 138 us a call for 130.
 //
 // A wave's operand of weights comes straight from memory, 32 consecutive weights

@@ -1,7 +1,7 @@
 // What a request's rules change its logits by before a token is chosen, behind
 // the C ABI of include/hscale.h:
 //
-//   l = l > 0 ? l / r : l r        of words in the history
+//   l = l > 0 ? l (1 / r) : l r    of words in the history
 //   l = l - f count - p            of words in the answer
 //   l = l + bias,  l = -inf        where the mask forbids a word
 //

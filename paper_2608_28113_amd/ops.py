@@ -694,8 +694,9 @@ def route_tokens(logits: torch.Tensor, k: int, normalize: bool = True, expert: t
 
     A logit of -inf or NaN is never chosen; a token with fewer than k others
     gets -1 and weight 0 for the rest.  NaN or +inf among a token's logits make
-    its weights NaN.  No graph is recorded: logits that require a gradient are
-    refused where torch would record one.
+    its weights NaN.  No graph is recorded: tensors that require a gradient are
+    refused where torch would record one, and tensors with a tangent where torch
+    would carry it on.
     """
     kind, ld = _logits(logits, "logits")
     T, E = logits.shape
@@ -813,15 +814,15 @@ def adjust_logits(logits: torch.Tensor, history: torch.Tensor | None = None, len
     history is int32 [rows, any length] (rows may be strided), of which the first
     length[row] words count (all when None) and the first prompt[row] of those
     are the prompt's, the rest the answer's (all when None); words outside the
-    vocabulary are passed over.  repetition (> 0), frequency and presence are
-    fp32 [rows].  bias is fp32 [biases, vocab], mask int32 [masks,
+    vocabulary are passed over.  repetition (normal, > 0), frequency and presence
+    are fp32 [rows].  bias is fp32 [biases, vocab], mask int32 [masks,
     ceil(vocab / 32)] whose bit v % 32 of number v / 32 allows word v; bias_row
     and mask_row (int32 [rows]) say which row uses which, any number outside
     for none; with exactly one they may be None: all rows use it.
 
     Returns `out`, new when None; out=logits works in place.  No graph is
     recorded: tensors that require a gradient are refused where torch would
-    record one.
+    record one, and tensors with a tangent where torch would carry it on.
     """
     kind, ld = _logits(logits, "logits")
     R, V = logits.shape
