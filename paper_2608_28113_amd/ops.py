@@ -516,7 +516,8 @@ def adapted_linear(X: torch.Tensor, global_scale: float, scale_codes: torch.Tens
     0 .. adapters - 1 means none; with one adapter it may be None: all use it.
 
     No graph is recorded: tensors that require a gradient are refused where
-    torch would record one (adapted_linear_grad returns the gradients).
+    torch would record one (adapted_linear_grad returns the gradients), and
+    tensors with a tangent where torch would carry it on.
     """
     ldx = _rows_in(X, "X")
     T, n = X.shape
@@ -624,7 +625,8 @@ def token_loss(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: tor
     (rows may be strided), W bf16 [vocab, d], target int64 [tokens]; a target
     outside 0 .. vocab - 1 is not scored (loss 0).  Tensors that require a
     gradient are refused where torch would record a graph (token_loss_grad
-    returns the gradients)."""
+    returns the gradients), and tensors with a tangent where torch would carry
+    it on."""
     ldx = _rows_in(X, "X")
     T, d = X.shape
     dev = X.device
